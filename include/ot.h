@@ -385,6 +385,112 @@ ot_status ot_qlinear_packed(const int8_t *Xq, const int8_t *Wp, const float *sW,
                             int a_bits, int w_bits, uint16_t *Y,
                             int32_t *acc_out, void *workspace, void *stream);
 
+/*
+ * MX4: microscaled 4-bit floating point, for linears whose weights and
+ * activations both take 4 bits.  A block of 32 consecutive input channels
+ * holds an 8-bit scale byte b, worth 2^(b-127), and 32 4-bit codes: the sign
+ * (bit 3) and one of the levels 0, 0.5, 1, 1.5, 2, 3, 4, 6 (bits 0..2).  With
+ * E the exponent field of the largest fp32 magnitude in the block,
+ *   b    = max(E - 2, 0), or 255 where E = 255
+ *   code = the level nearest to |v| 2^(127-b), ties to the even code, 6 where
+ *          that is larger; the sign is v's
+ * A block with a NaN or an infinity has b = 255 and stands for 32 NaNs (its
+ * codes are 0); every product with it is NaN.
+ *
+ * Codes and scales of a matrix [rows x K], K a multiple of 32:
+ *   c  [rows x K/2] uint8, channel 2j in the low half of byte j, 2j+1 in the
+ *      high half;
+ *   e  [ceil(K/256) x rows x 8] uint8: e[t][row][i] is the scale of the row's
+ *      block 8t + i, 0 past K.
+ *
+ * The per-channel shift and scale of Eq. (g) are kept: the activations are
+ * symmetrized and scaled per channel before their blocks are formed, the scale
+ * is folded into the weights and the shift into the bias, so that a channel
+ * with outliers does not take its block's other channels' resolution.
+ *
+ * For all mx4 entry points: 32 <= K <= 2^22, K % 32 == 0 (OT_ESHAPE), rows
+ * below 2^31, pointers 16-byte aligned (OT_EINVAL).
+ *
+ * ot_quantize_act_mx4 -- runtime activations:
+ *   v[m,k] = fp32(fp32(fp32(x[m,k]) - z_k) * inv_s_k), each rounded to nearest
+ *   even; z and inv_s both NULL: v = x.
+ *   x [M x K] fp16, z, inv_s [K] fp32 or NULL (device); Xc, Xe outputs (device).
+ *   M >= 0 (0 is a no-op).  Asynchronous on stream.
+ */
+ot_status ot_quantize_act_mx4(const uint16_t *x, int64_t M, int64_t K,
+                              const float *z, const float *inv_s, uint8_t *Xc,
+                              uint8_t *Xe, void *stream);
+
+/*
+ * ot_ln_quantize_act_mx4 -- the LayerNorm fused with the MX4 quantizer:
+ *   v[m,k] = ((((h - fp32(mean)) * fp32(rstd)) * gamma_k + (beta_k - z_k)) * inv_s_k)
+ * in fp32 rounded to nearest even (no fused multiply-add), with mean and rstd
+ * as defined for ot_ln_quantize_act.  Arguments as there (K <= 65536), outputs
+ * as ot_quantize_act_mx4; M < 2^22 (OT_ESHAPE).  Asynchronous on stream.
+ */
+ot_status ot_ln_quantize_act_mx4(const uint16_t *h, int64_t M, int64_t K,
+                                 const uint16_t *gamma, const uint16_t *beta,
+                                 float eps, const float *z, const float *inv_s,
+                                 uint8_t *Xc, uint8_t *Xe, void *stream);
+
+/*
+ * ot_fold_weights_mx4 -- the offline transform of a layer's weights:
+ *   v[n,k] = fp32(W[n,k] s_k)  (s NULL: W[n,k])
+ *   bprime[n] = fp32(sum_k z_k W[n,k] + b_n)  (fp64; z NULL: b_n alone)
+ *   W [N x K] fp16, b [N] fp16 or NULL, z, s [K] fp32 or NULL (device).
+ *   Wc, We, bprime [N] fp32 outputs (device).  N >= 1.
+ * Synchronous.  OT_ENONFINITE if a weight, a product with s or a bias is NaN or
+ * infinite; then the outputs are unspecified.
+ */
+ot_status ot_fold_weights_mx4(const uint16_t *W, const uint16_t *b, int64_t N,
+                              int64_t K, const float *z, const float *s,
+                              uint8_t *Wc, uint8_t *We, float *bprime,
+                              void *stream);
+
+/*
+ * ot_dequantize_mx4 -- the fp32 values that codes and scales stand for (exact;
+ * NaN where the scale byte is 255).  c, e [rows x K] in MX4, y [rows x K] fp32
+ * (device).  rows >= 0 (0 is a no-op).  Asynchronous on stream.
+ */
+ot_status ot_dequantize_mx4(const uint8_t *c, const uint8_t *e, int64_t rows,
+                            int64_t K, float *y, void *stream);
+
+/*
+ * Packed MX4 weights: the order in which the products read them, laid out
+ * once.  With T = ceil(K/256) and B = ceil(N/32), first the codes
+ *   Wp[b][t][s][h][r][0..15] = the 16 bytes of block 8t + 4h + s of row 32b + r
+ * for b < B, t < T, s < 4, h < 2, r < 32, then the scales
+ *   We[t][32b + r][4h + s] at [t][b][h][r][s],
+ * zeros past N and K.
+ * ot_packed_weights_mx4_size -- its bytes, 4352 T B (0 for sizes that
+ *   ot_pack_weights_mx4 rejects).  No device work.
+ * ot_pack_weights_mx4 -- Wc, We (device) -> Wp (device).  N >= 1.
+ *   Asynchronous on stream.
+ */
+size_t ot_packed_weights_mx4_size(int64_t N, int64_t K);
+ot_status ot_pack_weights_mx4(const uint8_t *Wc, const uint8_t *We, int64_t N,
+                              int64_t K, uint8_t *Wp, void *stream);
+
+/*
+ * ot_qlinear_mx4 -- the linear on MX4 operands:
+ *   Y[m,n] = fp16(fp32(sum_k x[m,k] w[n,k]) + bprime_n)
+ * with the values that the codes stand for; their products are exact, the sum
+ * is in fp32 (its order is fixed for given sizes and unspecified).
+ *   Xc, Xe [M x K] and Wp of ot_pack_weights_mx4 for N x K, bprime [N] fp32
+ *   (device).  M >= 0 (0 is a no-op), 1 <= N < 2^26.
+ *   Y  [M x N] fp16 output (device).
+ *   workspace  NULL, or at least ot_qlinear_mx4_workspace_size(M, N, K) bytes of
+ *           scratch as for ot_qlinear.  Calls that overlap in time must not
+ *           share one.
+ * Asynchronous on stream; no synchronization, no allocation.
+ */
+ot_status ot_qlinear_mx4(const uint8_t *Xc, const uint8_t *Xe, const uint8_t *Wp,
+                         const float *bprime, int64_t M, int64_t N, int64_t K,
+                         uint16_t *Y, void *workspace, void *stream);
+/* Bytes of optional scratch that ot_qlinear_mx4 can use for these sizes on the
+ * current device (0 if none, and for sizes it rejects).  No device work. */
+size_t ot_qlinear_mx4_workspace_size(int64_t M, int64_t N, int64_t K);
+
 #ifdef __cplusplus
 }
 #endif

@@ -9,7 +9,7 @@
 #include <mutex>
 #include <vector>
 
-#include "ot_common.h"
+#include "ot_mx4.h"
 
 namespace {
 
@@ -22,6 +22,12 @@ constexpr int64_t kMaxRows = (int64_t(1) << 31) - 1;
 // are a 32-bit count are refused (the launcher leaves a smaller tile out where
 // its own grid does not fit).
 bool grid_ok(int64_t M, int64_t N) { return (M + 127) / 128 * ((N + 255) / 256) <= kMaxRows; }
+
+// MX4: the largest LayerNorm and linear whose workgroups fit a launch (fewer than
+// 2^32 work-items, 1024 of them to a row or to 16 channels).
+constexpr int64_t kMaxLnMx4Rows = (int64_t(1) << 22) - 1;
+constexpr int64_t kMaxMx4N = (int64_t(1) << 26) - 1;
+bool mx4_k_ok(int64_t K) { return K >= 32 && K % 32 == 0 && K <= ot::kMx4MaxK; }
 
 bool bits_ok(int bits) { return bits >= 2 && bits <= 8; }
 int qmax(int bits) { return (1 << (bits - 1)) - 1; }
@@ -393,6 +399,90 @@ ot_status ot_qlinear_plan(int64_t M, int64_t N, int64_t K, int packed, int with_
 size_t ot_qlinear_workspace_size(int64_t M, int64_t N, int64_t K) {
   if (M <= 0 || N <= 0 || K <= 0 || M > kMaxRows || N > kMaxRows || K > kMaxK) return 0;
   return ot::qgemm_workspace_bytes(M, N, K);
+}
+
+ot_status ot_quantize_act_mx4(const uint16_t *x, int64_t M, int64_t K, const float *z,
+                              const float *inv_s, uint8_t *Xc, uint8_t *Xe, void *stream) {
+  if (M < 0 || K < 0) return OT_EINVAL;
+  if (!mx4_k_ok(K) || M > kMaxRows) return OT_ESHAPE;
+  if (M == 0) return OT_OK;
+  if (!x || !Xc || !Xe || (z == nullptr) != (inv_s == nullptr)) return OT_EINVAL;
+  if (!aligned16(x) || !aligned16(z) || !aligned16(inv_s) || !aligned16(Xc) || !aligned16(Xe))
+    return OT_EINVAL;
+  return hip_status(
+      ot::launch_quantize_act_mx4(x, M, K, z, inv_s, Xc, Xe, static_cast<hipStream_t>(stream)));
+}
+
+ot_status ot_ln_quantize_act_mx4(const uint16_t *h, int64_t M, int64_t K, const uint16_t *gamma,
+                                 const uint16_t *beta, float eps, const float *z,
+                                 const float *inv_s, uint8_t *Xc, uint8_t *Xe, void *stream) {
+  if (M < 0 || K < 0 || !(eps >= 0.f) || eps > 3.4e38f) return OT_EINVAL;
+  if (!mx4_k_ok(K) || K > kMaxLnK || M > kMaxLnMx4Rows) return OT_ESHAPE;
+  if (M == 0) return OT_OK;
+  if (!h || !gamma || !beta || !z || !inv_s || !Xc || !Xe) return OT_EINVAL;
+  if (!aligned16(h) || !aligned16(gamma) || !aligned16(beta) || !aligned16(z) ||
+      !aligned16(inv_s) || !aligned16(Xc) || !aligned16(Xe))
+    return OT_EINVAL;
+  return hip_status(ot::launch_ln_quantize_act_mx4(h, M, K, gamma, beta, eps, z, inv_s, Xc, Xe,
+                                                   static_cast<hipStream_t>(stream)));
+}
+
+ot_status ot_fold_weights_mx4(const uint16_t *W, const uint16_t *b, int64_t N, int64_t K,
+                              const float *z, const float *s, uint8_t *Wc, uint8_t *We,
+                              float *bprime, void *stream) {
+  if (N < 0 || K < 0) return OT_EINVAL;
+  if (N == 0 || !mx4_k_ok(K) || N > kMaxRows) return OT_ESHAPE;
+  if (!W || !Wc || !We || !bprime) return OT_EINVAL;
+  if (!aligned16(W) || !aligned16(z) || !aligned16(s) || !aligned16(Wc) || !aligned16(We))
+    return OT_EINVAL;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  StatusWord status(st);
+  const hipError_t e = ot::launch_fold_mx4(W, b, N, K, z, s, Wc, We, bprime, status.word(), st);
+  return fold_result(e, status, bprime, bprime, N, st);  // a row's NaN b' marks it
+}
+
+ot_status ot_dequantize_mx4(const uint8_t *c, const uint8_t *e, int64_t rows, int64_t K, float *y,
+                            void *stream) {
+  if (rows < 0 || K < 0) return OT_EINVAL;
+  if (!mx4_k_ok(K) || rows > kMaxRows) return OT_ESHAPE;
+  if (rows == 0) return OT_OK;
+  if (!c || !e || !y || !aligned16(c) || !aligned16(e) || !aligned16(y)) return OT_EINVAL;
+  return hip_status(ot::launch_dequantize_mx4(c, e, rows, K, y, static_cast<hipStream_t>(stream)));
+}
+
+size_t ot_packed_weights_mx4_size(int64_t N, int64_t K) {
+  if (N <= 0 || !mx4_k_ok(K) || N > kMaxRows) return 0;
+  return ot::mx4_packed_bytes(N, K);
+}
+
+ot_status ot_pack_weights_mx4(const uint8_t *Wc, const uint8_t *We, int64_t N, int64_t K,
+                              uint8_t *Wp, void *stream) {
+  if (N < 0 || K < 0) return OT_EINVAL;
+  if (N == 0 || !mx4_k_ok(K) || N > kMaxRows) return OT_ESHAPE;
+  if (!Wc || !We || !Wp || !aligned16(Wc) || !aligned16(We) || !aligned16(Wp)) return OT_EINVAL;
+  return hip_status(
+      ot::launch_pack_weights_mx4(Wc, We, N, K, Wp, static_cast<hipStream_t>(stream)));
+}
+
+ot_status ot_qlinear_mx4(const uint8_t *Xc, const uint8_t *Xe, const uint8_t *Wp,
+                         const float *bprime, int64_t M, int64_t N, int64_t K, uint16_t *Y,
+                         void *workspace, void *stream) {
+  if (M < 0 || N < 0 || K < 0) return OT_EINVAL;
+  if (N == 0 || !mx4_k_ok(K) || M > kMaxRows || N > kMaxMx4N || !ot::mx4_gemm_fits(M, N))
+    return OT_ESHAPE;
+  if (M == 0) return OT_OK;
+  if (!Xc || !Xe || !Wp || !bprime || !Y) return OT_EINVAL;
+  if (!aligned16(Xc) || !aligned16(Xe) || !aligned16(Wp) || !aligned16(bprime) || !aligned16(Y) ||
+      !aligned16(workspace))
+    return OT_EINVAL;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  return hip_status(M <= 64 ? ot::launch_mx4_decode(Xc, Xe, Wp, bprime, M, N, K, Y, st)
+                            : ot::launch_mx4_gemm(Xc, Xe, Wp, bprime, M, N, K, Y, st));
+}
+
+size_t ot_qlinear_mx4_workspace_size(int64_t M, int64_t N, int64_t K) {
+  (void)M; (void)N; (void)K;
+  return 0;
 }
 
 }  // extern "C"

@@ -36,7 +36,7 @@
 // from the statistics to the normalize pass (one HBM read).
 // The per-channel gamma, beta - z and inv_s (L2-resident) are read once per
 // chunk and applied to all R rows.
-#include "ot_common.h"
+#include "ot_mx4.h"
 
 namespace ot {
 namespace detail {
@@ -128,11 +128,14 @@ __device__ inline u128 wave_sum_u128(u128 v) {
   return v;
 }
 
-template <int CPT, int R, int MAXT>
+// MX4 false: int8 codes in Xq.  MX4 true: u = y * inv_s_k in blocks of 32, codes
+// and scales in Xq and Xe (qa unused).
+template <int CPT, int R, int MAXT, bool MX4>
 __global__ __launch_bounds__(MAXT) void ln_quantize_kernel(
     const uint16_t *__restrict__ h, int64_t M, int K, const uint16_t *__restrict__ gamma,
     const uint16_t *__restrict__ beta, double eps, double inv_k, float qa,
-    const float *__restrict__ z, const float *__restrict__ inv_s, int8_t *__restrict__ Xq) {
+    const float *__restrict__ z, const float *__restrict__ inv_s, int8_t *__restrict__ Xq,
+    uint8_t *__restrict__ Xe) {
   __shared__ double red[2][16][R];  // per wave partial sums of d and d^2
   const int T = blockDim.x;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, nwaves = T >> 6;
@@ -281,6 +284,49 @@ __global__ __launch_bounds__(MAXT) void ln_quantize_kernel(
 #pragma unroll
   for (int j = 0; j < CPT; ++j) {
     const int ch = t + j * T;
+    if constexpr (MX4) {
+      // whole waves up to the end of the last K tile: its scales are written,
+      // and a block's lanes meet, past K too
+      if ((ch & ~63) * 8 >= (K + kMx4Tile - 1) / kMx4Tile * kMx4Tile) continue;
+      const bool in = ch < nchunks;
+      float g[8] = {}, c[8] = {}, is[8] = {};
+      if (in) {
+        const uint4 gv = *reinterpret_cast<const uint4 *>(gamma + ch * 8);
+        const uint4 bv = *reinterpret_cast<const uint4 *>(beta + ch * 8);
+        const uint32_t gw[4] = {gv.x, gv.y, gv.z, gv.w}, bw[4] = {bv.x, bv.y, bv.z, bv.w};
+#pragma unroll
+        for (int e = 0; e < 8; e += 4) {
+          const float4 zz = *reinterpret_cast<const float4 *>(z + ch * 8 + e);
+          const float4 ii = *reinterpret_cast<const float4 *>(inv_s + ch * 8 + e);
+          g[e] = half_lo(gw[e >> 1]);
+          g[e + 1] = half_hi(gw[e >> 1]);
+          g[e + 2] = half_lo(gw[(e >> 1) + 1]);
+          g[e + 3] = half_hi(gw[(e >> 1) + 1]);
+          c[e] = half_lo(bw[e >> 1]) - zz.x;
+          c[e + 1] = half_hi(bw[e >> 1]) - zz.y;
+          c[e + 2] = half_lo(bw[(e >> 1) + 1]) - zz.z;
+          c[e + 3] = half_hi(bw[(e >> 1) + 1]) - zz.w;
+          is[e] = ii.x; is[e + 1] = ii.y; is[e + 2] = ii.z; is[e + 3] = ii.w;
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        if (row0 + r >= M) continue;
+        const uint32_t w[4] = {x[r][j].x, x[r][j].y, x[r][j].z, x[r][j].w};
+        float u[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float hv = (e & 1) ? half_hi(w[e >> 1]) : half_lo(w[e >> 1]);
+          const float d = hv - mu32[r];
+          const float n = d * r32[r];
+          const float gg = n * g[e];
+          const float y = gg + c[e];
+          u[e] = in ? y * is[e] : 0.f;
+        }
+        mx4_store8(u, row0 + r, M, K, (int64_t)ch * 8, lane, reinterpret_cast<uint8_t *>(Xq), Xe);
+      }
+      continue;
+    }
     if (ch >= nchunks) continue;
     const uint4 gv = *reinterpret_cast<const uint4 *>(gamma + ch * 8);
     const uint4 bv = *reinterpret_cast<const uint4 *>(beta + ch * 8);
@@ -326,27 +372,24 @@ __global__ __launch_bounds__(MAXT) void ln_quantize_kernel(
 }
 
 // MAXT bounds the workgroup (and so frees registers for larger CPT)
-template <int CPT, int R, int MAXT = 1024>
+template <int CPT, int R, bool MX4, int MAXT = 1024>
 hipError_t launch_lnq(const uint16_t *h, int64_t M, int64_t K, const uint16_t *gamma,
                       const uint16_t *beta, float eps, int qa, const float *z, const float *inv_s,
-                      int8_t *Xq, hipStream_t st) {
+                      int8_t *Xq, uint8_t *Xe, hipStream_t st) {
   static_assert(MAXT % 64 == 0 && MAXT <= 1024, "workgroup size");
   const int64_t nchunks = K / 8;
   const int threads = (int)((nchunks + CPT * 64 - 1) / (CPT * 64)) * 64;
   if (threads > MAXT) return hipErrorInvalidValue;
   const unsigned grid = (unsigned)((M + R - 1) / R);
-  ln_quantize_kernel<CPT, R, MAXT><<<grid, threads, 0, st>>>(
-      h, M, (int)K, gamma, beta, (double)eps, 1.0 / (double)K, (float)qa, z, inv_s, Xq);
+  ln_quantize_kernel<CPT, R, MAXT, MX4><<<grid, threads, 0, st>>>(
+      h, M, (int)K, gamma, beta, (double)eps, 1.0 / (double)K, (float)qa, z, inv_s, Xq, Xe);
   return hipGetLastError();
 }
 
-}  // namespace detail
-
-using namespace detail;
-
-hipError_t launch_ln_quantize_act(const uint16_t *h, int64_t M, int64_t K, const uint16_t *gamma,
-                                  const uint16_t *beta, float eps, int qa, const float *z,
-                                  const float *inv_s, int8_t *Xq, hipStream_t st) {
+template <bool MX4>
+hipError_t launch_ln(const uint16_t *h, int64_t M, int64_t K, const uint16_t *gamma,
+                     const uint16_t *beta, float eps, int qa, const float *z, const float *inv_s,
+                     int8_t *Xq, uint8_t *Xe, hipStream_t st) {
   // Two rows per workgroup for wide rows and many of them (140000 elements per
   // CU: 36 M on 256 CUs).  A row reads 12 bytes of parameters from the L2 per
   // channel beside its own 2, and two rows share them; each thread's chunks are
@@ -364,11 +407,11 @@ hipError_t launch_ln_quantize_act(const uint16_t *h, int64_t M, int64_t K, const
   if (wide && M * K >= 140000 * cus) {
     const int64_t waves = K <= 16384 ? 4 : 8;
     switch ((K / 8 + waves * 64 - 1) / (waves * 64)) {
-      case 4: return launch_lnq<4, 2>(h, M, K, gamma, beta, eps, qa, z, inv_s, Xq, st);
-      case 5: return launch_lnq<5, 2>(h, M, K, gamma, beta, eps, qa, z, inv_s, Xq, st);
-      case 6: return launch_lnq<6, 2>(h, M, K, gamma, beta, eps, qa, z, inv_s, Xq, st);
-      case 7: return launch_lnq<7, 2>(h, M, K, gamma, beta, eps, qa, z, inv_s, Xq, st);
-      default: return launch_lnq<8, 2>(h, M, K, gamma, beta, eps, qa, z, inv_s, Xq, st);
+      case 4: return launch_lnq<4, 2, MX4>(h, M, K, gamma, beta, eps, qa, z, inv_s, Xq, Xe, st);
+      case 5: return launch_lnq<5, 2, MX4>(h, M, K, gamma, beta, eps, qa, z, inv_s, Xq, Xe, st);
+      case 6: return launch_lnq<6, 2, MX4>(h, M, K, gamma, beta, eps, qa, z, inv_s, Xq, Xe, st);
+      case 7: return launch_lnq<7, 2, MX4>(h, M, K, gamma, beta, eps, qa, z, inv_s, Xq, Xe, st);
+      default: return launch_lnq<8, 2, MX4>(h, M, K, gamma, beta, eps, qa, z, inv_s, Xq, Xe, st);
     }
   }
   // Fewer: one row per workgroup, 6 chunks of 8 channels per thread up to
@@ -382,9 +425,27 @@ hipError_t launch_ln_quantize_act(const uint16_t *h, int64_t M, int64_t K, const
   // against 10.2, 8 x 5120 3.9 against 4.5; 2048 x 5120 13.0 against 13.1,
   // 512 x 20480 13.0 against 11.9, so up to K = 16384).
   if (M <= 4 * cus && K <= 16384)
-    return launch_lnq<3, 1>(h, M, K, gamma, beta, eps, qa, z, inv_s, Xq, st);
-  if (K <= 6 * 8 * 1024) return launch_lnq<6, 1>(h, M, K, gamma, beta, eps, qa, z, inv_s, Xq, st);
-  return launch_lnq<8, 1>(h, M, K, gamma, beta, eps, qa, z, inv_s, Xq, st);
+    return launch_lnq<3, 1, MX4>(h, M, K, gamma, beta, eps, qa, z, inv_s, Xq, Xe, st);
+  if (K <= 6 * 8 * 1024) return launch_lnq<6, 1, MX4>(h, M, K, gamma, beta, eps, qa, z, inv_s, Xq, Xe, st);
+  return launch_lnq<8, 1, MX4>(h, M, K, gamma, beta, eps, qa, z, inv_s, Xq, Xe, st);
+}
+
+}  // namespace detail
+
+using namespace detail;
+
+hipError_t launch_ln_quantize_act(const uint16_t *h, int64_t M, int64_t K, const uint16_t *gamma,
+                                  const uint16_t *beta, float eps, int qa, const float *z,
+                                  const float *inv_s, int8_t *Xq, hipStream_t st) {
+  return launch_ln<false>(h, M, K, gamma, beta, eps, qa, z, inv_s, Xq, nullptr, st);
+}
+
+hipError_t launch_ln_quantize_act_mx4(const uint16_t *h, int64_t M, int64_t K,
+                                      const uint16_t *gamma, const uint16_t *beta, float eps,
+                                      const float *z, const float *inv_s, uint8_t *Xc, uint8_t *Xe,
+                                      hipStream_t st) {
+  return launch_ln<true>(h, M, K, gamma, beta, eps, 0, z, inv_s, reinterpret_cast<int8_t *>(Xc), Xe,
+                         st);
 }
 
 }  // namespace ot

@@ -140,6 +140,23 @@ def lib() -> ctypes.CDLL:
         L.ot_pack_weights.argtypes = [vp, i64, i64, vp, vp]
         L.ot_qlinear_packed.restype = c_int
         L.ot_qlinear_packed.argtypes = [vp, vp, vp, vp, i64, i64, i64, c_int, c_int, vp, vp, vp, vp]
+        L.ot_quantize_act_mx4.restype = c_int
+        L.ot_quantize_act_mx4.argtypes = [vp, i64, i64, vp, vp, vp, vp, vp]
+        L.ot_ln_quantize_act_mx4.restype = c_int
+        L.ot_ln_quantize_act_mx4.argtypes = [vp, i64, i64, vp, vp, ctypes.c_float, vp, vp, vp, vp,
+                                             vp]
+        L.ot_fold_weights_mx4.restype = c_int
+        L.ot_fold_weights_mx4.argtypes = [vp, vp, i64, i64, vp, vp, vp, vp, vp, vp]
+        L.ot_dequantize_mx4.restype = c_int
+        L.ot_dequantize_mx4.argtypes = [vp, vp, i64, i64, vp, vp]
+        L.ot_packed_weights_mx4_size.restype = ctypes.c_size_t
+        L.ot_packed_weights_mx4_size.argtypes = [i64, i64]
+        L.ot_pack_weights_mx4.restype = c_int
+        L.ot_pack_weights_mx4.argtypes = [vp, vp, i64, i64, vp, vp]
+        L.ot_qlinear_mx4.restype = c_int
+        L.ot_qlinear_mx4.argtypes = [vp, vp, vp, vp, i64, i64, i64, vp, vp, vp]
+        L.ot_qlinear_mx4_workspace_size.restype = ctypes.c_size_t
+        L.ot_qlinear_mx4_workspace_size.argtypes = [i64, i64, i64]
         _load_bind(L)
         _lib = L
     return _lib
@@ -605,3 +622,165 @@ def qlinear_asym(Xq, Wq, sW, zW, bprime, a_bits, w_bits, want_acc=False, workspa
     acc = torch.empty((M, N), dtype=torch.int32, device=Xq.device) if want_acc else None
     ot_qlinear_asym(Xq, Wq, sW, zW, bprime, a_bits, w_bits, Y, acc, _ws(workspace, Xq, Wq))
     return (Y, acc) if want_acc else Y
+
+
+# ---------------------------------------------------------------------------
+# MX4: microscaled 4-bit floating point.  A matrix [rows, K] is a pair of
+# tensors: codes [rows, K / 2] uint8 and scales [ceil(K / 256), rows, 8] uint8.
+# ---------------------------------------------------------------------------
+def _mx4_pair(c, e, name, shape=None):
+    """(rows, K, codes pointer, scales pointer) of a matrix in MX4, checked
+    against the [rows, K] it should be."""
+    if shape is None:
+        if not isinstance(c, torch.Tensor) or c.dim() != 2:
+            raise ValueError(f"{name}'s codes must be a tensor [rows, K / 2]")
+        shape = (c.shape[0], 2 * c.shape[1])
+    rows, K = shape
+    if K % 32:
+        raise ValueError(f"{name} must have a multiple of 32 channels, got {K}")
+    return (rows, K, _dev(c, torch.uint8, f"{name}'s codes", (rows, K // 2)),
+            _dev(e, torch.uint8, f"{name}'s scales", ((K + 255) // 256, rows, 8)))
+
+
+def ot_quantize_act_mx4(x, z, inv_s, Xc, Xe, stream=None):
+    """x [M, K] fp16 -> MX4 codes Xc and scales Xe of (x - z) * inv_s, or of x
+    (z and inv_s both None).  Asynchronous."""
+    M, K = x.shape
+    _, _, pc, pe = _mx4_pair(Xc, Xe, "X", (M, K))
+    rc = lib().ot_quantize_act_mx4(_dev(x, torch.float16, "x"), M, K,
+                                   _dev(z, torch.float32, "z", (K,)),
+                                   _dev(inv_s, torch.float32, "inv_s", (K,)), pc, pe,
+                                   _stream(stream))
+    _check(rc, "ot_quantize_act_mx4")
+
+
+def ot_ln_quantize_act_mx4(h, gamma, beta, eps, z, inv_s, Xc, Xe, stream=None):
+    """h [M, K] fp16 LayerNorm input -> MX4 codes and scales of the symmetrized
+    and scaled LayerNorm output.  Asynchronous."""
+    M, K = h.shape
+    _, _, pc, pe = _mx4_pair(Xc, Xe, "X", (M, K))
+    rc = lib().ot_ln_quantize_act_mx4(_dev(h, torch.float16, "h"), M, K,
+                                      _dev(gamma, torch.float16, "gamma", (K,)),
+                                      _dev(beta, torch.float16, "beta", (K,)), float(eps),
+                                      _dev(z, torch.float32, "z", (K,)),
+                                      _dev(inv_s, torch.float32, "inv_s", (K,)), pc, pe,
+                                      _stream(stream))
+    _check(rc, "ot_ln_quantize_act_mx4")
+
+
+def ot_fold_weights_mx4(W, b, z, s, Wc, We, bprime, stream=None):
+    """W [N, K] fp16, b [N] fp16 or None, z and s [K] fp32 or None -> MX4 codes
+    and scales of W diag(s), bprime [N] fp32.  Synchronous."""
+    N, K = W.shape
+    _, _, pc, pe = _mx4_pair(Wc, We, "W", (N, K))
+    rc = lib().ot_fold_weights_mx4(_dev(W, torch.float16, "W"), _dev(b, torch.float16, "b", (N,)),
+                                   N, K, _dev(z, torch.float32, "z", (K,)),
+                                   _dev(s, torch.float32, "s", (K,)), pc, pe,
+                                   _dev(bprime, torch.float32, "bprime", (N,)), _stream(stream))
+    _check(rc, "ot_fold_weights_mx4")
+
+
+def ot_dequantize_mx4(c, e, y, stream=None):
+    """MX4 codes and scales of [rows, K] -> their values y [rows, K] fp32.
+    Asynchronous."""
+    rows, K, pc, pe = _mx4_pair(c, e, "the matrix")
+    rc = lib().ot_dequantize_mx4(pc, pe, rows, K, _dev(y, torch.float32, "y", (rows, K)),
+                                 _stream(stream))
+    _check(rc, "ot_dequantize_mx4")
+
+
+def ot_packed_weights_mx4_size(N: int, K: int) -> int:
+    return int(lib().ot_packed_weights_mx4_size(N, K))
+
+
+def ot_pack_weights_mx4(Wc, We, Wp, stream=None):
+    """MX4 weights -> Wp (ot_packed_weights_mx4_size(N, K) bytes, uint8).
+    Asynchronous."""
+    N, K, pc, pe = _mx4_pair(Wc, We, "W")
+    rc = lib().ot_pack_weights_mx4(pc, pe, N, K,
+                                   _dev(Wp, torch.uint8, "Wp", (ot_packed_weights_mx4_size(N, K),)),
+                                   _stream(stream))
+    _check(rc, "ot_pack_weights_mx4")
+
+
+def ot_qlinear_mx4_workspace_size(M: int, N: int, K: int) -> int:
+    return int(lib().ot_qlinear_mx4_workspace_size(M, N, K))
+
+
+def _scratch(workspace, need):
+    """Device pointer of an optional workspace of at least `need` bytes."""
+    if workspace is None:
+        return None
+    ptr = _dev(workspace, torch.uint8, "workspace")
+    if workspace.numel() < need:
+        raise ValueError(f"workspace holds {workspace.numel()} bytes, the call needs {need}")
+    return ptr
+
+
+def ot_qlinear_mx4(Xc, Xe, Wp, N, bprime, Y, workspace=None, stream=None):
+    """Xc, Xe [M, K] in MX4, Wp packed MX4 weights of N output channels, bprime
+    [N] fp32 -> Y [M, N] fp16.  Asynchronous."""
+    M, K, pc, pe = _mx4_pair(Xc, Xe, "X")
+    rc = lib().ot_qlinear_mx4(pc, pe,
+                              _dev(Wp, torch.uint8, "Wp", (ot_packed_weights_mx4_size(N, K),)),
+                              _dev(bprime, torch.float32, "bprime", (N,)), M, N, K,
+                              _dev(Y, torch.float16, "Y", (M, N)),
+                              _scratch(workspace, ot_qlinear_mx4_workspace_size(M, N, K)),
+                              _stream(stream))
+    _check(rc, "ot_qlinear_mx4")
+
+
+def _mx4_empty(rows, K, device):
+    if K % 32:
+        raise ValueError(f"MX4 takes a multiple of 32 channels, got {K}")
+    return (torch.empty((rows, K // 2), dtype=torch.uint8, device=device),
+            torch.empty(((K + 255) // 256, rows, 8), dtype=torch.uint8, device=device))
+
+
+def quantize_act_mx4(x, z=None, inv_s=None):
+    """Allocating wrapper of ot_quantize_act_mx4; returns (Xc, Xe)."""
+    Xc, Xe = _mx4_empty(x.shape[0], x.shape[1], x.device)
+    ot_quantize_act_mx4(x, z, inv_s, Xc, Xe)
+    return Xc, Xe
+
+
+def ln_quantize_act_mx4(h, gamma, beta, eps, z, inv_s):
+    Xc, Xe = _mx4_empty(h.shape[0], h.shape[1], h.device)
+    ot_ln_quantize_act_mx4(h, gamma, beta, eps, z, inv_s, Xc, Xe)
+    return Xc, Xe
+
+
+def fold_weights_mx4(W, b=None, z=None, s=None):
+    """Allocating wrapper of ot_fold_weights_mx4; returns (Wc, We, bprime)."""
+    Wc, We = _mx4_empty(W.shape[0], W.shape[1], W.device)
+    bprime = torch.empty(W.shape[0], dtype=torch.float32, device=W.device)
+    ot_fold_weights_mx4(W, b, z, s, Wc, We, bprime)
+    return Wc, We, bprime
+
+
+def dequantize_mx4(c, e):
+    y = torch.empty((c.shape[0], 2 * c.shape[1]), dtype=torch.float32, device=c.device)
+    ot_dequantize_mx4(c, e, y)
+    return y
+
+
+def pack_weights_mx4(Wc, We):
+    Wp = torch.empty(ot_packed_weights_mx4_size(Wc.shape[0], 2 * Wc.shape[1]), dtype=torch.uint8,
+                     device=Wc.device)
+    ot_pack_weights_mx4(Wc, We, Wp)
+    return Wp
+
+
+def qlinear_mx4_workspace_for(M: int, N: int, K: int, device=None):
+    """A scratch buffer for ot_qlinear_mx4 at these sizes, or None when it uses
+    none."""
+    n = ot_qlinear_mx4_workspace_size(M, N, K)
+    return torch.empty(n, dtype=torch.uint8, device=device or "cuda") if n else None
+
+
+def qlinear_mx4(Xc, Xe, Wp, N, bprime, workspace=None):
+    Y = torch.empty((Xc.shape[0], N), dtype=torch.float16, device=Xc.device)
+    if workspace is True:
+        workspace = qlinear_mx4_workspace_for(Xc.shape[0], N, 2 * Xc.shape[1], Xc.device)
+    ot_qlinear_mx4(Xc, Xe, Wp, N, bprime, Y, None if workspace is False else workspace)
+    return Y

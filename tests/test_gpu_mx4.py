@@ -1,0 +1,196 @@
+"""The MX4 operators on the GPU against plain forms in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import mx4_oracle as X
+from oracle import ot_oracle as O
+from paper_2406_18832_amd import ot
+
+pytestmark = pytest.mark.gpu
+
+# One fp16 rounding of Y: half a unit, 2^-11 of the value (2^-25 below the
+# normal range).  The sum in fp32: products are exact (two levels of 2 bits and
+# powers of two), so only additions round, each by at most 2^-24 of a partial sum
+# that stays below S = sum |x w| + |b'|.  K channels and the bias take at most K
+# additions whatever their order; the matrix unit may truncate rather than round,
+# which doubles the step.
+def y_tolerance(y, mags, K):
+    return np.maximum(np.abs(y) * 2.0 ** -11, 2.0 ** -25) + (K + 1) * 2.0 ** -23 * mags
+
+
+def dev(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def host(t):
+    return t.cpu().numpy()
+
+
+def draw_activations(r, M, K):
+    x = r.standard_normal((M, K)).astype(np.float32)
+    x[:, r.integers(0, K, max(1, K // 100))] *= 50
+    z = r.uniform(-3, 3, K).astype(np.float32)
+    inv_s = np.float32(1) / r.uniform(0.1, 2, K).astype(np.float32)
+    return x.astype(np.float16), z, inv_s
+
+
+# rows, channels: one row and one block; ragged tails of a K tile and of a wave's
+# 512 channels; rows in groups of 1, 2 and 8 per wave
+SHAPES = [(1, 32), (1, 64), (3, 96), (5, 256), (7, 288), (2, 512), (9, 544), (33, 768), (64, 1056),
+          (130, 4128), (700, 2016), (2100, 2080)]
+
+
+@pytest.mark.parametrize("M,K", SHAPES)
+@pytest.mark.parametrize("sym", [True, False])
+def test_quantize_codes_and_scales(M, K, sym):
+    r = np.random.default_rng([M, K, sym])
+    x, z, inv_s = draw_activations(r, M, K)
+    x[r.integers(0, M), :32] = 0  # an empty block (without symmetrization)
+    a = (z, inv_s) if sym else (None, None)
+    c, e = X.to_mx4(X.activations(x, *a))
+    # what a call must not leave: stale scales past K
+    Xc, Xe = torch.full((M, K // 2), 0x5A, dtype=torch.uint8, device="cuda"), \
+        torch.full(((K + 255) // 256, M, 8), 0x5A, dtype=torch.uint8, device="cuda")
+    ot.ot_quantize_act_mx4(dev(x), *(None if v is None else dev(v) for v in a), Xc, Xe)
+    assert np.array_equal(host(Xe), e)
+    assert np.array_equal(host(Xc), c)
+    assert np.array_equal(host(ot.dequantize_mx4(Xc, Xe)), X.values(c, e).astype(np.float32))
+
+
+def test_quantize_every_level_tie_and_neighbour():
+    """Every level, halfway point and its fp32 neighbours, over exponents from
+    the smallest fp16 subnormal to the largest value, with both signs."""
+    t = np.concatenate([X.LEVELS, X.HALFWAY, np.nextafter(X.HALFWAY.astype(np.float32), 0),
+                        np.nextafter(X.HALFWAY.astype(np.float32), 9), [7.0, 7.75, 6.5, 5.5]])
+    t = np.concatenate([t, -t]).astype(np.float32)
+    rows = []
+    for e in range(-120, 121, 5):
+        for lead in (4.0, 6.0, 7.9):
+            for i in range(0, t.size, 31):
+                row = np.zeros(32, dtype=np.float32)
+                row[0] = lead
+                part = t[i:i + 31]
+                row[1:1 + part.size] = part
+                rows.append(np.ldexp(row, e))
+    v = np.stack(rows)
+    M, K = v.shape
+    # x = 0 and z = -v put the values there: fp32(0 - z) * 1 (a +0 for v = -0)
+    c, s = X.to_mx4(X.activations(np.zeros((M, K), np.float16), -v, np.ones((M, K), np.float32)))
+    z = dev(-v.reshape(-1))
+    x = torch.zeros((1, M * K), dtype=torch.float16, device="cuda")
+    Xc, Xe = ot.quantize_act_mx4(x, z, torch.ones(M * K, device="cuda"))
+    assert np.array_equal(host(Xc).reshape(M, K // 2), c)
+    got = host(Xe).transpose(1, 0, 2).reshape(-1)[:M]
+    assert np.array_equal(got, s[0, :, 0])
+
+
+def test_quantize_non_finite_blocks():
+    """A NaN or an infinity, of the input or of the symmetrization, makes its
+    block NaN and no other."""
+    x = np.ones((3, 96), dtype=np.float16)
+    x[0, 5], x[1, 40], x[2, 95] = np.nan, np.inf, -np.inf
+    inv_s = np.ones(96, dtype=np.float32)
+    inv_s[33] = 3e38
+    x[2, 33] = 60000
+    Xc, Xe = ot.quantize_act_mx4(dev(x), dev(np.zeros(96, np.float32)), dev(inv_s))
+    v = host(ot.dequantize_mx4(Xc, Xe))
+    bad = np.isnan(v).reshape(3, 3, 32)
+    assert np.array_equal(bad.all(2), bad.any(2))
+    assert np.array_equal(bad.any(2), [[1, 0, 0], [0, 1, 0], [0, 1, 1]])
+    c, e = X.to_mx4(X.activations(x, np.zeros(96, np.float32), inv_s))
+    assert np.array_equal(host(Xe), e) and np.array_equal(host(Xc), c)
+
+
+@pytest.mark.parametrize("M,K", [(1, 32), (2, 64), (5, 288), (8, 5120), (3, 9248), (1030, 1056),
+                                 (40, 20512), (2, 50176), (2100, 17408 + 1024)])
+def test_ln_quantize(M, K):
+    r = np.random.default_rng([M, K, 3])
+    h = (r.standard_normal((M, K)) * r.uniform(0.5, 2, K) + r.standard_normal(K)).astype(np.float16)
+    if M > 1:
+        h[1] -= h[1].mean(dtype=np.float64).astype(np.float16)
+        h[0, ::2], h[0, 1::2] = 1.0, -1.0  # a mean of exactly 0
+    gamma = r.uniform(0.5, 1.5, K).astype(np.float16)
+    beta = (r.standard_normal(K) * 0.2).astype(np.float16)
+    z = (r.standard_normal(K) * 0.2).astype(np.float32)
+    inv_s = r.uniform(0.5, 2, K).astype(np.float32)
+    rows = slice(None) if M <= 64 else np.r_[0:8, M - 8:M]
+    f = np.float32
+    mean, var = O.layernorm_stats(h[rows])
+    rstd = 1 / np.sqrt(var + float(f(1e-5)))
+    n = (h[rows].astype(f) - mean.astype(f)[:, None]) * rstd.astype(f)[:, None]
+    v = (n * gamma.astype(f) + (beta.astype(f) - z)) * inv_s
+    c, e = X.to_mx4(v)
+    Xc, Xe = torch.full((M, K // 2), 0x5A, dtype=torch.uint8, device="cuda"), \
+        torch.full(((K + 255) // 256, M, 8), 0x5A, dtype=torch.uint8, device="cuda")
+    ot.ot_ln_quantize_act_mx4(*map(dev, (h, gamma, beta)), 1e-5, dev(z), dev(inv_s), Xc, Xe)
+    assert np.array_equal(host(Xe)[:, rows], e)
+    assert np.array_equal(host(Xc)[rows], c)
+
+
+@pytest.mark.parametrize("N,K", [(1, 32), (2, 96), (5, 256), (31, 544), (33, 2048), (70, 2080),
+                                 (256, 4128), (6, 20480)])
+@pytest.mark.parametrize("how", ["all", "no z", "no s", "no bias", "none"])
+def test_fold(N, K, how):
+    r = np.random.default_rng([N, K])
+    W = (r.standard_normal((N, K)) * 0.02).astype(np.float16)
+    W[0, :32] = 0
+    b = None if how in ("no bias", "none") else r.standard_normal(N).astype(np.float16)
+    z = None if how in ("no z", "none") else r.uniform(-3, 3, K).astype(np.float32)
+    s = None if how in ("no s", "none") else r.uniform(0.01, 20, K).astype(np.float32)
+    c, e, bias = X.fold(W, b, z, s)
+    Wc, We, bp = ot.fold_weights_mx4(dev(W), *(None if v is None else dev(v) for v in (b, z, s)))
+    assert np.array_equal(host(We), e) and np.array_equal(host(Wc), c)
+    # a float64 sum of K exact products, then one rounding to fp32 (2^-24)
+    mags = np.abs(W.astype(np.float64)) @ np.abs(z.astype(np.float64)) if z is not None else 0.0
+    assert np.all(np.abs(host(bp) - bias) <= 2.0 ** -24 * np.abs(bias) * 1.01 + 2.0 ** -52 * K * mags)
+    assert np.array_equal(host(ot.pack_weights_mx4(Wc, We)), X.pack(c, e))
+
+
+@pytest.mark.parametrize("where", ["weight", "product", "bias"])
+def test_fold_refuses_non_finite(where):
+    W = torch.full((5, 64), 0.5, dtype=torch.float16, device="cuda")
+    b = torch.zeros(5, dtype=torch.float16, device="cuda")
+    s = torch.ones(64, device="cuda")
+    if where == "weight":
+        W[3, 63] = float("nan")
+    elif where == "product":
+        W[4, 0], s[0] = 60000.0, 1e36
+    else:
+        b[2] = float("inf")
+    with pytest.raises(ot.OTError) as err:
+        ot.fold_weights_mx4(W, b, None, s)
+    assert err.value.code == ot.OT_ENONFINITE
+
+
+def draw_mx4(r, rows, K, spread=3):
+    """Random codes and scales (blocks of different magnitudes, some empty)."""
+    c = r.integers(0, 256, (rows, K // 2), dtype=np.uint8)
+    tiles = -(-K // 256)
+    e = np.zeros((tiles, rows, 8), dtype=np.uint8)
+    for i in range(K // 32):
+        e[i // 8, :, i % 8] = r.integers(124 - spread, 124 + spread, rows)
+    if rows > 2:
+        c[rows // 2] = 0
+    return c, e
+
+
+LINEARS = [(1, 1, 32), (1, 33, 64), (2, 16, 96), (16, 768, 768), (17, 100, 288), (5, 4100, 5120),
+           (32, 65, 2080), (33, 200, 1056), (64, 513, 4128), (8, 64, 36864),
+           (65, 1, 32), (65, 70, 96), (100, 130, 288), (131, 615, 4128), (128, 128, 256),
+           (129, 257, 512), (300, 1000, 1056), (513, 2050, 544), (1000, 3000, 800),
+           (2048, 4096, 2048)]
+
+
+@pytest.mark.parametrize("M,N,K", LINEARS)
+def test_linear(M, N, K):
+    r = np.random.default_rng([M, N, K])
+    xc, xe = draw_mx4(r, M, K)
+    wc, we = draw_mx4(r, N, K)
+    bias = r.standard_normal(N).astype(np.float32)
+    y, mags = X.linear(X.values(xc, xe), X.values(wc, we), bias)
+    Wp = ot.pack_weights_mx4(dev(wc), dev(we))
+    Y = torch.full((M, N), float("nan"), dtype=torch.float16, device="cuda")
+    ot.ot_qlinear_mx4(dev(xc), dev(xe), Wp, N, dev(bias), Y,
+                      ot.qlinear_mx4_workspace_for(M, N, K))
+    assert np.all(np.abs(host(Y).astype(np.float64) - y) <= y_tolerance(y, mags, K))

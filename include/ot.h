@@ -491,6 +491,46 @@ ot_status ot_qlinear_mx4(const uint8_t *Xc, const uint8_t *Xe, const uint8_t *Wp
  * current device (0 if none, and for sizes it rejects).  No device work. */
 size_t ot_qlinear_mx4_workspace_size(int64_t M, int64_t N, int64_t K);
 
+/*
+ * ot_moe_mx4 -- a whole mixture-of-experts layer for a few tokens on packed MX4
+ * weights (a decode step; larger batches run an expert's linears through
+ * ot_qlinear_mx4).  For token m, with its top_k largest logits (the lower expert
+ * first among equals) and p the softmax over them,
+ *   g_j  = W1_e x_m + b1_e             for its j-th expert e, in fp32
+ *   h_j  = max(g_j, 0)                 OT_MOE_RELU, F1 = F
+ *          silu(g_j[0..F)) g_j[F..2F)  OT_MOE_SWIGLU, F1 = 2F; silu(v) = v / (1 + e^-v)
+ *   Y[m] = fp16(sum_j p_j (W2_e q(h_j) + b2_e)),  q: the values of h_j in MX4
+ * A logit of -inf or NaN is never chosen: such a token takes fewer experts, and
+ * one with no other logit gets Y = 0.
+ *   Xc, Xe [M x H] in MX4; logits [M x E] fp16 (device).
+ *   W1p  packed weights of all experts' fc1 as one matrix [E F1 x H] (an
+ *        expert's rows together; the gate's rows before the others).
+ *   W2p  the same of fc2, [E H x F].
+ *   b1 [E x F1], b2 [E x H] fp32, or NULL (device).
+ *   M    0 (a no-op) .. OT_MOE_MAX_TOKENS.   E 1 .. OT_MOE_MAX_EXPERTS.
+ *   top_k  1 .. min(E, OT_MOE_MAX_TOP_K).
+ *   H, F   multiples of 32 up to 65536.
+ *   Y    [M x H] fp16 output (device).
+ *   workspace  ot_moe_mx4_workspace_size(M, H, F, E, top_k) bytes, 16-byte
+ *        aligned (device).  Needs no initialization; calls that overlap in time
+ *        must not share one.
+ * OT_ESHAPE for sizes outside these.  The result does not depend on how calls
+ * are scheduled: no atomics on sums.  Asynchronous on stream.
+ */
+#define OT_MOE_RELU 0
+#define OT_MOE_SWIGLU 1
+#define OT_MOE_MAX_TOKENS 64
+#define OT_MOE_MAX_EXPERTS 256
+#define OT_MOE_MAX_TOP_K 16
+ot_status ot_moe_mx4(const uint8_t *Xc, const uint8_t *Xe,
+                     const uint16_t *logits, const uint8_t *W1p,
+                     const float *b1, const uint8_t *W2p, const float *b2,
+                     int64_t M, int64_t H, int64_t F, int64_t E, int64_t top_k,
+                     int act, uint16_t *Y, void *workspace, void *stream);
+/* Bytes of the workspace (0 for M == 0 and for sizes it rejects). */
+size_t ot_moe_mx4_workspace_size(int64_t M, int64_t H, int64_t F, int64_t E,
+                                 int64_t top_k);
+
 #ifdef __cplusplus
 }
 #endif

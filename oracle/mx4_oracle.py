@@ -115,3 +115,27 @@ def top_k(logits, k):
     M, E = l.shape
     return np.array([sorted(range(E), key=lambda j: (bool(nan[m, j]), -l[m, j], j))[:k]
                      for m in range(M)], dtype=np.int64).reshape(M, k)
+
+
+def moe(x, logits, k, w1, b1, w2, b2, act):
+    """float64 outputs of the mixture-of-experts layer: x [M, H], w1 [E, F1, H],
+    w2 [E, H, F] as float64 values, b1 [E, F1], b2 [E, H] or None; and the hidden
+    activations before their quantization, {(m, j): [F]}."""
+    M, H = x.shape
+    y, hidden = np.zeros((M, H)), {}
+    for m, experts in enumerate(top_k(logits, k)):
+        l = logits[m].astype(np.float64)
+        experts = [e for e in experts if not np.isnan(l[e]) and l[e] != -np.inf]
+        if not experts:
+            continue
+        most = max(l[e] for e in experts)
+        p = np.array([1.0 if l[e] == most else np.exp(l[e] - most) for e in experts])
+        p /= p.sum()
+        for j, e in enumerate(experts):
+            g = w1[e] @ x[m] + (b1[e] if b1 is not None else 0.0)
+            F = w2.shape[2]
+            h = np.maximum(g, 0) if act == "relu" else g[:F] / (1 + np.exp(-g[:F])) * g[F:]
+            hidden[m, j] = h
+            q = values(*to_mx4(h[None].astype(np.float32)))[0]
+            y[m] += p[j] * (w2[e] @ q + (b2[e] if b2 is not None else 0.0))
+    return y, hidden

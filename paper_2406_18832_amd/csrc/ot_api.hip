@@ -485,4 +485,34 @@ size_t ot_qlinear_mx4_workspace_size(int64_t M, int64_t N, int64_t K) {
   return 0;
 }
 
+// Sizes of a mixture-of-experts layer: M == 0 is fine.
+static bool moe_shape_ok(int64_t M, int64_t H, int64_t F, int64_t E, int64_t top_k) {
+  return M <= OT_MOE_MAX_TOKENS && H > 0 && H % 32 == 0 && H <= kMaxLnK && F > 0 && F % 32 == 0 &&
+         F <= kMaxLnK && E > 0 && E <= OT_MOE_MAX_EXPERTS && top_k > 0 && top_k <= E &&
+         top_k <= OT_MOE_MAX_TOP_K;
+}
+
+size_t ot_moe_mx4_workspace_size(int64_t M, int64_t H, int64_t F, int64_t E, int64_t top_k) {
+  if (M <= 0 || !moe_shape_ok(M, H, F, E, top_k)) return 0;
+  return ot::moe_mx4_workspace_bytes(M, F, top_k);
+}
+
+ot_status ot_moe_mx4(const uint8_t *Xc, const uint8_t *Xe, const uint16_t *logits,
+                     const uint8_t *W1p, const float *b1, const uint8_t *W2p, const float *b2,
+                     int64_t M, int64_t H, int64_t F, int64_t E, int64_t top_k, int act,
+                     uint16_t *Y, void *workspace, void *stream) {
+  if (M < 0 || H < 0 || F < 0 || E < 0 || top_k < 0) return OT_EINVAL;
+  if (act != OT_MOE_RELU && act != OT_MOE_SWIGLU) return OT_EINVAL;
+  if (!moe_shape_ok(M, H, F, E, top_k)) return OT_ESHAPE;
+  if (M == 0) return OT_OK;
+  if (!Xc || !Xe || !logits || !W1p || !W2p || !Y || !workspace) return OT_EINVAL;
+  if (!aligned16(Xc) || !aligned16(Xe) || !aligned16(logits) || !aligned16(W1p) ||
+      !aligned16(b1) || !aligned16(W2p) || !aligned16(b2) || !aligned16(Y) ||
+      !aligned16(workspace))
+    return OT_EINVAL;
+  return hip_status(ot::launch_moe_mx4(Xc, Xe, logits, W1p, b1, W2p, b2, M, H, F, E, top_k,
+                                       act == OT_MOE_SWIGLU, Y, workspace,
+                                       static_cast<hipStream_t>(stream)));
+}
+
 }  // extern "C"

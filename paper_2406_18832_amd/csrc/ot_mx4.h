@@ -132,4 +132,11 @@ hipError_t launch_mx4_decode(const uint8_t *Xc, const uint8_t *Xe, const uint8_t
                              const float *bp, int64_t M, int64_t N, int64_t K, uint16_t *Y,
                              hipStream_t st);
 
+// A mixture-of-experts layer; workspace of at least moe_mx4_workspace_bytes.
+size_t moe_mx4_workspace_bytes(int64_t M, int64_t F, int64_t top_k);
+hipError_t launch_moe_mx4(const uint8_t *Xc, const uint8_t *Xe, const uint16_t *logits,
+                          const uint8_t *W1, const float *b1, const uint8_t *W2, const float *b2,
+                          int64_t M, int64_t H, int64_t F, int64_t E, int64_t top_k, bool glu,
+                          uint16_t *Y, void *workspace, hipStream_t st);
+
 }  // namespace ot

@@ -157,6 +157,11 @@ def lib() -> ctypes.CDLL:
         L.ot_qlinear_mx4.argtypes = [vp, vp, vp, vp, i64, i64, i64, vp, vp, vp]
         L.ot_qlinear_mx4_workspace_size.restype = ctypes.c_size_t
         L.ot_qlinear_mx4_workspace_size.argtypes = [i64, i64, i64]
+        L.ot_moe_mx4.restype = c_int
+        L.ot_moe_mx4.argtypes = [vp, vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, i64, c_int, vp, vp,
+                                 vp]
+        L.ot_moe_mx4_workspace_size.restype = ctypes.c_size_t
+        L.ot_moe_mx4_workspace_size.argtypes = [i64, i64, i64, i64, i64]
         _load_bind(L)
         _lib = L
     return _lib
@@ -730,6 +735,39 @@ def ot_qlinear_mx4(Xc, Xe, Wp, N, bprime, Y, workspace=None, stream=None):
     _check(rc, "ot_qlinear_mx4")
 
 
+MOE_ACTIVATIONS = {"relu": 0, "swiglu": 1}
+
+
+def ot_moe_mx4_workspace_size(M: int, H: int, F: int, E: int, top_k: int) -> int:
+    return int(lib().ot_moe_mx4_workspace_size(M, H, F, E, top_k))
+
+
+def ot_moe_mx4(Xc, Xe, logits, top_k, W1p, b1, W2p, b2, F, act, Y, workspace, stream=None):
+    """A mixture-of-experts layer for up to 64 tokens: Xc, Xe [M, H] in MX4,
+    logits [M, E] fp16, W1p and W2p the packed MX4 weights of all experts' fc1
+    [E F1, H] and fc2 [E H, F], b1 [E, F1] and b2 [E, H] fp32 or None, act "relu"
+    (F1 = F) or "swiglu" (F1 = 2 F, the gate first) -> Y [M, H] fp16.
+    workspace: ot_moe_mx4_workspace_size(M, H, F, E, top_k) bytes (uint8).
+    Asynchronous."""
+    if act not in MOE_ACTIVATIONS:
+        raise ValueError(f"act must be one of {sorted(MOE_ACTIVATIONS)}, got {act!r}")
+    M, H, pc, pe = _mx4_pair(Xc, Xe, "X")
+    if not isinstance(logits, torch.Tensor) or logits.dim() != 2:
+        raise ValueError("logits must be a tensor [M, E]")
+    E, F1 = logits.shape[1], (2 if act == "swiglu" else 1) * F
+    if workspace is None and M:
+        raise ValueError("ot_moe_mx4 needs a workspace")
+    rc = lib().ot_moe_mx4(pc, pe, _dev(logits, torch.float16, "logits", (M, E)),
+                          _dev(W1p, torch.uint8, "W1p", (ot_packed_weights_mx4_size(E * F1, H),)),
+                          _dev(b1, torch.float32, "b1", (E, F1)),
+                          _dev(W2p, torch.uint8, "W2p", (ot_packed_weights_mx4_size(E * H, F),)),
+                          _dev(b2, torch.float32, "b2", (E, H)), M, H, F, E, int(top_k),
+                          MOE_ACTIVATIONS[act], _dev(Y, torch.float16, "Y", (M, H)),
+                          _scratch(workspace, ot_moe_mx4_workspace_size(M, H, F, E, top_k)),
+                          _stream(stream))
+    _check(rc, "ot_moe_mx4")
+
+
 def _mx4_empty(rows, K, device):
     if K % 32:
         raise ValueError(f"MX4 takes a multiple of 32 channels, got {K}")
@@ -783,4 +821,20 @@ def qlinear_mx4(Xc, Xe, Wp, N, bprime, workspace=None):
     if workspace is True:
         workspace = qlinear_mx4_workspace_for(Xc.shape[0], N, 2 * Xc.shape[1], Xc.device)
     ot_qlinear_mx4(Xc, Xe, Wp, N, bprime, Y, None if workspace is False else workspace)
+    return Y
+
+
+def moe_mx4_workspace_for(M: int, H: int, F: int, E: int, top_k: int, device=None):
+    """The scratch buffer of ot_moe_mx4 at these sizes."""
+    return torch.empty(ot_moe_mx4_workspace_size(M, H, F, E, top_k), dtype=torch.uint8,
+                       device=device or "cuda")
+
+
+def moe_mx4(Xc, Xe, logits, top_k, W1p, b1, W2p, b2, F, act, workspace=None):
+    """Allocating wrapper of ot_moe_mx4 (the workspace too, unless given)."""
+    M, H = Xc.shape[0], 2 * Xc.shape[1]
+    if workspace is None:
+        workspace = moe_mx4_workspace_for(M, H, F, logits.shape[1], top_k, Xc.device)
+    Y = torch.empty((M, H), dtype=torch.float16, device=Xc.device)
+    ot_moe_mx4(Xc, Xe, logits, top_k, W1p, b1, W2p, b2, F, act, Y, workspace)
     return Y

@@ -194,3 +194,99 @@ def test_linear(M, N, K):
     ot.ot_qlinear_mx4(dev(xc), dev(xe), Wp, N, dev(bias), Y,
                       ot.qlinear_mx4_workspace_for(M, N, K))
     assert np.all(np.abs(host(Y).astype(np.float64) - y) <= y_tolerance(y, mags, K))
+
+
+def draw_moe(r, M, H, F, E, act):
+    F1 = 2 * F if act == "swiglu" else F
+    x = draw_mx4(r, M, H, 1)
+    logits = (r.standard_normal((M, E)) * 2).astype(np.float16)
+    w1, w2 = draw_mx4(r, E * F1, H, 1), draw_mx4(r, E * H, F, 1)
+    b1, b2 = (r.standard_normal((E, n)).astype(np.float32) for n in (F1, H))
+    return x, logits, w1, b1, w2, b2
+
+
+def run_moe(x, logits, k, w1, b1, w2, b2, F, act):
+    return ot.moe_mx4(dev(x[0]), dev(x[1]), dev(logits), k, ot.pack_weights_mx4(*map(dev, w1)),
+                      None if b1 is None else dev(b1), ot.pack_weights_mx4(*map(dev, w2)),
+                      None if b2 is None else dev(b2), F, act)
+
+
+# draw_mx4(spread 1) gives scales of 2^-4 and 2^-3, so fc1's products are multiples
+# of 2^-10 and its sums below 2^24 of those units: exact in fp32 in any order.  Then
+# g takes one rounding (the bias), and silu(gate) * up a few of fp32 and those of
+# exp.  A hidden value that close to a halfway point may take the other code: a step
+# of at most 2 scales.  The tolerance lets every such value move by its whole step.
+def moe_expected(x, logits, k, w1, b1, w2, b2, F, act):
+    H, E = x[0].shape[1] * 2, logits.shape[1]
+    xv = X.values(*x)
+    w1v, w2v = X.values(*w1).reshape(E, -1, H), X.values(*w2).reshape(E, H, F)
+    y, hidden = X.moe(xv, logits, k, w1v, b1, w2v, b2, act)
+    tol = np.maximum(np.abs(y) * 2.0 ** -11, 2.0 ** -25)
+    for (m, j), h in hidden.items():
+        e = X.top_k(logits[m:m + 1], k)[0, j]
+        assert (np.abs(w1v[e]) @ np.abs(xv[m])).max() < 2.0 ** 14
+        g = w1v[e] @ xv[m] + (b1[e] if b1 is not None else 0)
+        g_err = 2.0 ** -24 * np.abs(g)
+        if act == "relu":
+            err = g_err
+        else:
+            err = 1.1 * g_err[:F] * np.abs(g[F:]) + np.abs(g[:F]) * g_err[F:] + 2.0 ** -20 * np.abs(h)
+        scale = np.ldexp(1.0, X.scale_bytes(h.astype(np.float32).reshape(-1, 32)).astype(int) - 127)
+        scale = np.repeat(scale, 32)
+        t = np.abs(h) / scale
+        near = np.abs(t[:, None] - X.HALFWAY).min(1) * scale <= err + 2.0 ** -24 * np.abs(h)
+        step = np.where(near, 2 * scale, 0.0)
+        q = np.abs(X.values(*X.to_mx4(h[None].astype(np.float32)))[0])
+        tol[m] += np.abs(w2v[e]) @ step + (F * k + 8) * 2.0 ** -23 * (
+            np.abs(w2v[e]) @ q + (np.abs(b2[e]) if b2 is not None else 0))
+    return y, tol
+
+
+MOES = [(1, 32, 32, 1, 1), (1, 256, 512, 8, 2), (2, 96, 288, 4, 2), (3, 544, 96, 70, 8),
+        (16, 512, 256, 4, 4), (17, 288, 544, 3, 2), (33, 256, 96, 2, 2), (64, 64, 32, 1, 1),
+        (64, 512, 352, 32, 4), (64, 96, 64, 256, 16), (40, 2048, 1408, 5, 1)]
+
+
+@pytest.mark.parametrize("M,H,F,E,k", MOES)
+@pytest.mark.parametrize("act", ["relu", "swiglu"])
+def test_moe(M, H, F, E, k, act):
+    r = np.random.default_rng([M, H, F, E, k])
+    x, logits, w1, b1, w2, b2 = draw_moe(r, M, H, F, E, act)
+    y, tol = moe_expected(x, logits, k, w1, b1, w2, b2, F, act)
+    assert np.median(tol) <= 0.05 * np.sqrt(np.mean(y * y))  # the bound says something
+    got = host(run_moe(x, logits, k, w1, b1, w2, b2, F, act)).astype(np.float64)
+    assert np.all(np.abs(got - y) <= tol)
+
+
+@pytest.mark.parametrize("by_choice", [True, False])
+def test_moe_ties_and_logits_that_choose_nothing(by_choice):
+    """Equal logits (also 0 and -0) go to the lower expert; -inf and NaN are not
+    chosen; a token with nothing else gets zeros; +inf takes all the weight."""
+    M, H, F, E, k = (3, 64, 64, 40, 3) if by_choice else (8, 64, 64, 9, 3)
+    r = np.random.default_rng(11)
+    x, logits, w1, b1, w2, b2 = draw_moe(r, M, H, F, E, "relu")
+    logits[0] = 1.0
+    logits[0, 1] = 0.5
+    logits[1] = -np.inf
+    logits[1, E - 1] = -7.0
+    logits[2] = np.nan
+    if not by_choice:
+        logits[3, ::2], logits[3, 1::2] = -0.0, 0.0
+        logits[4] = -np.inf
+        logits[5, 2:4] = np.inf
+        logits[6] = np.nan
+        logits[6, 4] = -65504
+    y, tol = moe_expected(x, logits, k, w1, b1, w2, b2, F, "relu")
+    got = host(run_moe(x, logits, k, w1, b1, w2, b2, F, "relu")).astype(np.float64)
+    assert np.all(np.abs(got - y) <= tol)
+    assert not got[2].any() and got[1].any()
+
+
+def test_moe_without_biases_and_twice():
+    r = np.random.default_rng(5)
+    args = draw_moe(r, 6, 288, 160, 8, "swiglu")
+    x, logits, w1, _, w2, _ = args
+    y, tol = moe_expected(x, logits, 2, w1, None, w2, None, 160, "swiglu")
+    a = run_moe(x, logits, 2, w1, None, w2, None, 160, "swiglu")
+    assert np.all(np.abs(host(a).astype(np.float64) - y) <= tol)
+    assert torch.equal(a, run_moe(x, logits, 2, w1, None, w2, None, 160, "swiglu"))

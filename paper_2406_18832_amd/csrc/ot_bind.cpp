@@ -66,6 +66,31 @@ struct Args {
     if (t == nullptr || t->numel() < (int64_t)need()) return miss();
     return t->data_ptr();
   }
+  // A vector that may be None (nullptr).
+  template <class T>
+  T *vec_or_none(int i, at::ScalarType type, int64_t n) {
+    if (ok && a[i] == Py_None) return nullptr;
+    return vec<T>(i, type, n);
+  }
+  // The scales of an MX4 matrix.
+  uint8_t *mx4_scales(int i, int64_t rows, int64_t K) {
+    const at::Tensor *t = tensor(i, at::kByte);
+    if (t == nullptr || t->dim() != 3 || t->size(0) != (K + 255) / 256 || t->size(1) != rows ||
+        t->size(2) != 8)
+      return static_cast<uint8_t *>(miss());
+    return static_cast<uint8_t *>(t->data_ptr());
+  }
+  // The codes of an MX4 matrix that defines its sizes.
+  const uint8_t *mx4_codes(int i, int64_t &rows, int64_t &K) {
+    const uint8_t *p = matrix<uint8_t>(i, at::kByte, rows, K);
+    if (ok && K % 16 != 0) ok = false;
+    if (ok) K *= 2;
+    return p;
+  }
+  float real(int i) {
+    if (ok && !PyFloat_CheckExact(a[i])) ok = false;
+    return ok ? (float)PyFloat_AS_DOUBLE(a[i]) : 0.f;
+  }
   int64_t integer(int i) {
     if (!ok || !PyLong_CheckExact(a[i])) {
       ok = false;
@@ -298,6 +323,101 @@ PyObject *qlinear_asym(PyObject *, PyObject *const *a, Py_ssize_t n) {
   });
 }
 
+// (fn, x, z, inv_s, Xc, Xe, stream)
+PyObject *quantize_act_mx4(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return run(a, n, 7, [](Args &g) -> int {
+    int64_t M, K;
+    auto fn = g.address<decltype(&ot_quantize_act_mx4)>(0);
+    auto *x = g.matrix<uint16_t>(1, kF16, M, K);
+    if (g.ok && K % 32 != 0) g.ok = false;
+    auto *z = g.vec_or_none<float>(2, kF32, K), *is = g.vec_or_none<float>(3, kF32, K);
+    auto *c = g.sized<uint8_t>(4, at::kByte, M, K / 2);
+    auto *e = g.mx4_scales(5, M, K);
+    auto *st = g.stream(6);
+    return g.call([&] { return fn(x, M, K, z, is, c, e, st); });
+  });
+}
+
+// (fn, h, gamma, beta, eps, z, inv_s, Xc, Xe, stream)
+PyObject *ln_quantize_act_mx4(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return run(a, n, 10, [](Args &g) -> int {
+    int64_t M, K;
+    auto fn = g.address<decltype(&ot_ln_quantize_act_mx4)>(0);
+    auto *h = g.matrix<uint16_t>(1, kF16, M, K);
+    if (g.ok && K % 32 != 0) g.ok = false;
+    auto *ga = g.vec<uint16_t>(2, kF16, K), *be = g.vec<uint16_t>(3, kF16, K);
+    const float eps = g.real(4);
+    auto *z = g.vec<float>(5, kF32, K), *is = g.vec<float>(6, kF32, K);
+    auto *c = g.sized<uint8_t>(7, at::kByte, M, K / 2);
+    auto *e = g.mx4_scales(8, M, K);
+    auto *st = g.stream(9);
+    return g.call([&] { return fn(h, M, K, ga, be, eps, z, is, c, e, st); });
+  });
+}
+
+// (fn, c, e, y, stream)
+PyObject *dequantize_mx4(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return run(a, n, 5, [](Args &g) -> int {
+    int64_t M, K;
+    auto fn = g.address<decltype(&ot_dequantize_mx4)>(0);
+    auto *c = g.mx4_codes(1, M, K);
+    auto *e = g.mx4_scales(2, M, K);
+    auto *y = g.sized<float>(3, kF32, M, K);
+    auto *st = g.stream(4);
+    return g.call([&] { return fn(c, e, M, K, y, st); });
+  });
+}
+
+using PackedFn = size_t (*)(int64_t, int64_t);
+
+// (fn, ws_size, packed_size, Xc, Xe, Wp, N, bprime, Y, workspace, stream)
+PyObject *qlinear_mx4(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return run(a, n, 11, [](Args &g) -> int {
+    int64_t M, K;
+    auto fn = g.address<decltype(&ot_qlinear_mx4)>(0);
+    auto ws_size = g.address<WsFn>(1);
+    auto packed = g.address<PackedFn>(2);
+    auto *c = g.mx4_codes(3, M, K);
+    auto *e = g.mx4_scales(4, M, K);
+    const int64_t N = g.integer(6);
+    auto *w = g.ok ? g.vec<uint8_t>(5, at::kByte, (int64_t)packed(N, K)) : nullptr;
+    auto *b = g.vec<float>(7, kF32, N);
+    auto *y = g.sized<uint16_t>(8, kF16, M, N);
+    auto *ws = g.scratch(9, [&] { return ws_size(M, N, K); });
+    auto *st = g.stream(10);
+    return g.call([&] { return fn(c, e, w, b, M, N, K, y, ws, st); });
+  });
+}
+
+using MoeWsFn = size_t (*)(int64_t, int64_t, int64_t, int64_t, int64_t);
+
+// (fn, ws_size, packed_size, Xc, Xe, logits, top_k, W1p, b1, W2p, b2, F, act (its
+//  number), Y, workspace, stream)
+PyObject *moe_mx4(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return run(a, n, 16, [](Args &g) -> int {
+    int64_t M, H, rows, E;
+    auto fn = g.address<decltype(&ot_moe_mx4)>(0);
+    auto ws_size = g.address<MoeWsFn>(1);
+    auto packed = g.address<PackedFn>(2);
+    auto *c = g.mx4_codes(3, M, H);
+    auto *e = g.mx4_scales(4, M, H);
+    auto *l = g.matrix<uint16_t>(5, kF16, rows, E);
+    if (g.ok && rows != M) g.ok = false;
+    const int64_t k = g.integer(6), F = g.integer(11), act = g.integer(12);
+    if (g.ok && (act < 0 || act > 1 || F < 0 || F > (int64_t(1) << 31))) g.ok = false;
+    const int64_t F1 = act == OT_MOE_SWIGLU ? 2 * F : F;
+    auto *w1 = g.ok ? g.vec<uint8_t>(7, at::kByte, (int64_t)packed(E * F1, H)) : nullptr;
+    auto *b1 = g.sized<float>(8, kF32, E, F1, true);
+    auto *w2 = g.ok ? g.vec<uint8_t>(9, at::kByte, (int64_t)packed(E * H, F)) : nullptr;
+    auto *b2 = g.sized<float>(10, kF32, E, H, true);
+    auto *y = g.sized<uint16_t>(13, kF16, M, H);
+    if (g.ok && g.a[14] == Py_None) g.ok = false;
+    auto *ws = g.scratch(14, [&] { return ws_size(M, H, F, E, k); });
+    auto *st = g.stream(15);
+    return g.call([&] { return fn(c, e, l, w1, b1, w2, b2, M, H, F, E, k, (int)act, y, ws, st); });
+  });
+}
+
 // (fn): the function that returns the current stream's handle
 PyObject *set_current_stream(PyObject *, PyObject *const *a, Py_ssize_t n) {
   if (n != 1 || !PyCallable_Check(a[0])) {
@@ -314,7 +434,9 @@ PyObject *set_current_stream(PyObject *, PyObject *const *a, Py_ssize_t n) {
 PyMethodDef kMethods[] = {
     OT_DEF(set_current_stream), OT_DEF(quantize_act), OT_DEF(quantize_act_per_token), OT_DEF(ln_quantize_act),
     OT_DEF(qlinear), OT_DEF(qlinear_noalloc), OT_DEF(qlinear_packed),
-    OT_DEF(qlinear_per_token), OT_DEF(qlinear_asym), {nullptr, nullptr, 0, nullptr}};
+    OT_DEF(qlinear_per_token), OT_DEF(qlinear_asym),
+    OT_DEF(quantize_act_mx4), OT_DEF(ln_quantize_act_mx4), OT_DEF(dequantize_mx4),
+    OT_DEF(qlinear_mx4), OT_DEF(moe_mx4), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_otbind", nullptr, -1, kMethods,
                        nullptr, nullptr, nullptr, nullptr};
 

@@ -55,6 +55,17 @@ _BOUND = {
 _n_quantize_act = _n_quantize_act_per_token = _n_ln_quantize_act = _unbound
 _n_qlinear = _n_qlinear_noalloc = _n_qlinear_packed = _unbound
 _n_qlinear_per_token = _n_qlinear_asym = _unbound
+# the same for the MX4 entry points
+_BOUND_MX4 = {
+    "quantize_act_mx4": ("ot_quantize_act_mx4",),
+    "ln_quantize_act_mx4": ("ot_ln_quantize_act_mx4",),
+    "dequantize_mx4": ("ot_dequantize_mx4",),
+    "qlinear_mx4": ("ot_qlinear_mx4", "ot_qlinear_mx4_workspace_size",
+                    "ot_packed_weights_mx4_size"),
+    "moe_mx4": ("ot_moe_mx4", "ot_moe_mx4_workspace_size", "ot_packed_weights_mx4_size"),
+}
+_n_quantize_act_mx4 = _n_ln_quantize_act_mx4 = _n_dequantize_mx4 = _unbound
+_n_qlinear_mx4 = _n_moe_mx4 = _unbound
 
 
 def _load_bind(L) -> None:
@@ -76,7 +87,7 @@ def _load_bind(L) -> None:
         return
     _bind = _otbind
     _otbind.set_current_stream(_current_stream)
-    for name, symbols in _BOUND.items():
+    for name, symbols in (*_BOUND.items(), *_BOUND_MX4.items()):
         addresses = [ctypes.cast(getattr(L, s), ctypes.c_void_p).value for s in symbols]
         globals()["_n_" + name] = partial(getattr(_otbind, name), *addresses)
 
@@ -650,6 +661,9 @@ def _mx4_pair(c, e, name, shape=None):
 def ot_quantize_act_mx4(x, z, inv_s, Xc, Xe, stream=None):
     """x [M, K] fp16 -> MX4 codes Xc and scales Xe of (x - z) * inv_s, or of x
     (z and inv_s both None).  Asynchronous."""
+    rc = _n_quantize_act_mx4(x, z, inv_s, Xc, Xe, stream)
+    if rc is not None:
+        return _check(rc, "ot_quantize_act_mx4")
     M, K = x.shape
     _, _, pc, pe = _mx4_pair(Xc, Xe, "X", (M, K))
     rc = lib().ot_quantize_act_mx4(_dev(x, torch.float16, "x"), M, K,
@@ -662,6 +676,9 @@ def ot_quantize_act_mx4(x, z, inv_s, Xc, Xe, stream=None):
 def ot_ln_quantize_act_mx4(h, gamma, beta, eps, z, inv_s, Xc, Xe, stream=None):
     """h [M, K] fp16 LayerNorm input -> MX4 codes and scales of the symmetrized
     and scaled LayerNorm output.  Asynchronous."""
+    rc = _n_ln_quantize_act_mx4(h, gamma, beta, eps, z, inv_s, Xc, Xe, stream)
+    if rc is not None:
+        return _check(rc, "ot_ln_quantize_act_mx4")
     M, K = h.shape
     _, _, pc, pe = _mx4_pair(Xc, Xe, "X", (M, K))
     rc = lib().ot_ln_quantize_act_mx4(_dev(h, torch.float16, "h"), M, K,
@@ -688,6 +705,9 @@ def ot_fold_weights_mx4(W, b, z, s, Wc, We, bprime, stream=None):
 def ot_dequantize_mx4(c, e, y, stream=None):
     """MX4 codes and scales of [rows, K] -> their values y [rows, K] fp32.
     Asynchronous."""
+    rc = _n_dequantize_mx4(c, e, y, stream)
+    if rc is not None:
+        return _check(rc, "ot_dequantize_mx4")
     rows, K, pc, pe = _mx4_pair(c, e, "the matrix")
     rc = lib().ot_dequantize_mx4(pc, pe, rows, K, _dev(y, torch.float32, "y", (rows, K)),
                                  _stream(stream))
@@ -725,6 +745,9 @@ def _scratch(workspace, need):
 def ot_qlinear_mx4(Xc, Xe, Wp, N, bprime, Y, workspace=None, stream=None):
     """Xc, Xe [M, K] in MX4, Wp packed MX4 weights of N output channels, bprime
     [N] fp32 -> Y [M, N] fp16.  Asynchronous."""
+    rc = _n_qlinear_mx4(Xc, Xe, Wp, N, bprime, Y, workspace, stream)
+    if rc is not None:
+        return _check(rc, "ot_qlinear_mx4")
     M, K, pc, pe = _mx4_pair(Xc, Xe, "X")
     rc = lib().ot_qlinear_mx4(pc, pe,
                               _dev(Wp, torch.uint8, "Wp", (ot_packed_weights_mx4_size(N, K),)),
@@ -751,6 +774,10 @@ def ot_moe_mx4(Xc, Xe, logits, top_k, W1p, b1, W2p, b2, F, act, Y, workspace, st
     Asynchronous."""
     if act not in MOE_ACTIVATIONS:
         raise ValueError(f"act must be one of {sorted(MOE_ACTIVATIONS)}, got {act!r}")
+    rc = _n_moe_mx4(Xc, Xe, logits, top_k, W1p, b1, W2p, b2, F, MOE_ACTIVATIONS[act], Y, workspace,
+                    stream)
+    if rc is not None:
+        return _check(rc, "ot_moe_mx4")
     M, H, pc, pe = _mx4_pair(Xc, Xe, "X")
     if not isinstance(logits, torch.Tensor) or logits.dim() != 2:
         raise ValueError("logits must be a tensor [M, E]")

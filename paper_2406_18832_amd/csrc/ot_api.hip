@@ -475,9 +475,8 @@ ot_status ot_qlinear_mx4(const uint8_t *Xc, const uint8_t *Xe, const uint8_t *Wp
   if (!aligned16(Xc) || !aligned16(Xe) || !aligned16(Wp) || !aligned16(bprime) || !aligned16(Y) ||
       !aligned16(workspace))
     return OT_EINVAL;
-  hipStream_t st = static_cast<hipStream_t>(stream);
-  return hip_status(M <= 64 ? ot::launch_mx4_decode(Xc, Xe, Wp, bprime, M, N, K, Y, st)
-                            : ot::launch_mx4_gemm(Xc, Xe, Wp, bprime, M, N, K, Y, st));
+  return hip_status(ot::launch_mx4_linear(Xc, Xe, Wp, bprime, M, N, K, Y,
+                                          static_cast<hipStream_t>(stream)));
 }
 
 size_t ot_qlinear_mx4_workspace_size(int64_t M, int64_t N, int64_t K) {
@@ -494,7 +493,7 @@ static bool moe_shape_ok(int64_t M, int64_t H, int64_t F, int64_t E, int64_t top
 
 size_t ot_moe_mx4_workspace_size(int64_t M, int64_t H, int64_t F, int64_t E, int64_t top_k) {
   if (M <= 0 || !moe_shape_ok(M, H, F, E, top_k)) return 0;
-  return ot::moe_mx4_workspace_bytes(M, F, top_k);
+  return ot::moe_mx4_workspace_bytes(M, F, E, top_k);
 }
 
 ot_status ot_moe_mx4(const uint8_t *Xc, const uint8_t *Xe, const uint16_t *logits,

@@ -121,19 +121,19 @@ hipError_t launch_dequantize_mx4(const uint8_t *c, const uint8_t *e, int64_t row
 hipError_t launch_pack_weights_mx4(const uint8_t *Wc, const uint8_t *We, int64_t N, int64_t K,
                                    uint8_t *Wp, hipStream_t st);
 
-// The product above 64 tokens; whether its tiles' count fits a launch.
-bool mx4_gemm_fits(int64_t M, int64_t N);
-const char *mx4_gemm_tile_name(int64_t M, int64_t N, int64_t K);
+// The product: up to 64 tokens mostly by streaming the weights
+// (ot_mx4_decode.hip), else on tiles.
+hipError_t launch_mx4_linear(const uint8_t *Xc, const uint8_t *Xe, const uint8_t *Wp,
+                             const float *bp, int64_t M, int64_t N, int64_t K, uint16_t *Y,
+                             hipStream_t st);
+// The tiles; whether their count fits a launch, and the one that is picked.
 hipError_t launch_mx4_gemm(const uint8_t *Xc, const uint8_t *Xe, const uint8_t *Wp,
                            const float *bp, int64_t M, int64_t N, int64_t K, uint16_t *Y,
                            hipStream_t st);
-// The product up to 64 tokens, bound by streaming the weights.
-hipError_t launch_mx4_decode(const uint8_t *Xc, const uint8_t *Xe, const uint8_t *Wp,
-                             const float *bp, int64_t M, int64_t N, int64_t K, uint16_t *Y,
-                             hipStream_t st);
-
+bool mx4_gemm_fits(int64_t M, int64_t N);
+const char *mx4_gemm_tile_name(int64_t M, int64_t N, int64_t K);
 // A mixture-of-experts layer; workspace of at least moe_mx4_workspace_bytes.
-size_t moe_mx4_workspace_bytes(int64_t M, int64_t F, int64_t top_k);
+size_t moe_mx4_workspace_bytes(int64_t M, int64_t F, int64_t E, int64_t top_k);
 hipError_t launch_moe_mx4(const uint8_t *Xc, const uint8_t *Xe, const uint16_t *logits,
                           const uint8_t *W1, const float *b1, const uint8_t *W2, const float *b2,
                           int64_t M, int64_t H, int64_t F, int64_t E, int64_t top_k, bool glu,

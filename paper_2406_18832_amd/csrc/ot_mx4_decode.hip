@@ -3,43 +3,31 @@
 // Bound by reading the weights.  A workgroup takes 16 RB weight rows and all
 // tokens; its waves share out the K tiles and add their fp32 sums through LDS
 // in wave order (ot_mx4_stream.h).
+//
+// Up to 16 tokens a wave loads the tokens' codes straight into registers.  With
+// more, those loads (pieces of 32 bytes from each of 16 rows) cost more than the
+// weights': there the wave copies its K tile of all tokens into LDS of its own,
+// whole 128-byte row pieces at a time, and takes the fragments from there.  No
+// wave waits for another before the sums meet.
 #include "ot_mx4_stream.h"
+#include "ot_mx4_tiles.h"
 
 namespace ot {
 namespace detail {
 
-template <int RB, int MB, int kDepth, int kMaxWaves>
-__global__ __launch_bounds__(64 * kMaxWaves) void mx4_decode_kernel(
-    const uint8_t *__restrict__ Xc, const uint8_t *__restrict__ Xe, const uint8_t *__restrict__ Wp,
-    const float *__restrict__ bp, int M, int N, int K, int tiles, uint16_t *__restrict__ Y) {
-  extern __shared__ v4f red[];  // [waves][RB][MB][64]
-  const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int waves = blockDim.x >> 6;
-  const int64_t u0 = (int64_t)blockIdx.x * RB;
-
-  Mx4Rows<RB> w;
-  w.aim(Wp, (N + 31) / 32, tiles, u0, lane);
-  Mx4Cols<MB> x;
-  x.open(Xc, Xe, M, K);
-#pragma unroll
-  for (int j = 0; j < MB; ++j) {
-    const int m = 16 * j + (lane & 15);
-    x.aim(j, m < M ? m : -1, K, lane);
-  }
-  v4f acc[RB][MB];
-#pragma unroll
-  for (int i = 0; i < RB; ++i)
-#pragma unroll
-    for (int j = 0; j < MB; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
-  mx4_stream<RB, MB, kDepth>(acc, w, x, wave, tiles, waves, lane);
+// Adds the waves' sums, in wave order, and writes the outputs.  red: [waves][RB]
+// [MB][64]; lane l of block (i, j) holds token 16 j + l mod 16 and rows
+// 4 (l / 16) .. +3 of unit u0 + i.
+template <int RB, int MB>
+__device__ __forceinline__ void mx4_decode_finish(const v4f (&acc)[RB][MB], v4f *red, int64_t u0,
+                                                  const float *__restrict__ bp, int M, int N,
+                                                  uint16_t *__restrict__ Y, int wave, int waves,
+                                                  int lane) {
 #pragma unroll
   for (int i = 0; i < RB; ++i)
 #pragma unroll
     for (int j = 0; j < MB; ++j) red[((wave * RB + i) * MB + j) * 64 + lane] = acc[i][j];
   __syncthreads();
-  // item o: lane l of block (i, j) holds token 16 j + l mod 16 and rows
-  // 4 (l / 16) .. +3 of unit i
   for (int o = threadIdx.x; o < RB * MB * 64; o += blockDim.x) {
     v4f s = red[o];
     for (int v = 1; v < waves; ++v) s += red[v * RB * MB * 64 + o];
@@ -62,17 +50,154 @@ __global__ __launch_bounds__(64 * kMaxWaves) void mx4_decode_kernel(
   }
 }
 
-template <int RB, int MB, int kDepth, int kMaxWaves>
+// Up to 16 tokens.
+template <int RB, int kMaxWaves>
+__global__ __launch_bounds__(64 * kMaxWaves) void mx4_decode_kernel(
+    const uint8_t *__restrict__ Xc, const uint8_t *__restrict__ Xe, const uint8_t *__restrict__ Wp,
+    const float *__restrict__ bp, int M, int N, int K, int tiles, uint16_t *__restrict__ Y) {
+  extern __shared__ v4f red[];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int waves = blockDim.x >> 6;
+  const int64_t u0 = (int64_t)blockIdx.x * RB;
+  Mx4Rows<RB> w;
+  w.aim(Wp, (N + 31) / 32, tiles, u0, lane);
+  Mx4Cols<1> x;
+  x.open(Xc, Xe, M, K);
+  x.aim(0, (lane & 15) < M ? lane & 15 : -1, K, lane);
+  v4f acc[RB][1];
+#pragma unroll
+  for (int i = 0; i < RB; ++i) acc[i][0] = v4f{0.f, 0.f, 0.f, 0.f};
+  mx4_stream<RB, 1, 2>(acc, w, x, wave, tiles, waves, lane);
+  mx4_decode_finish<RB, 1>(acc, red, u0, bp, M, N, Y, wave, waves, lane);
+}
+
+// 17 to 16 MB tokens: a wave's LDS is its K tile of 16 MB token rows, 128 bytes
+// each, 16-byte chunk c of row r at chunk c ^ swz_mx4(r).
+template <int RB, int MB>
+struct Mx4LdsFrag {
+  v4i a[RB][2];
+  uint32_t ea[RB], eb[MB];
+};
+
+template <int RB, int MB, int kMaxWaves>
+__global__ __launch_bounds__(64 * kMaxWaves) void mx4_decode_lds_kernel(
+    const uint8_t *__restrict__ Xc, const uint8_t *__restrict__ Xe, const uint8_t *__restrict__ Wp,
+    const float *__restrict__ bp, int M, int N, int K, int tiles, uint16_t *__restrict__ Y) {
+  extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int waves = blockDim.x >> 6;
+  const int64_t u0 = (int64_t)blockIdx.x * RB;
+  const int r = lane & 15, q = lane >> 4, KB = K / 2;
+  Mx4Rows<RB> w;
+  w.aim(Wp, (N + 31) / 32, tiles, u0, lane);
+  const __amdgpu_buffer_rsrc_t rx = make_rsrc(Xc, (uint32_t)(M * KB));
+  const __amdgpu_buffer_rsrc_t re = make_rsrc(Xe, (uint32_t)(tiles * M * 8));
+  uint8_t *const own = lds + wave * (MB * 2048);
+  // rows 8 j + lane / 8: the swizzle of their chunk goes by 8 (j mod 2)
+  const int row8 = lane >> 3;
+  const int ck0 = ((lane & 7) ^ swz_mx4(row8)) * 16, ck1 = ((lane & 7) ^ swz_mx4(8 + row8)) * 16;
+  int off_f[2];
+#pragma unroll
+  for (int p = 0; p < 2; ++p)
+    off_f[p] = r * 128 + 16 * ((4 * (q & 1) + 2 * p + (q >> 1)) ^ swz_mx4(r));
+
+  // K tile t: the tokens to LDS, then the weights and scales to registers
+  auto issue = [&](Mx4LdsFrag<RB, MB> &f, int t) {
+    const int k0 = t * kMx4TileBytes;
+#pragma unroll
+    for (int j = 0; j < 2 * MB; ++j) {
+      const int ck = j & 1 ? ck1 : ck0;
+      if (8 * j < M)  // the other rows' columns are never written
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(
+            rx, (lds_void *)(own + j * 1024), 16,
+            k0 + ck < KB ? (uint32_t)((8 * j + row8) * KB + k0 + ck) : kOobOffset, 0, 0, 0);
+    }
+    asm volatile("" ::: "memory");  // the copies are the older loads
+#pragma unroll
+    for (int j = 0; j < MB; ++j)
+      f.eb[j] = __builtin_amdgcn_raw_buffer_load_b32(
+          re, (uint32_t)(t * M + 16 * j + r) * 8 + 4 * (q & 1), 0, 0);
+#pragma unroll
+    for (int i = 0; i < RB; ++i) {
+      const v4i *p = reinterpret_cast<const v4i *>(w.codes[i] + (int64_t)t * kMx4PackedTile);
+      f.ea[i] = *reinterpret_cast<const uint32_t *>(w.scales[i] + t * w.scale_step);
+      f.a[i][0] = __builtin_nontemporal_load(p);
+      f.a[i][1] = __builtin_nontemporal_load(p + 128);
+    }
+    asm volatile("" ::: "memory");
+  };
+  v4f acc[RB][MB];
+#pragma unroll
+  for (int i = 0; i < RB; ++i)
+#pragma unroll
+    for (int j = 0; j < MB; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
+  // The tile in f: once its weights are here (loads return in order) the older
+  // copies have landed.  The tokens' fragments out of LDS, then the next tile's
+  // loads, then the products.
+  auto step = [&](Mx4LdsFrag<RB, MB> &f, Mx4LdsFrag<RB, MB> &next, int t) {
+#pragma unroll
+    for (int i = 0; i < RB; ++i)
+      asm volatile("" : "+v"(f.a[i][0]), "+v"(f.a[i][1]), "+v"(f.ea[i])::"memory");
+    v4i b[MB][2];
+#pragma unroll
+    for (int j = 0; j < MB; ++j)
+#pragma unroll
+      for (int p = 0; p < 2; ++p)
+        b[j][p] = *reinterpret_cast<const v4i *>(own + j * 2048 + off_f[p]);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // before the copies below
+#pragma unroll
+    for (int j = 0; j < MB; ++j) asm volatile("" : "+v"(b[j][0]), "+v"(b[j][1])::"memory");
+    if (t + waves < tiles) issue(next, t + waves);
+    const int down = 8 * (lane >> 5);
+#pragma unroll
+    for (int i = 0; i < RB; ++i)
+#pragma unroll
+      for (int j = 0; j < MB; ++j)
+        acc[i][j] = mfma_mx4_16<0>(f.a[i][0], b[j][0], acc[i][j], f.ea[i] >> down, f.eb[j] >> down);
+#pragma unroll
+    for (int i = 0; i < RB; ++i)
+#pragma unroll
+      for (int j = 0; j < MB; ++j)
+        acc[i][j] = mfma_mx4_16<2>(f.a[i][1], b[j][1], acc[i][j], f.ea[i] >> down, f.eb[j] >> down);
+  };
+  Mx4LdsFrag<RB, MB> f0, f1;
+  if (wave < tiles) issue(f0, wave);
+  for (int t = wave; t < tiles; t += 2 * waves) {
+    step(f0, f1, t);
+    if (t + waves < tiles) step(f1, f0, t + waves);
+  }
+  __syncthreads();  // the waves' LDS becomes the sums'
+  mx4_decode_finish<RB, MB>(acc, reinterpret_cast<v4f *>(lds), u0, bp, M, N, Y, wave, waves, lane);
+}
+
+// Waves of a workgroup: as many as share the K tiles evenly.
+template <int kMaxWaves>
+int decode_waves(int tiles) {
+  const int rounds = (tiles + kMaxWaves - 1) / kMaxWaves;
+  return (tiles + rounds - 1) / rounds;
+}
+
+template <int RB, int kMaxWaves>
 hipError_t launch_decode(const uint8_t *Xc, const uint8_t *Xe, const uint8_t *Wp, const float *bp,
                          int64_t M, int64_t N, int64_t K, uint16_t *Y, hipStream_t st) {
-  const int tiles = (int)mx4_tiles(K);
-  // waves: as many as share the K tiles evenly
-  const int rounds = (tiles + kMaxWaves - 1) / kMaxWaves;
-  const int waves = (tiles + rounds - 1) / rounds;
+  const int tiles = (int)mx4_tiles(K), waves = decode_waves<kMaxWaves>(tiles);
   const unsigned grid = (unsigned)(((N + 15) / 16 + RB - 1) / RB);
-  mx4_decode_kernel<RB, MB, kDepth, kMaxWaves>
-      <<<grid, 64 * waves, (size_t)waves * RB * MB * 1024, st>>>(Xc, Xe, Wp, bp, (int)M, (int)N,
-                                                                 (int)K, tiles, Y);
+  mx4_decode_kernel<RB, kMaxWaves><<<grid, 64 * waves, (size_t)waves * RB * 1024, st>>>(
+      Xc, Xe, Wp, bp, (int)M, (int)N, (int)K, tiles, Y);
+  return hipGetLastError();
+}
+
+template <int RB, int MB, int kMaxWaves>
+hipError_t launch_decode_lds(const uint8_t *Xc, const uint8_t *Xe, const uint8_t *Wp,
+                             const float *bp, int64_t M, int64_t N, int64_t K, uint16_t *Y,
+                             hipStream_t st) {
+  static_assert(RB <= 2, "the sums fit the waves' LDS");
+  const int tiles = (int)mx4_tiles(K), waves = decode_waves<kMaxWaves>(tiles);
+  const unsigned grid = (unsigned)(((N + 15) / 16 + RB - 1) / RB);
+  mx4_decode_lds_kernel<RB, MB, kMaxWaves><<<grid, 64 * waves, (size_t)waves * MB * 2048, st>>>(
+      Xc, Xe, Wp, bp, (int)M, (int)N, (int)K, tiles, Y);
   return hipGetLastError();
 }
 
@@ -80,12 +205,41 @@ hipError_t launch_decode(const uint8_t *Xc, const uint8_t *Xe, const uint8_t *Wp
 
 using namespace detail;
 
-hipError_t launch_mx4_decode(const uint8_t *Xc, const uint8_t *Xe, const uint8_t *Wp,
+// Which kernel: 16 rows to a workgroup where that is at most one of them per CU
+// (more, and they read the tokens too often), or where the whole launch is
+// latency; else 32.  From 33 tokens on, with more 32-row workgroups than CUs,
+// the tiles of ot_mx4_gemm.hip, which read the tokens once per 64 or 128 rows.
+// Measured on MI355X, 16 and 32 rows (us):
+//   up to 16 tokens  9 x 3466, K = 24416 12.0 and 15.6; 16 x 5120, K = 20480
+//                    20.2 and 15.2; 8 x 20480, K = 5120 14.0 and 12.2;
+//                    2 x 4352, K = 1024 3.0 and 3.2
+//   17 .. 32         24 x 3840, K = 22528 12.5 and 15.8; 32 x 20480, K = 5120
+//                    17.5 and 14.1
+//   33 .. 64         40 x 3840, K = 22528 15.9 and 19.5; 45 x 5888, K = 14336
+//                    20.0 and 14.6 (64 x 64 tiles 22.8); 64 x 20480, K = 5120
+//                    23.8 and 21.7 (128 x 64 tiles 15.2)
+enum class DecodePlan { kRows16, kRows32, kTiles };
+static DecodePlan decode_plan(int64_t M, int64_t N, int64_t K) {
+  const int64_t cus = device_cus();
+  if (N <= 16 * cus) return DecodePlan::kRows16;
+  if (M <= 16) return N * K < (int64_t(1) << 24) ? DecodePlan::kRows16 : DecodePlan::kRows32;
+  return M <= 32 || N <= 32 * cus ? DecodePlan::kRows32 : DecodePlan::kTiles;
+}
+
+hipError_t launch_mx4_linear(const uint8_t *Xc, const uint8_t *Xe, const uint8_t *Wp,
                              const float *bp, int64_t M, int64_t N, int64_t K, uint16_t *Y,
                              hipStream_t st) {
-  if (M <= 16) return launch_decode<1, 1, 4, 16>(Xc, Xe, Wp, bp, M, N, K, Y, st);
-  if (M <= 32) return launch_decode<2, 2, 2, 8>(Xc, Xe, Wp, bp, M, N, K, Y, st);
-  return launch_decode<2, 4, 2, 8>(Xc, Xe, Wp, bp, M, N, K, Y, st);
+  const DecodePlan plan = M <= 64 ? decode_plan(M, N, K) : DecodePlan::kTiles;
+  if (plan == DecodePlan::kTiles) return launch_mx4_gemm(Xc, Xe, Wp, bp, M, N, K, Y, st);
+  const bool narrow = plan == DecodePlan::kRows16;
+  if (M <= 16)
+    return narrow ? launch_decode<1, 16>(Xc, Xe, Wp, bp, M, N, K, Y, st)
+                  : launch_decode<2, 8>(Xc, Xe, Wp, bp, M, N, K, Y, st);
+  if (M <= 32)
+    return narrow ? launch_decode_lds<1, 2, 8>(Xc, Xe, Wp, bp, M, N, K, Y, st)
+                  : launch_decode_lds<2, 2, 8>(Xc, Xe, Wp, bp, M, N, K, Y, st);
+  return narrow ? launch_decode_lds<1, 4, 8>(Xc, Xe, Wp, bp, M, N, K, Y, st)
+                : launch_decode_lds<2, 4, 8>(Xc, Xe, Wp, bp, M, N, K, Y, st);
 }
 
 }  // namespace ot

@@ -8,14 +8,14 @@
 //
 // Bound by reading the weights of the experts that some token chose, each once.
 //
-// Kernel 1: a workgroup takes 32 hidden channels of one expert and the tokens
-// that chose it (found from the logits by every workgroup for itself: counting
-// the logits before the expert's own takes less than a launch would), runs fc1
-// over H with its waves sharing the K tiles, then forms the activation and the
-// MX4 block of each token's 32 channels, which go to the workspace as row
-// m top_k + j.  Experts that nobody chose have workgroups that end at once; with
+// Kernel 1: a workgroup serves one expert and the tokens that chose it (found
+// from the logits by every workgroup for itself: counting the logits before the
+// expert's own takes less than a launch would).  A wave runs fc1 over H for 32
+// hidden channels (or, where there are few, shares the K tiles with others), then
+// forms the activation and the MX4 block of each token's 32 channels, which go to
+// the workspace in the operand order of the other kernel.  Experts that nobody chose have workgroups that end at once; with
 // fewer choices than experts the workgroups go by choice instead of by expert.
-// One workgroup more writes down every token's experts and weights.
+// A row of workgroups more writes down every token's experts and weights.
 //
 // Kernel 2: a workgroup takes 16 output channels and all tokens.  Its waves
 // share out the K tiles of all chosen experts in one row, add p_j times each
@@ -26,7 +26,7 @@
 namespace ot {
 namespace detail {
 
-constexpr int kMoeWaves1 = 8, kMoeWaves2 = 16;
+constexpr int kMoeWaves1 = 4, kMoeWaves2 = 16;
 
 // A token's logit for expert e as an integer that orders as the choice does:
 // larger comes first, the lower expert first among equals, -0 equal to 0, NaN
@@ -51,19 +51,37 @@ __device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
   return v;
 }
 
-// The largest of a token's keys below `below` (0: none), over the wave.
-__device__ __forceinline__ uint32_t moe_next(const uint16_t *__restrict__ l, int E, uint32_t below,
-                                             int lane) {
-  uint32_t best = 0;
-  for (int e = lane; e < E; e += 64) {
-    const uint32_t k = moe_key(l[e], e);
-    if (k < below) best = max(best, k);
+// A token's keys over a wave, OT_MOE_MAX_EXPERTS / 64 to a lane (0: no expert).
+struct MoeKeys {
+  static constexpr int kLane = OT_MOE_MAX_EXPERTS / 64;
+  uint32_t k[kLane];
+  __device__ __forceinline__ MoeKeys(const uint16_t *__restrict__ l, int E, int lane) {
+#pragma unroll
+    for (int i = 0; i < kLane; ++i) {
+      const int e = 64 * i + lane;
+      k[i] = e < E ? moe_key(l[e], e) : 0;
+    }
   }
-  return wave_max_u32(best);
-}
+  // the largest key below `below` (0: none)
+  __device__ __forceinline__ uint32_t next(uint32_t below) const {
+    uint32_t best = 0;
+#pragma unroll
+    for (int i = 0; i < kLane; ++i)
+      if (k[i] < below) best = max(best, k[i]);
+    return wave_max_u32(best);
+  }
+};
 
+// Hidden rows.  An expert's tokens in order take columns 0, 1, ..; with G =
+// ceil(M / 16) and T = ceil(F / 256), columns 16 g .. +15 of expert e are
+//   codes  [e G + g][T][2 instructions][64 lanes][16 bytes]
+//   scales [e G + g][T][64 lanes][4 bytes]  (bytes 0 and 2: instructions 0 and 1)
+// as v_mfma_scale_f32_16x16x128_f8f6f4 takes them (ot_mx4_stream.h), so that the
+// other kernel's loads are whole KiB.  Row by row, those loads (32 bytes from each
+// of 16 rows) took longer than its weights'.  Most of it is never touched; it is
+// M / 2H of the experts' weights at most.
 struct MoeWs {
-  uint8_t *codes, *scales;  // hidden rows [M top_k][F / 2], [T][M top_k][8]
+  uint8_t *codes, *scales;
   int *expert;              // [M top_k], -1: none
   float *weight;            // [M top_k]
 };
@@ -78,38 +96,37 @@ struct MoeArgs {
   MoeWs ws;
 };
 
-// Every token's experts and weights (one workgroup).
-__device__ void moe_route(const MoeArgs &a) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int m = wave; m < a.M; m += blockDim.x >> 6) {
-    const uint16_t *l = a.logits + (int64_t)m * a.E;
-    uint32_t key = 0xffffffffu;
-    float most = 0.f, sum = 0.f, w = 0.f;
-    int expert = -1;
-    for (int j = 0; j < a.top_k; ++j) {
-      key = moe_next(l, a.E, key, lane);
-      if (!moe_chosen(key)) break;
-      const float v = moe_logit(key);
-      if (j == 0) most = v;
-      const float x = v == most ? 1.f : expf(v - most);
-      sum += x;
-      if (lane == j) {
-        w = x;
-        expert = 0xffff - (int)(key & 0xffff);
-      }
+// Token m's experts and weights, by one wave.
+__device__ __forceinline__ void moe_route(const MoeArgs &a, int m, int lane) {
+  const MoeKeys keys(a.logits + (int64_t)m * a.E, a.E, lane);
+  uint32_t key = 0xffffffffu;
+  float most = 0.f, sum = 0.f, w = 0.f;
+  int expert = -1;
+  for (int j = 0; j < a.top_k; ++j) {
+    key = keys.next(key);
+    if (!moe_chosen(key)) break;
+    const float v = moe_logit(key);
+    if (j == 0) most = v;
+    const float x = v == most ? 1.f : expf(v - most);
+    sum += x;
+    if (lane == j) {
+      w = x;
+      expert = 0xffff - (int)(key & 0xffff);
     }
-    if (lane < a.top_k) {
-      a.ws.expert[m * a.top_k + lane] = expert;
-      a.ws.weight[m * a.top_k + lane] = expert < 0 ? 0.f : w / sum;
-    }
+  }
+  if (lane < a.top_k) {
+    a.ws.expert[m * a.top_k + lane] = expert;
+    a.ws.weight[m * a.top_k + lane] = expert < 0 ? 0.f : w / sum;
   }
 }
 
-// The hidden rows of up to 16 MB of an expert's tokens, columns c0 .. of its
-// list: fc1 over H, activation, MX4.
+// The hidden channels 32 f .. +31 of up to 16 MB of an expert's tokens (columns c0
+// .. of its list): fc1 over H by this wave, or its share `part` of `parts` waves'
+// K tiles, whose sums meet in red; activation; MX4.
 template <bool GLU, int MB>
-__device__ __forceinline__ void moe_hidden(const MoeArgs &a, v4f *red, int e, int f, int c0,
-                                           int count, const int *list, const int *rank_of) {
+__device__ __forceinline__ void moe_hidden(const MoeArgs &a, v4f *red, int part, int parts, int e,
+                                           int f, int c0, int count, const int *list,
+                                           const int *rank_of) {
   constexpr int RB = GLU ? 4 : 2;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -148,72 +165,90 @@ __device__ __forceinline__ void moe_hidden(const MoeArgs &a, v4f *red, int e, in
   for (int i = 0; i < RB; ++i)
 #pragma unroll
     for (int j = 0; j < MB; ++j) acc[i][j] = v4f{0.f, 0.f, 0.f, 0.f};
-  mx4_stream<RB, MB, RB * MB == 8 ? 1 : 2>(acc, w, x, wave, tiles, kMoeWaves1, lane);
+  mx4_stream<RB, MB, RB * MB == 8 ? 1 : 2>(acc, w, x, part, tiles, parts, lane);
+  if (parts > 1) {  // the same for the whole workgroup
+    __syncthreads();  // an earlier call's sums are read
 #pragma unroll
-  for (int i = 0; i < RB; ++i)
+    for (int i = 0; i < RB; ++i)
 #pragma unroll
-    for (int j = 0; j < MB; ++j) red[((wave * RB + i) * MB + j) * 64 + lane] = acc[i][j];
-  __syncthreads();
+      for (int j = 0; j < MB; ++j) red[((wave * RB + i) * MB + j) * 64 + lane] = acc[i][j];
+    __syncthreads();
+    if (part > 0) return;
+    for (int v = 1; v < parts; ++v)
+#pragma unroll
+      for (int i = 0; i < RB; ++i)
+#pragma unroll
+        for (int j = 0; j < MB; ++j) acc[i][j] += red[(((wave + v) * RB + i) * MB + j) * 64 + lane];
+  }
+  if (f >= a.F / 32) return;  // a wave past the last channels
 
-  // activation and MX4: a quad of lanes to a token, 8 channels to a lane
-  if (threadIdx.x >= MB * 64) return;
-  const int col = threadIdx.x >> 2, q = threadIdx.x & 3;
-  float g[RB / 2][8];
+  // Lane l holds, for column l mod 16, rows 4 (l / 16) .. +3 of each unit: eight
+  // channels of the token's block, whose four lanes are 16 apart.
+  const int q = lane >> 4;
+  const int64_t b_at = row0 + 4 * q;
+  float b1[RB][4];
 #pragma unroll
-  for (int u = 0; u < RB / 2; ++u)  // (the gate's and) the value's 32 rows
+  for (int i = 0; i < RB; ++i) {
+    const float4 v = a.b1 ? *reinterpret_cast<const float4 *>(a.b1 + b_at + (i >> 1) * (int64_t)a.F +
+                                                             16 * (i & 1))
+                          : make_float4(0.f, 0.f, 0.f, 0.f);
+    b1[i][0] = v.x; b1[i][1] = v.y; b1[i][2] = v.z; b1[i][3] = v.w;
+  }
 #pragma unroll
-    for (int v = 0; v < 2; ++v) {
-      const int i = 2 * u + (q >> 1), l = 16 * (2 * (q & 1) + v) + (col & 15);
-      v4f s = v4f{0.f, 0.f, 0.f, 0.f};
+  for (int j = 0; j < MB; ++j) {
+    float h[8];
 #pragma unroll
-      for (int wv = 0; wv < kMoeWaves1; ++wv)
-        s += red[((wv * RB + i) * MB + (col >> 4)) * 64 + l];
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const int64_t row = row0 + u * (int64_t)a.F + 8 * q + 4 * v + t;
-        g[u][4 * v + t] = s[t] + (a.b1 ? a.b1[row] : 0.f);
+    for (int t = 0; t < 8; ++t) {
+      const int u = t >> 2, r = t & 3;
+      const float g = acc[u][j][r] + b1[u][r];
+      if constexpr (GLU) {
+        const float up = acc[RB / 2 + u][j][r] + b1[RB / 2 + u][r];
+        h[t] = g / (1.f + expf(-g)) * up;
+      } else {
+        h[t] = g > 0.f || g != g ? g : 0.f;  // keeps a NaN
       }
     }
-  float h[8];
+    uint32_t most = abs_bits(h[0]);
 #pragma unroll
-  for (int t = 0; t < 8; ++t) {
-    if constexpr (GLU) {
-      const float silu = g[0][t] / (1.f + expf(-g[0][t]));
-      h[t] = silu * g[RB / 2 - 1][t];
-    } else {
-      h[t] = g[0][t] > 0.f || g[0][t] != g[0][t] ? g[0][t] : 0.f;  // keeps a NaN
+    for (int t = 1; t < 8; ++t) most = max(most, abs_bits(h[t]));
+    most = max(most, (uint32_t)__shfl_xor((int)most, 16));
+    most = max(most, (uint32_t)__shfl_xor((int)most, 32));
+    const uint32_t b = mx4_scale_byte(most);
+    const uint32_t codes = mx4_codes8(h, b);
+    const int c = c0 + 16 * j + (lane & 15);
+    if (c >= count) continue;
+    // block f of the row is block 4 hf + st of K tile f / 8: instruction st / 2,
+    // lane group hf + 2 (st mod 2)
+    const int64_t group = (int64_t)e * ((a.M + 15) / 16) + (c >> 4), tiles2 = (a.F + 255) / 256;
+    auto lane_of = [&](int blk) { return 16 * ((blk >> 2) + 2 * (blk & 1)) + (c & 15); };
+    const int blk = f & 7;
+    uint16_t *dst = reinterpret_cast<uint16_t *>(
+        a.ws.codes + (group * tiles2 + (f >> 3)) * 2048 + (blk >> 1 & 1) * 1024 +
+        lane_of(blk) * 16 + 2 * q);
+    dst[0] = (uint16_t)codes;
+    dst[4] = (uint16_t)(codes >> 16);
+    if (q == 0) {
+      uint8_t *sc = a.ws.scales + (group * tiles2 + (f >> 3)) * 256;
+      sc[lane_of(blk) * 4 + (blk & 2)] = (uint8_t)b;
+      if (f == a.F / 32 - 1)  // the last tile's scales past F: a finite one, against zeros
+        for (int i = blk + 1; i < 8; ++i) sc[lane_of(i) * 4 + (i & 2)] = 0;
     }
-  }
-  uint32_t most = abs_bits(h[0]);
-#pragma unroll
-  for (int t = 1; t < 8; ++t) most = max(most, abs_bits(h[t]));
-  const uint32_t b = mx4_scale_byte(quad_max(most));
-  const uint32_t codes = mx4_codes8(h, b);
-  if (c0 + col >= count) return;
-  const int m = list[c0 + col], rows = a.M * a.top_k;
-  const int64_t slot = (int64_t)m * a.top_k + rank_of[m];
-  *reinterpret_cast<uint32_t *>(a.ws.codes + slot * (a.F / 2) + 16 * f + 4 * q) = codes;
-  if (q == 0) {
-    a.ws.scales[((int64_t)(f >> 3) * rows + slot) * 8 + (f & 7)] = (uint8_t)b;
-    // the last tile's scales past F
-    if (f == a.F / 32 - 1)
-      for (int i = f + 1; i & 7; ++i) a.ws.scales[((int64_t)(i >> 3) * rows + slot) * 8 + (i & 7)] = 0;
   }
 }
 
-// gridDim.x = F / 32 (+ 1: the routing), gridDim.y = min(E, M top_k).  An expert
-// of more than 16 tokens takes 32 at a time (MB 2), reading its weights again for
-// the second 32.
+// gridDim.x = 1 (the routing) + groups of hidden blocks, gridDim.y = min(E, M top_k).  A workgroup's waves take kMoeWaves1 / parts blocks of 32 hidden
+// channels, `parts` waves each.  An expert of more than 16 tokens takes 32 at a
+// time (MB 2), reading its weights again for the second 32.
 template <bool GLU, int MB>
-__global__ __launch_bounds__(64 * kMoeWaves1) void moe_mx4_hidden_kernel(MoeArgs a) {
-  __shared__ v4f red[kMoeWaves1 * (GLU ? 4 : 2) * MB * 64];
+__global__ __launch_bounds__(64 * kMoeWaves1, 2) void moe_mx4_hidden_kernel(MoeArgs a, int parts) {
+  extern __shared__ v4f red[];  // parts > 1: [waves][RB][MB][64]
   __shared__ int first_of, list[64], rank_of[64];
   __shared__ unsigned long long members;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int f = blockIdx.x, hidden_tiles = a.F / 32;
-  if (f == hidden_tiles) {
-    if (blockIdx.y == 0) moe_route(a);
+  if (blockIdx.x == 0) {  // first, since the other kernel waits for it: the routing
+    for (int m = blockIdx.y * kMoeWaves1 + wave; m < a.M; m += gridDim.y * kMoeWaves1)
+      moe_route(a, m, lane);
     return;
   }
 
@@ -223,8 +258,9 @@ __global__ __launch_bounds__(64 * kMoeWaves1) void moe_mx4_hidden_kernel(MoeArgs
   if (by_choice) {
     if (wave == 0) {
       const int m = blockIdx.y / a.top_k, j = blockIdx.y % a.top_k;
+      const MoeKeys keys(a.logits + (int64_t)m * a.E, a.E, lane);
       uint32_t key = 0xffffffffu;
-      for (int i = 0; i <= j; ++i) key = moe_next(a.logits + (int64_t)m * a.E, a.E, key, lane);
+      for (int i = 0; i <= j; ++i) key = keys.next(key);
       if (lane == 0) first_of = moe_chosen(key) ? 0xffff - (int)(key & 0xffff) : -1;
     }
     __syncthreads();
@@ -232,21 +268,30 @@ __global__ __launch_bounds__(64 * kMoeWaves1) void moe_mx4_hidden_kernel(MoeArgs
     if (e < 0) return;
   }
 
-  // ---- the tokens that chose it: 8 threads to a token count the logits before
+  // ---- the tokens that chose it: a few threads to a token count the logits before
   // the expert's own --------------------------------------------------------------
   {
-    const int m = threadIdx.x >> 3, part = threadIdx.x & 7;
+    constexpr int kShare = kMoeWaves1;  // 64 tokens
+    const int m = threadIdx.x / kShare, part = threadIdx.x % kShare;
     bool in = false;
     int before = 0;
     if (m < a.M) {
       const uint16_t *l = a.logits + (int64_t)m * a.E;
       const uint32_t own = moe_key(l[e], e);
-      for (int i = part; i < a.E; i += 8) before += moe_key(l[i], i) > own;
+      for (int i0 = part; i0 < a.E; i0 += 8 * kShare) {  // 8 loads at a time
+        uint16_t v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = l[min(i0 + u * kShare, a.E - 1)];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          const int i = i0 + u * kShare;
+          before += i < a.E && moe_key(v[u], i) > own;
+        }
+      }
       in = moe_chosen(own);
     }
-    before += __shfl_xor(before, 1);
-    before += __shfl_xor(before, 2);
-    before += __shfl_xor(before, 4);
+#pragma unroll
+    for (int off = 1; off < kShare; off <<= 1) before += __shfl_xor(before, off);
     if (part == 0) rank_of[m] = in && before < a.top_k ? before : -1;
   }
   __syncthreads();
@@ -262,73 +307,46 @@ __global__ __launch_bounds__(64 * kMoeWaves1) void moe_mx4_hidden_kernel(MoeArgs
   if (by_choice && __builtin_ctzll(all) != (int)blockIdx.y / a.top_k) return;
   const int count = __builtin_amdgcn_readfirstlane(__popcll(all));
 
+  const int part = wave % parts;
+  const int f = (blockIdx.x - 1) * (kMoeWaves1 / parts) + wave / parts;
+  if (parts == 1 && f >= a.F / 32) return;  // (otherwise the workgroup meets at barriers)
   if (MB == 1 || count <= 16) {
-    moe_hidden<GLU, 1>(a, red, e, f, 0, count, list, rank_of);
+    moe_hidden<GLU, 1>(a, red, part, parts, e, f, 0, count, list, rank_of);
   } else {
-    moe_hidden<GLU, MB>(a, red, e, f, 0, count, list, rank_of);
-    if (count > 32) {
-      __syncthreads();  // the sums of the first 32 are read
-      moe_hidden<GLU, MB>(a, red, e, f, 32, count, list, rank_of);
-    }
+    for (int c0 = 0; c0 < count; c0 += 32)
+      moe_hidden<GLU, MB>(a, red, part, parts, e, f, c0, count, list, rank_of);
   }
 }
 
-// One expert's K tiles t0 .. t1-1 for this wave: p_j times the product onto the
-// wave's sums.
+// MB column blocks of 16 tokens to a step (an expert's further tokens are steps
+// of their own, which read its weights again).
 template <int MB>
-__device__ __forceinline__ void moe_expert(const MoeArgs &a, const Mx4Rows<1> &w,
-                                           const Mx4Cols<1> &cols, const uint16_t *slots, int c0,
-                                           int count, int t0, int t1, const float *weight,
-                                           float *sums, int lane) {
-  Mx4Cols<MB> x;
-  x.codes = cols.codes;
-  x.scales = cols.scales;
-  x.scale_step = cols.scale_step;
-  x.blocks = cols.blocks;
-#pragma unroll
-  for (int j = 0; j < MB; ++j) {
-    const int c = c0 + 16 * j + (lane & 15);
-    x.aim(j, c < count ? slots[c] : -1, a.F, lane);
-  }
-  v4f acc[1][MB];
-#pragma unroll
-  for (int j = 0; j < MB; ++j) acc[0][j] = v4f{0.f, 0.f, 0.f, 0.f};
-  mx4_stream<1, MB, MB == 1 ? 3 : 1>(acc, w, x, t0, t1, 1, lane);
-#pragma unroll
-  for (int j = 0; j < MB; ++j) {
-    const int c = c0 + 16 * j + (lane & 15);
-    if (c < count) {
-      const int slot = slots[c];
-      v4f *s = reinterpret_cast<v4f *>(sums + (slot / a.top_k) * 16 + 4 * (lane >> 4));
-      *s += weight[slot] * acc[0][j];
-    }
-  }
-}
-
 __global__ __launch_bounds__(64 * kMoeWaves2) void moe_mx4_out_kernel(MoeArgs a) {
-  // LDS: the waves' sums [waves][M][16], the slots' weights and experts, each
-  // expert's tokens as a mask and its slots in token order, the chosen experts
+  // LDS: the waves' sums and the biases' [waves + 1][M][16], the slots' weights and experts, each
+  // expert's tokens as a mask and its slots in token order, the groups of up to
+  // 16 MB tokens of the chosen experts (expert and first column)
   extern __shared__ v4f lds[];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int nslots = a.M * a.top_k;
   float *sums = reinterpret_cast<float *>(lds);
-  unsigned long long *mask = reinterpret_cast<unsigned long long *>(sums + kMoeWaves2 * a.M * 16);
+  unsigned long long *mask = reinterpret_cast<unsigned long long *>(sums + (kMoeWaves2 + 1) * a.M * 16);
   float *weight = reinterpret_cast<float *>(mask + a.E);
   int *expert = reinterpret_cast<int *>(weight + nslots);
-  uint16_t *slots = reinterpret_cast<uint16_t *>(expert + nslots);  // [E][M]
-  uint16_t *chosen = slots + a.E * a.M;                             // [E]
-  __shared__ int nchosen;
+  int *groups = expert + nslots;                                   // [<= E + nslots / 16]
+  uint16_t *slots = reinterpret_cast<uint16_t *>(groups + a.E + nslots / 16);  // [E][M]
+  __shared__ int ngroups;
 
-  for (int i = threadIdx.x; i < kMoeWaves2 * a.M * 16; i += blockDim.x) sums[i] = 0.f;
+  for (int i = threadIdx.x; i < kMoeWaves2 * a.M * 4; i += blockDim.x)
+    lds[i] = v4f{0.f, 0.f, 0.f, 0.f};
   for (int i = threadIdx.x; i < a.E; i += blockDim.x) mask[i] = 0;
-  for (int i = threadIdx.x; i < nslots; i += blockDim.x) {
-    weight[i] = a.ws.weight[i];
-    expert[i] = a.ws.expert[i];
-  }
   __syncthreads();
-  for (int i = threadIdx.x; i < nslots; i += blockDim.x)
-    if (expert[i] >= 0) atomicOr(&mask[expert[i]], 1ull << (i / a.top_k));
+  for (int i = threadIdx.x; i < nslots; i += blockDim.x) {
+    const int e = a.ws.expert[i];
+    expert[i] = e;
+    weight[i] = a.ws.weight[i];
+    if (e >= 0) atomicOr(&mask[e], 1ull << (i / a.top_k));
+  }
   __syncthreads();
   for (int i = threadIdx.x; i < nslots; i += blockDim.x) {
     const int e = expert[i];
@@ -338,50 +356,128 @@ __global__ __launch_bounds__(64 * kMoeWaves2) void moe_mx4_out_kernel(MoeArgs a)
   if (wave == 0) {
     int n = 0;
     for (int e0 = 0; e0 < a.E; e0 += 64) {
-      const bool in = e0 + lane < a.E && mask[e0 + lane] != 0;
-      const unsigned long long all = __ballot(in);
-      if (in) chosen[n + __popcll(all & ((1ull << lane) - 1))] = (uint16_t)(e0 + lane);
-      n += __popcll(all);
+      const int mine = e0 + lane < a.E ? (__popcll(mask[e0 + lane]) + 16 * MB - 1) / (16 * MB) : 0;
+      int sum = mine;  // inclusive prefix sum over the wave
+#pragma unroll
+      for (int off = 1; off < 64; off <<= 1) {
+        const int other = __shfl_up(sum, off);
+        if (lane >= off) sum += other;
+      }
+      for (int g = 0; g < mine; ++g)
+        groups[n + sum - mine + g] = (e0 + lane) << 8 | g * 16 * MB;
+      n += __shfl(sum, 63);
     }
-    if (lane == 0) nchosen = n;
+    if (lane == 0) ngroups = n;
   }
   __syncthreads();
 
-  // ---- this wave's share of the chosen experts' K tiles -----------------------------
+  // ---- this wave's share of the groups' K tiles, as one row of steps ------------------
   const int tiles = (a.F + kMx4Tile - 1) / kMx4Tile;
-  const int total = __builtin_amdgcn_readfirstlane(nchosen) * tiles;
+  const int total = __builtin_amdgcn_readfirstlane(ngroups) * tiles;
   const int i0 = (int)((int64_t)total * wave / kMoeWaves2);
   const int i1 = (int)((int64_t)total * (wave + 1) / kMoeWaves2);
   const int64_t blocks = (int64_t)a.E * a.H / 32;
-  Mx4Cols<1> cols;
-  cols.open(a.ws.codes, a.ws.scales, nslots, a.F);
-  for (int i = i0; i < i1;) {
-    const int n = i / tiles, t0 = i - n * tiles, t1 = min(tiles, t0 + i1 - i);
-    const int e = __builtin_amdgcn_readfirstlane((int)chosen[n]);
-    const int count = __builtin_amdgcn_readfirstlane(__popcll(mask[e]));
-    Mx4Rows<1> w;
-    w.aim(a.W2, blocks, tiles, (int64_t)e * a.H / 16 + blockIdx.x, lane);
-    float *own = sums + wave * a.M * 16;
-    if (count <= 16)
-      moe_expert<1>(a, w, cols, slots + e * a.M, 0, count, t0, t1, weight, own, lane);
-    else
-      for (int c = 0; c < count; c += 32)
-        moe_expert<2>(a, w, cols, slots + e * a.M, c, count, t0, t1, weight, own, lane);
-    i += t1 - t0;
-  }
-  __syncthreads();
+  float *own = sums + wave * a.M * 16;
+  // Loads run kDepth steps ahead, over the groups' borders.
+  struct Frag {
+    v4i a[2], b[MB][2];
+    uint32_t ea, eb[MB];
+  };
+  const int64_t per_expert = (a.M + 15) / 16;
+  Mx4Rows<1> w;
+  // (columns that no token takes are not loaded)
+  const int64_t code_bytes = (int64_t)a.E * per_expert * tiles * 2048;
+  const __amdgpu_buffer_rsrc_t rc = make_rsrc(a.ws.codes, (uint32_t)code_bytes);
+  const __amdgpu_buffer_rsrc_t rs = make_rsrc(a.ws.scales, (uint32_t)(code_bytes / 8));
+  uint32_t xc[MB], xe[MB];  // this lane's bytes of K tile 0
+  int aimed = -1;
+  auto load = [&](Frag &f, int i) {
+    const int g = i / tiles, t = i - g * tiles;
+    if (g != aimed) {
+      aimed = g;
+      const int id = __builtin_amdgcn_readfirstlane(groups[g]);
+      const int e = id >> 8, c0 = id & 255, count = __popcll(mask[e]);
+      w.aim(a.W2, blocks, tiles, (int64_t)e * a.H / 16 + blockIdx.x, lane);
+#pragma unroll
+      for (int j = 0; j < MB; ++j) {
+        const uint32_t group = (uint32_t)(e * per_expert + c0 / 16 + j);
+        const bool in = c0 + 16 * j + (lane & 15) < count;
+        xc[j] = in ? group * tiles * 2048 + lane * 16 : kOobOffset;
+        xe[j] = in ? group * tiles * 256 + lane * 4 : kOobOffset;
+      }
+    }
+    const v4i *p = reinterpret_cast<const v4i *>(w.codes[0] + (int64_t)t * kMx4PackedTile);
+    f.a[0] = __builtin_nontemporal_load(p);
+    f.a[1] = __builtin_nontemporal_load(p + 128);
+    f.ea = *reinterpret_cast<const uint32_t *>(w.scales[0] + t * w.scale_step);
+#pragma unroll
+    for (int j = 0; j < MB; ++j) {  // (kOobOffset + t KiB stays out of range)
+      f.b[j][0] = __builtin_bit_cast(
+          v4i, __builtin_amdgcn_raw_buffer_load_b128(rc, xc[j] + t * 2048, 0, 0));
+      f.b[j][1] = __builtin_bit_cast(
+          v4i, __builtin_amdgcn_raw_buffer_load_b128(rc, xc[j] + t * 2048 + 1024, 0, 0));
+      f.eb[j] = __builtin_amdgcn_raw_buffer_load_b32(rs, xe[j] + t * 256, 0, 0);
+    }
+  };
+  v4f acc[MB];
+#pragma unroll
+  for (int j = 0; j < MB; ++j) acc[j] = v4f{0.f, 0.f, 0.f, 0.f};
+  // p_j times the group's product onto the wave's sums
+  auto flush = [&](int g) {
+    const int id = __builtin_amdgcn_readfirstlane(groups[g]);
+    const int e = id >> 8, c0 = id & 255, count = __popcll(mask[e]);
+#pragma unroll
+    for (int j = 0; j < MB; ++j) {
+      const int c = c0 + 16 * j + (lane & 15);
+      if (c < count) {
+        const int slot = slots[e * a.M + c];
+        v4f *s = reinterpret_cast<v4f *>(own + (slot / a.top_k) * 16 + 4 * (lane >> 4));
+        *s += weight[slot] * acc[j];
+      }
+      acc[j] = v4f{0.f, 0.f, 0.f, 0.f};
+    }
+  };
+  constexpr int kDepth = MB == 1 ? 4 : 2;
+  Frag f[kDepth];
+#pragma unroll
+  for (int d = 0; d < kDepth; ++d)
+    if (i0 + d < i1) load(f[d], i0 + d);
+  // sum_j p_j b2_e meanwhile
   for (int i = threadIdx.x; i < a.M * 4; i += blockDim.x) {
     const int m = i >> 2;
-    const int64_t n = (int64_t)blockIdx.x * 16 + 4 * (i & 3);
     v4f s = v4f{0.f, 0.f, 0.f, 0.f};
-    for (int v = 0; v < kMoeWaves2; ++v) s += lds[(v * a.M + m) * 4 + (i & 3)];
     if (a.b2)
       for (int j = 0; j < a.top_k; ++j) {
         const int e = expert[m * a.top_k + j];
         if (e >= 0)
           s += weight[m * a.top_k + j] *
-               *reinterpret_cast<const v4f *>(a.b2 + (int64_t)e * a.H + n);
+               *reinterpret_cast<const v4f *>(a.b2 + (int64_t)e * a.H + blockIdx.x * 16 +
+                                              4 * (i & 3));
       }
+    lds[(kMoeWaves2 * a.M + m) * 4 + (i & 3)] = s;
+  }
+  for (int i = i0; i < i1; i += kDepth) {
+#pragma unroll
+    for (int d = 0; d < kDepth; ++d) {
+      if (i + d < i1) {
+        const uint32_t ea = f[d].ea >> (8 * (lane >> 5));
+#pragma unroll
+        for (int j = 0; j < MB; ++j)
+          acc[j] = mfma_mx4_16<0>(f[d].a[0], f[d].b[j][0], acc[j], ea, f[d].eb[j]);
+#pragma unroll
+        for (int j = 0; j < MB; ++j)
+          acc[j] = mfma_mx4_16<2>(f[d].a[1], f[d].b[j][1], acc[j], ea, f[d].eb[j]);
+        if (i + d + kDepth < i1) load(f[d], i + d + kDepth);
+        if ((i + d + 1) % tiles == 0 || i + d + 1 == i1) flush((i + d) / tiles);
+      }
+    }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < a.M * 4; i += blockDim.x) {
+    const int m = i >> 2;
+    const int64_t n = (int64_t)blockIdx.x * 16 + 4 * (i & 3);
+    v4f s = lds[m * 4 + (i & 3)];
+    for (int v = 1; v <= kMoeWaves2; ++v) s += lds[(v * a.M + m) * 4 + (i & 3)];
     uint2 h;
     h.x = (uint32_t)float_to_half_bits(s[0]) | ((uint32_t)float_to_half_bits(s[1]) << 16);
     h.y = (uint32_t)float_to_half_bits(s[2]) | ((uint32_t)float_to_half_bits(s[3]) << 16);
@@ -390,8 +486,8 @@ __global__ __launch_bounds__(64 * kMoeWaves2) void moe_mx4_out_kernel(MoeArgs a)
 }
 
 size_t moe_out_lds(int M, int E, int top_k) {
-  return (size_t)kMoeWaves2 * M * 64 + (size_t)E * 8 + (size_t)M * top_k * 8 + (size_t)E * M * 2 +
-         (size_t)E * 2;
+  return (size_t)(kMoeWaves2 + 1) * M * 64 + (size_t)E * 8 + (size_t)M * top_k * 8 +
+         (size_t)(E + M * top_k / 16) * 4 + (size_t)E * M * 2;
 }
 
 size_t align16(size_t n) { return (n + 15) & ~size_t(15); }
@@ -400,10 +496,14 @@ size_t align16(size_t n) { return (n + 15) & ~size_t(15); }
 
 using namespace detail;
 
-size_t moe_mx4_workspace_bytes(int64_t M, int64_t F, int64_t top_k) {
+static size_t moe_code_bytes(int64_t M, int64_t F, int64_t E) {
+  return (size_t)(E * ((M + 15) / 16)) * mx4_tiles(F) * 2048;
+}
+
+size_t moe_mx4_workspace_bytes(int64_t M, int64_t F, int64_t E, int64_t top_k) {
   const size_t slots = (size_t)M * top_k;
-  return align16(slots * (F / 2)) + align16((size_t)mx4_tiles(F) * slots * 8) +
-         align16(slots * sizeof(int)) + align16(slots * sizeof(float));
+  return moe_code_bytes(M, F, E) + moe_code_bytes(M, F, E) / 8 + align16(slots * sizeof(int)) +
+         align16(slots * sizeof(float));
 }
 
 hipError_t launch_moe_mx4(const uint8_t *Xc, const uint8_t *Xe, const uint16_t *logits,
@@ -414,25 +514,41 @@ hipError_t launch_moe_mx4(const uint8_t *Xc, const uint8_t *Xe, const uint16_t *
   uint8_t *p = static_cast<uint8_t *>(workspace);
   MoeArgs a{Xc, Xe, logits, W1, W2, b1, b2, (int)M, (int)H, (int)F, (int)E, (int)top_k, Y, {}};
   a.ws.codes = p;
-  p += align16(slots * (F / 2));
+  p += moe_code_bytes(M, F, E);
   a.ws.scales = p;
-  p += align16((size_t)mx4_tiles(F) * slots * 8);
+  p += moe_code_bytes(M, F, E) / 8;
   a.ws.expert = reinterpret_cast<int *>(p);
   p += align16(slots * sizeof(int));
   a.ws.weight = reinterpret_cast<float *>(p);
-  const dim3 grid((unsigned)(F / 32 + 1), (unsigned)(E < (int64_t)slots ? E : (int64_t)slots));
+  // Waves to a block of hidden channels: enough that a CU has some 70 KB of weights
+  // in flight (4 waves of gate and value rows, 8 of one kind), as far as H has K
+  // tiles for them.  One token through two experts of 16384, H = 4096: 18.6 us with
+  // one wave, 15.7 with two; 64 tokens through 32 gated ones of 1408, H = 2048: 22.2
+  // with one, 24.2 with two (a second round of workgroups).
+  const int64_t rows = E < (int64_t)slots ? E : (int64_t)slots, hidden = F / 32;
+  const int64_t enough = (glu ? 4 : 8) * (int64_t)device_cus();
+  int parts = 1;
+  while (parts < kMoeWaves1 && rows * hidden * parts < enough && 2 * parts <= mx4_tiles(H))
+    parts *= 2;
+  const int64_t per_wg = kMoeWaves1 / parts;
+  const dim3 grid((unsigned)((hidden + per_wg - 1) / per_wg + 1), (unsigned)rows);
   const int threads = 64 * kMoeWaves1;
+  const int units = (glu ? 4 : 2) * (M <= 16 ? 1 : 2);
+  const size_t sums = parts > 1 ? (size_t)kMoeWaves1 * units * 1024 : 0;
   if (M <= 16) {
-    if (glu) moe_mx4_hidden_kernel<true, 1><<<grid, threads, 0, st>>>(a);
-    else moe_mx4_hidden_kernel<false, 1><<<grid, threads, 0, st>>>(a);
+    if (glu) moe_mx4_hidden_kernel<true, 1><<<grid, threads, sums, st>>>(a, parts);
+    else moe_mx4_hidden_kernel<false, 1><<<grid, threads, sums, st>>>(a, parts);
   } else {
-    if (glu) moe_mx4_hidden_kernel<true, 2><<<grid, threads, 0, st>>>(a);
-    else moe_mx4_hidden_kernel<false, 2><<<grid, threads, 0, st>>>(a);
+    if (glu) moe_mx4_hidden_kernel<true, 2><<<grid, threads, sums, st>>>(a, parts);
+    else moe_mx4_hidden_kernel<false, 2><<<grid, threads, sums, st>>>(a, parts);
   }
   hipError_t err = hipGetLastError();
   if (err != hipSuccess) return err;
-  moe_mx4_out_kernel<<<(unsigned)(H / 16), 64 * kMoeWaves2,
-                       moe_out_lds((int)M, (int)E, (int)top_k), st>>>(a);
+  const size_t lds = moe_out_lds((int)M, (int)E, (int)top_k);
+  // 32 tokens of an expert to a step where it has more than 12 on average: with
+  // fewer, half of the token loads and products would be of nobody
+  if (M <= 16 || (int64_t)slots <= 12 * E) moe_mx4_out_kernel<1><<<(unsigned)(H / 16), 64 * kMoeWaves2, lds, st>>>(a);
+  else moe_mx4_out_kernel<2><<<(unsigned)(H / 16), 64 * kMoeWaves2, lds, st>>>(a);
   return hipGetLastError();
 }
 

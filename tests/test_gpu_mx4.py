@@ -179,7 +179,13 @@ LINEARS = [(1, 1, 32), (1, 33, 64), (2, 16, 96), (16, 768, 768), (17, 100, 288),
            (32, 65, 2080), (33, 200, 1056), (64, 513, 4128), (8, 64, 36864),
            (65, 1, 32), (65, 70, 96), (100, 130, 288), (131, 615, 4128), (128, 128, 256),
            (129, 257, 512), (300, 1000, 1056), (513, 2050, 544), (1000, 3000, 800),
-           (2048, 4096, 2048)]
+           (2048, 4096, 2048),
+           # 32 rows to a workgroup: more than 16 x 256 channels
+           (1, 4128, 4352), (16, 4100, 5120), (17, 4100, 288), (32, 4097, 2304), (40, 4100, 544),
+           (64, 4099, 2080), (40, 8300, 96), (64, 8193, 800),
+           # each tile's own sizes, ragged: 256 x 256, 192 x 256, 256 x 128, 128 x 128, 64 x 128
+           (4000, 8000, 320), (2000, 12250, 96), (1100, 7700, 160), (500, 5100, 1056),
+           (128, 9000, 96)]
 
 
 @pytest.mark.parametrize("M,N,K", LINEARS)

@@ -27,22 +27,17 @@ struct Mx4Cfg {
   static constexpr int kTN = BN / WN, kTM = BM / WM;
   static constexpr int kFN = kTN / 32, kFM = kTM / 32;
   static constexpr int kABytes = BN * 128, kBBytes = BM * 128;
-  // scales in pieces of 1 KiB (128 rows)
-  static constexpr int kPiecesA = (BN + 127) / 128, kPiecesB = (BM + 127) / 128;
-  static constexpr int kPieces = kPiecesA + kPiecesB;
-  static constexpr int kStage = kABytes + kBBytes;
-  // S stages of codes, then S + 1 of scales
-  static constexpr int kScales = S * kStage, kScaleStage = kPieces * 1024;
-  static constexpr int kTurns = kWaves / kPieces;  // K tiles between a wave's pieces
+  static constexpr int kScaleA = kABytes + kBBytes, kScaleB = kScaleA + BN * 8;
+  static constexpr int kStage = kScaleB + BM * 8;
   static constexpr int kLoadsA = BN / 8 / kWaves, kLoadsB = BM / 8 / kWaves;  // 1 KiB each
-  static constexpr int kLoads = kLoadsA + kLoadsB;
+  static constexpr int kPieces = (BN + BM) / 32;  // of scales, 256 bytes (32 rows) each
+  static constexpr int kLoadsE = (kPieces + kWaves - 1) / kWaves;
+  static constexpr int kLoads = kLoadsA + kLoadsB + kLoadsE;
   static constexpr int kMfma = kFN * kFM, kReads = kFN + kFM;
   static constexpr int kOut = BN * BM * 2;  // the fp16 output tile, staged after the loop
-  static constexpr int kRing = kScales + (S + 1) * kScaleStage;
-  static constexpr int kSmem = kRing > kOut ? kRing : kOut;
+  static constexpr int kSmem = S * kStage > kOut ? S * kStage : kOut;
   static_assert(kLoadsA * 8 * kWaves == BN && kLoadsB * 8 * kWaves == BM, "whole code loads");
   static_assert(kTN % 32 == 0 && kTM % 32 == 0, "32x32 blocks");
-  static_assert(kTurns >= 1, "a wave copies at most one scale piece of a K tile");
   static_assert(S >= 2 && (S - 2) * kLoads <= 63, "vmcnt range");
   static_assert(kSmem <= 160 * 1024, "LDS");
 };
@@ -101,36 +96,31 @@ __device__ __forceinline__ void mx4_gemm_body(
       __builtin_amdgcn_raw_ptr_buffer_load_lds(
           rsrc_a, (lds_void *)(st + (wave * C::kLoadsA + ja) * 1024), 16,
           kt < KT ? off_a[ja] + (uint32_t)kt * kMx4PackedTile : kOobOffset, 0, 0, 0);
-    } else {
-      const int jb = j >= C::kLoadsA && j < C::kLoads ? j - C::kLoadsA : 0;
+    } else if (j < C::kLoadsA + C::kLoadsB) {
+      const int jb = j >= C::kLoadsA && j < C::kLoadsA + C::kLoadsB ? j - C::kLoadsA : 0;
       const int k0 = kt * kMx4TileBytes;
       __builtin_amdgcn_raw_ptr_buffer_load_lds(
           rsrc_b, (lds_void *)(st + C::kABytes + (wave * C::kLoadsB + jb) * 1024), 16,
           k0 + ck_b[jb] < KB ? off_b[jb] + (uint32_t)k0 : kOobOffset, 0, 0, 0);
-    }
-  };
-  // Scales: a 1 KiB piece (128 rows) is copied by one wave, each wave with a
-  // piece of its own every kTurns K tiles.  (As 256-byte loads, two per wave and
-  // tile beside its eight of codes, they cost 8 % of the kernel.)  Two rows to a
-  // lane; the last row of an odd count by itself, since 16 bytes there could
-  // reach past the end of the scales.  They have a stage more than the codes, so
-  // that a tile's are issued away from the barrier that frees its codes' stage.
-  const int piece = wave % C::kPieces, turn = wave / C::kPieces;
-  const bool of_w = piece < C::kPiecesA;
-  const int prow = (of_w ? piece : piece - C::kPiecesA) * 128;  // its first row
-  const int prows = (of_w ? blocks_a * 32 : rows_b) - prow;     // rows from there
-  const uint8_t *pbase = (of_w ? scales_w : scales_x) + (int64_t)prow * 8;
-  const int64_t pstep = of_w ? (int64_t)NB * 256 : (int64_t)M * 8;
-  auto issue_scales = [&](int kt, int slot) {
-    if (kt % C::kTurns != turn || kt >= KT || prows <= 0) return;
-    const __amdgpu_buffer_rsrc_t r = make_rsrc(pbase + kt * pstep, (uint32_t)prows * 8);
-    uint8_t *dst = smem + C::kScales + slot * C::kScaleStage + piece * 1024;
-    if (2 * lane + 1 < prows)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void *)dst, 16, lane * 16, 0, 0, 0);
-    if ((prows & 1) && prows < 128) {
-      if (lane < 2)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void *)(dst + (prows - 1) * 8), 4,
-                                                 (prows - 1) * 8 + lane * 4, 0, 0, 0);
+    } else {
+      // Scales: 256-byte piece q, of 32 weight rows or 32 token rows (waves left
+      // over load the last one once more).  By 4 bytes a lane, since an odd number
+      // of token rows leaves no wider alignment.  Fewer waves copying a KiB each
+      // saved loads and cost more (OPT-66B fc2, 8192 tokens: 1229 us, and 1260 so).
+      const int q = min(wave * C::kLoadsE + (j - C::kLoadsA - C::kLoadsB), C::kPieces - 1);
+      const int t = min(kt, KT - 1);
+      if (q < BN / 32) {
+        const __amdgpu_buffer_rsrc_t r =
+            make_rsrc(scales_w + (int64_t)t * NB * 256, (uint32_t)blocks_a * 256);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void *)(st + C::kScaleA + q * 256), 4,
+                                                 q * 256 + lane * 4, 0, 0, 0);
+      } else {
+        const int qb = q - BN / 32;
+        const __amdgpu_buffer_rsrc_t r =
+            make_rsrc(scales_x + (int64_t)t * M * 8, (uint32_t)rows_b * 8);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void *)(st + C::kScaleB + qb * 256), 4,
+                                                 qb * 256 + lane * 4, 0, 0, 0);
+      }
     }
   };
 
@@ -141,8 +131,8 @@ __device__ __forceinline__ void mx4_gemm_body(
   for (int s = 0; s < 4; ++s) off_f[s] = fr * 128 + 16 * ((4 * fh + s) ^ swz_mx4(fr));
   const int a_base = wn * C::kFN * kMx4PackedTile + lane * 16;
   const int b_base = C::kABytes + wm * C::kTM * 128;
-  const int ea_base = wn * C::kTN * 8 + lane * 4;
-  const int eb_base = C::kPiecesA * 1024 + wm * C::kTM * 8 + fr * 8 + fh * 4;
+  const int ea_base = C::kScaleA + wn * C::kTN * 8 + lane * 4;
+  const int eb_base = C::kScaleB + wm * C::kTM * 8 + fr * 8 + fh * 4;
 
   v4i fa[2][C::kFN], fb[2][C::kFM];
   int ea[C::kFN], eb[C::kFM], na[C::kFN], nb[C::kFM];
@@ -160,9 +150,9 @@ __device__ __forceinline__ void mx4_gemm_body(
     return n < C::kLoads ? n : C::kLoads;
   };
   // One K step: its MFMAs, the fragment reads of the next step (step rstep of
-  // the tile in stage st; with it that tile's scales from se where rstep is 0) and
+  // the tile in stage st; with it the next tile's scales where rstep is 0) and
   // tile lt's loads from slot u0 on, in that interleaved order.
-  auto kstep = [&](auto step, const uint8_t *st, const uint8_t *se, int lt, int u0) {
+  auto kstep = [&](auto step, const uint8_t *st, int lt, int u0) {
     constexpr int kS = decltype(step)::value;
     constexpr int cb = kS & 1, nxt = cb ^ 1, rstep = (kS + 1) & 3;
     constexpr int kN = C::kMfma > C::kReads ? C::kMfma : C::kReads;
@@ -170,11 +160,11 @@ __device__ __forceinline__ void mx4_gemm_body(
     for (int i = 0; i < kN; ++i) {
       if (i < C::kFN) {
         fa[nxt][i] = *reinterpret_cast<const v4i *>(st + a_base + i * kMx4PackedTile + rstep * 1024);
-        if constexpr (rstep == 0) na[i] = *reinterpret_cast<const int *>(se + ea_base + i * 256);
+        if constexpr (rstep == 0) na[i] = *reinterpret_cast<const int *>(st + ea_base + i * 256);
       } else if (i < C::kReads) {
         const int g = i - C::kFN;
         fb[nxt][g] = *reinterpret_cast<const v4i *>(st + b_base + g * 32 * 128 + off_f[rstep]);
-        if constexpr (rstep == 0) nb[g] = *reinterpret_cast<const int *>(se + eb_base + g * 256);
+        if constexpr (rstep == 0) nb[g] = *reinterpret_cast<const int *>(st + eb_base + g * 256);
       }
       if (i < C::kMfma) {
         // one operand changes from MFMA to MFMA
@@ -200,38 +190,30 @@ __device__ __forceinline__ void mx4_gemm_body(
   };
 
   // ---- main loop ------------------------------------------------------------
-  // A wave waits by its loads of codes alone; where some of the younger ones are
-  // of scales it waits for a few of those too.
 #pragma unroll
-  for (int t = 0; t < S - 1; ++t) {
-    issue_scales(t, t);
+  for (int t = 0; t < S - 1; ++t)
 #pragma unroll
     for (int j = 0; j < C::kLoads; ++j) issue_one(t, j);
-  }
   wait_vmcnt<(S - 2) * C::kLoads>();  // tile 0 has landed
   lds_barrier();
-  issue_scales(S - 1, S - 1);
 #pragma unroll
   for (int j = 0; j < C::kLoads; ++j)
     if (j < upto(C::kMfma)) issue_one(S - 1, j);
 #pragma unroll
   for (int f = 0; f < C::kFN; ++f) {
     fa[0][f] = *reinterpret_cast<const v4i *>(smem + a_base + f * kMx4PackedTile);
-    ea[f] = *reinterpret_cast<const int *>(smem + C::kScales + ea_base + f * 256);
+    ea[f] = *reinterpret_cast<const int *>(smem + ea_base + f * 256);
   }
 #pragma unroll
   for (int g = 0; g < C::kFM; ++g) {
     fb[0][g] = *reinterpret_cast<const v4i *>(smem + b_base + g * 32 * 128 + off_f[0]);
-    eb[g] = *reinterpret_cast<const int *>(smem + C::kScales + eb_base + g * 256);
+    eb[g] = *reinterpret_cast<const int *>(smem + eb_base + g * 256);
   }
-  int e_slot = 0;  // of tile kt's scales
   for (int kt = 0; kt < KT; ++kt) {
     const uint8_t *st = smem + (kt % S) * C::kStage;
-    kstep(IntC<0>{}, st, nullptr, kt + S - 1, C::kMfma);
-    issue_scales(kt + S, e_slot == 0 ? S : e_slot - 1);  // the slot of tile kt - 1
-    e_slot = e_slot == S ? 0 : e_slot + 1;
-    kstep(IntC<1>{}, st, nullptr, kt + S - 1, 2 * C::kMfma);
-    kstep(IntC<2>{}, st, nullptr, kt + S - 1, 3 * C::kMfma);
+    kstep(IntC<0>{}, st, kt + S - 1, C::kMfma);
+    kstep(IntC<1>{}, st, kt + S - 1, 2 * C::kMfma);
+    kstep(IntC<2>{}, st, kt + S - 1, 3 * C::kMfma);
     // This wave's reads of tile kt are done once lgkmcnt drains, tile kt+1 has
     // landed once at most S-2 younger tiles are in flight; after the barrier
     // tile kt's stage takes tile kt+S.  At kt = KT-1 the reads of "tile KT" are
@@ -240,8 +222,7 @@ __device__ __forceinline__ void mx4_gemm_body(
     __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
     wait_vmcnt<(S - 2) * C::kLoads>();
     lds_barrier();
-    kstep(IntC<3>{}, smem + ((kt + 1) % S) * C::kStage,
-          smem + C::kScales + e_slot * C::kScaleStage, kt + S, 0);
+    kstep(IntC<3>{}, smem + ((kt + 1) % S) * C::kStage, kt + S, 0);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int f = 0; f < C::kFN; ++f) ea[f] = na[f];
@@ -273,26 +254,25 @@ hipError_t launch_mx4_tile(const uint8_t *Xc, const uint8_t *Xe, const uint8_t *
   return hipGetLastError();
 }
 
-// The tiles and the launch's estimated time in microseconds: passes over the CUs
-// (`per_cu` workgroups on each), each of `pass` and `per_k` per K tile, plus
-// `share` per K tile for the workgroups' mean number per CU (what they take from
-// each other), plus `once`.  Fitted to 319 random launches on MI355X (33 .. 8192
-// tokens, 512 .. 28672 channels, K = 512 .. 36864) whose weights come from HBM:
-// the tile it picks is 1.2 % over the fastest of these (57 % at worst, on a 4 us
-// launch), 1.5 % over the fastest of ten shapes tried.
+// The tiles and the launch's estimated time in microseconds: passes over the
+// CUs, each of `pass` and `per_k` per K tile, plus `share` per K tile for the
+// workgroups' mean number per CU (what they take from each other), plus `once`.
+// Fitted to 360 random launches on MI355X (33 .. 8192 tokens, 512 .. 28672
+// channels, K = 512 .. 36864) whose weights come from HBM: the tile it picks is
+// 0.6 % over the fastest of these (52 % at worst, on a 4 us launch), 1.3 % over
+// the fastest of nine shapes tried.
 struct Mx4Tile {
-  int bn, bm, threads, per_cu;
+  int bn, bm, threads;
   double once, pass, per_k, share;
-  const char *name;
 };
 constexpr Mx4Tile kTiles[] = {
-    {256, 256, 512, 1, 0.4, 7.03, 1.200, 0.810, "prefill 256x256"},
-    {192, 256, 512, 1, 3.0, 6.11, 1.025, 0.594, "prefill 192x256"},
-    {256, 128, 512, 1, 0.8, 4.58, 0.889, 0.505, "prefill 256x128"},
-    {128, 128, 512, 1, -2.8, 7.43, 0.413, 0.229, "prefill 128x128"},
-    {64, 128, 256, 1, 0.5, 4.35, 0.321, 0.126, "prefill 64x128"},
-    {128, 64, 512, 1, -0.8, 4.75, 0.376, 0.137, "prefill 128x64"},
-    {64, 64, 256, 2, -0.4, 4.17, 0.273, 0.140, "prefill 64x64"},
+    {256, 256, 512, -0.485, 9.442, 1.175, 0.631},
+    {192, 256, 512, -0.814, 10.617, 1.014, 0.377},
+    {256, 128, 512, -0.314, 5.946, 0.929, 0.334},
+    {128, 128, 512, 1.111, 4.042, 0.422, 0.205},
+    {64, 128, 256, 1.034, 3.509, 0.343, 0.105},
+    {128, 64, 512, 1.126, 2.890, 0.352, 0.141},
+    {64, 64, 256, 2.539, 1.251, 0.295, -0.004},
 };
 constexpr int kTileCount = sizeof(kTiles) / sizeof(kTiles[0]);
 
@@ -313,8 +293,8 @@ int pick_tile(int64_t M, int64_t N, int64_t K) {
   for (int i = 0; i < kTileCount; ++i) {
     const Mx4Tile &t = kTiles[i];
     if (i > 0 && !fits(t, M, N)) continue;
-    const int64_t tiles = tiles_of(t, M, N), slots = cus * t.per_cu;
-    const double passes = (double)((tiles + slots - 1) / slots);
+    const int64_t tiles = tiles_of(t, M, N);
+    const double passes = (double)((tiles + cus - 1) / cus);
     const double us = t.once + passes * (t.pass + t.per_k * kt) + t.share * kt * tiles / cus;
     if (i == 0 || us < least) {
       best = i;
@@ -329,10 +309,6 @@ int pick_tile(int64_t M, int64_t N, int64_t K) {
 using namespace detail;
 
 bool mx4_gemm_fits(int64_t M, int64_t N) { return fits(kTiles[0], M, N); }
-
-const char *mx4_gemm_tile_name(int64_t M, int64_t N, int64_t K) {
-  return kTiles[pick_tile(M, N, K)].name;
-}
 
 hipError_t launch_mx4_gemm(const uint8_t *Xc, const uint8_t *Xe, const uint8_t *Wp,
                            const float *bp, int64_t M, int64_t N, int64_t K, uint16_t *Y,

@@ -88,8 +88,8 @@ __device__ __forceinline__ uint32_t row_scales(uint32_t b, int lane) {
 
 // Lane l of a wave holds eight consecutive channels from k0 = 8 (64 i + l) on,
 // zeros past K: their codes and scales to row `row` of [M x K].  All 64 lanes
-// take part.
-__device__ __forceinline__ void mx4_store8(const float (&v)[8], int64_t row, int64_t M, int64_t K,
+// take part.  The scale byte of the lane's block.
+__device__ __forceinline__ uint32_t mx4_store8(const float (&v)[8], int64_t row, int64_t M, int64_t K,
                                            int64_t k0, int lane, uint8_t *__restrict__ Xc,
                                            uint8_t *__restrict__ Xe) {
   uint32_t most = abs_bits(v[0]);
@@ -102,6 +102,7 @@ __device__ __forceinline__ void mx4_store8(const float (&v)[8], int64_t row, int
   // the end of the K tile
   if ((lane & 15) == 0 && k0 < (K + kMx4Tile - 1) / kMx4Tile * kMx4Tile)
     *reinterpret_cast<uint32_t *>(Xe + ((k0 >> 8) * M + row) * 8 + ((k0 >> 5) & 7)) = e;
+  return b;
 }
 
 }  // namespace detail
@@ -131,7 +132,6 @@ hipError_t launch_mx4_gemm(const uint8_t *Xc, const uint8_t *Xe, const uint8_t *
                            const float *bp, int64_t M, int64_t N, int64_t K, uint16_t *Y,
                            hipStream_t st);
 bool mx4_gemm_fits(int64_t M, int64_t N);
-const char *mx4_gemm_tile_name(int64_t M, int64_t N, int64_t K);
 // A mixture-of-experts layer; workspace of at least moe_mx4_workspace_bytes.
 size_t moe_mx4_workspace_bytes(int64_t M, int64_t F, int64_t E, int64_t top_k);
 hipError_t launch_moe_mx4(const uint8_t *Xc, const uint8_t *Xe, const uint16_t *logits,

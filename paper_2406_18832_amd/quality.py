@@ -2,14 +2,15 @@
 workloads: a symmetrization ablation and bit-width sweep standing in for the
 paper's Table 6 (with and without symmetrization, Sec. 4.4) and Table 10
 (W8A6, W6A6, W8A4, W4A4), plus the per-token path of Eq. (c) as the
-baseline the paper argues against (Sec. 2.2).
+baseline the paper argues against (Sec. 2.2), and the same linears on 4-bit
+floating point (MX4) with and without the channels' shift and scale.
 
 The paper measures perplexity on checkpoints and datasets that are not used
 here; this measures the error the method introduces in one linear, which is
 what those numbers follow from.  Every step runs through libot: one
 calibration pass (ot_calibrate) gives the minmax state, ot_scales_from_minmax
 derives each configuration's z and s from it, then ot_fold_weights,
-ot_quantize_act and ot_qlinear (or the per-token entry points).  The
+ot_quantize_act and ot_qlinear (or the per-token or mx4 entry points).  The
 reference is X W^T + b in float64 (torch, on the GPU).
 """
 from __future__ import annotations
@@ -29,6 +30,11 @@ CONFIGS = [
     ("W8A8 per-token", 8, 8, "token"), ("W6A6 per-token", 6, 6, "token"),
 ]
 
+# 4-bit floating point in blocks of 32: with the channels' shift and scale taken
+# out first, with the scale alone, and with neither
+MX4_CONFIGS = [("MX4", 4, 4, "mx4"), ("MX4 no-sym", 4, 4, "mx4-nosym"),
+               ("MX4 plain", 4, 4, "mx4-plain")]
+
 
 def layer_inputs(wl, li, rows, calib_rows, calib_batches, device="cuda"):
     """Device tensors of one layer: X [rows, K], W, b, and the calibration
@@ -47,6 +53,14 @@ def run_config(X, W, b, minmax, a_bits, w_bits, path):
         Xq, sX = ot.quantize_act_per_token(X, a_bits)
         Wq, sW, bp = ot.fold_weights_per_token(W, b, None, w_bits)
         return ot.qlinear_per_token(Xq, Wq, sX, sW, bp, a_bits, w_bits)
+    if path.startswith("mx4"):
+        # a block's own scale takes care of the magnitude, so any a_bits gives the
+        # same channel-to-channel proportions
+        z, s, inv_s = (None, None, None) if path == "mx4-plain" else \
+            ot.scales_from_minmax(minmax, 8, path == "mx4")
+        Wc, We, bp = ot.fold_weights_mx4(W, b, z, s)
+        return ot.qlinear_mx4(*ot.quantize_act_mx4(X, z, inv_s), ot.pack_weights_mx4(Wc, We),
+                              W.shape[0], bp, True)
     z, s, inv_s = ot.scales_from_minmax(minmax, a_bits, path == "channel")
     Wq, sW, bp = ot.fold_weights(W, b, w_bits, z, s)
     Xq = ot.quantize_act(X, a_bits, z, inv_s)
@@ -61,7 +75,7 @@ def errors(Y, ref):
 
 
 def sweep(workloads=("opt6.7b_w8a8", "opt13b_w6a6", "opt66b_w8a8"), rows=256, calib_rows=None,
-          calib_batches=None, configs=CONFIGS, device="cuda", log=None):
+          calib_batches=None, configs=CONFIGS + MX4_CONFIGS, device="cuda", log=None):
     """Errors of every configuration on every linear of the given workloads
     (calibration: the workload's own batches unless given).  Returns a list
     of dicts (workload, layer, config, a_bits, w_bits, path, rel_fro,

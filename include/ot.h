@@ -475,13 +475,16 @@ ot_status ot_pack_weights_mx4(const uint8_t *Wc, const uint8_t *We, int64_t N,
  * ot_qlinear_mx4 -- the linear on MX4 operands:
  *   Y[m,n] = fp16(fp32(sum_k x[m,k] w[n,k]) + bprime_n)
  * with the values that the codes stand for; their products are exact, the sum
- * is in fp32 (its order is fixed for given sizes and unspecified).
+ * is in fp32 (its order is fixed for given sizes, with or without a workspace,
+ * and unspecified).
  *   Xc, Xe [M x K] and Wp of ot_pack_weights_mx4 for N x K, bprime [N] fp32
- *   (device).  M >= 0 (0 is a no-op), 1 <= N < 2^26.
+ *   (device).  M >= 0 (0 is a no-op), 1 <= N < 2^26 and
+ *   ceil(M/256) ceil(N/256) < 2^23 (OT_ESHAPE).
  *   Y  [M x N] fp16 output (device).
  *   workspace  NULL, or at least ot_qlinear_mx4_workspace_size(M, N, K) bytes of
- *           scratch as for ot_qlinear.  Calls that overlap in time must not
- *           share one.
+ *           scratch as for ot_qlinear, with which few tokens on a long K are
+ *           faster (K is shared between workgroups).  Calls that overlap in time
+ *           must not share one.
  * Asynchronous on stream; no synchronization, no allocation.
  */
 ot_status ot_qlinear_mx4(const uint8_t *Xc, const uint8_t *Xe, const uint8_t *Wp,
@@ -490,6 +493,17 @@ ot_status ot_qlinear_mx4(const uint8_t *Xc, const uint8_t *Xe, const uint8_t *Wp
 /* Bytes of optional scratch that ot_qlinear_mx4 can use for these sizes on the
  * current device (0 if none, and for sizes it rejects).  No device work. */
 size_t ot_qlinear_mx4_workspace_size(int64_t M, int64_t N, int64_t K);
+
+/*
+ * ot_qlinear_mx4_plan -- which kernel configuration ot_qlinear_mx4 launches for
+ * these sizes on the current device, given a workspace or not; as
+ * ot_qlinear_plan.  Writes "none" for M == 0, "decode <R> rows" (output channels
+ * per workgroup: 16 or 32), or "tiles <R>x<T>" (output channels x tokens per
+ * workgroup: 256x256, 192x256, 256x128, 128x128, 64x128, 128x64 or 64x64), with
+ * " split-K <parts>" where K is shared between workgroups.
+ */
+ot_status ot_qlinear_mx4_plan(int64_t M, int64_t N, int64_t K, int with_workspace,
+                              char *buf, size_t len);
 
 /*
  * ot_moe_mx4 -- a whole mixture-of-experts layer for a few tokens on packed MX4

@@ -464,24 +464,38 @@ ot_status ot_pack_weights_mx4(const uint8_t *Wc, const uint8_t *We, int64_t N, i
       ot::launch_pack_weights_mx4(Wc, We, N, K, Wp, static_cast<hipStream_t>(stream)));
 }
 
+static bool mx4_linear_ok(int64_t M, int64_t N, int64_t K) {
+  return N > 0 && mx4_k_ok(K) && M <= kMaxRows && N <= kMaxMx4N && ot::mx4_gemm_fits(M, N);
+}
+
 ot_status ot_qlinear_mx4(const uint8_t *Xc, const uint8_t *Xe, const uint8_t *Wp,
                          const float *bprime, int64_t M, int64_t N, int64_t K, uint16_t *Y,
                          void *workspace, void *stream) {
   if (M < 0 || N < 0 || K < 0) return OT_EINVAL;
-  if (N == 0 || !mx4_k_ok(K) || M > kMaxRows || N > kMaxMx4N || !ot::mx4_gemm_fits(M, N))
-    return OT_ESHAPE;
+  if (!mx4_linear_ok(M, N, K)) return OT_ESHAPE;
   if (M == 0) return OT_OK;
   if (!Xc || !Xe || !Wp || !bprime || !Y) return OT_EINVAL;
   if (!aligned16(Xc) || !aligned16(Xe) || !aligned16(Wp) || !aligned16(bprime) || !aligned16(Y) ||
       !aligned16(workspace))
     return OT_EINVAL;
-  return hip_status(ot::launch_mx4_linear(Xc, Xe, Wp, bprime, M, N, K, Y,
+  return hip_status(ot::launch_mx4_linear(Xc, Xe, Wp, bprime, M, N, K, Y, workspace,
                                           static_cast<hipStream_t>(stream)));
 }
 
 size_t ot_qlinear_mx4_workspace_size(int64_t M, int64_t N, int64_t K) {
-  (void)M; (void)N; (void)K;
-  return 0;
+  if (M <= 0 || !mx4_linear_ok(M, N, K)) return 0;
+  return ot::mx4_linear_workspace_bytes(M, N, K);
+}
+
+ot_status ot_qlinear_mx4_plan(int64_t M, int64_t N, int64_t K, int with_workspace, char *buf,
+                              size_t len) {
+  if (!buf || len == 0 || M < 0 || N < 0 || K < 0) return OT_EINVAL;
+  if (!mx4_linear_ok(M, N, K)) return OT_ESHAPE;
+  if (M == 0)
+    snprintf(buf, len, "none");
+  else
+    ot::describe_mx4_linear(M, N, K, with_workspace != 0, buf, len);
+  return OT_OK;
 }
 
 // Sizes of a mixture-of-experts layer: M == 0 is fine.

@@ -44,6 +44,7 @@ namespace detail {
 typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 typedef float v2f __attribute__((ext_vector_type(2)));
+typedef float v4f __attribute__((ext_vector_type(4)));
 typedef unsigned v4u32 __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
@@ -122,16 +123,38 @@ hipError_t launch_dequantize_mx4(const uint8_t *c, const uint8_t *e, int64_t row
 hipError_t launch_pack_weights_mx4(const uint8_t *Wc, const uint8_t *We, int64_t N, int64_t K,
                                    uint8_t *Wp, hipStream_t st);
 
+// Estimated time of a launch in microseconds: passes over the CUs, each of `pass`
+// and `per_k` per K tile, plus `share` per K tile for the workgroups' mean number
+// per CU (what they take from each other), plus `once`.
+struct Mx4Time {
+  double once, pass, per_k, share;
+  double us(int64_t workgroups, int64_t k_tiles, int64_t cus) const {
+    const double passes = (double)((workgroups + cus - 1) / cus), kt = (double)k_tiles;
+    return once + passes * (pass + per_k * kt) + share * kt * (double)workgroups / (double)cus;
+  }
+};
+
+// A launch of the tile kernels: its tile, the parts that K is shared out to, the
+// workspace for their sums and the estimated time.
+struct Mx4Plan {
+  int tile, bn, bm, parts;
+  size_t bytes;
+  double us;
+};
+Mx4Plan mx4_gemm_plan(int64_t M, int64_t N, int64_t K, bool with_workspace);
+hipError_t launch_mx4_gemm(const Mx4Plan &plan, const uint8_t *Xc, const uint8_t *Xe,
+                           const uint8_t *Wp, const float *bp, int64_t M, int64_t N, int64_t K,
+                           uint16_t *Y, void *ws, hipStream_t st);
+bool mx4_gemm_fits(int64_t M, int64_t N);  // whether some tile's grid does
+
 // The product: up to 64 tokens mostly by streaming the weights
-// (ot_mx4_decode.hip), else on tiles.
+// (ot_mx4_decode.hip), else on tiles.  ws: NULL or mx4_linear_workspace_bytes.
 hipError_t launch_mx4_linear(const uint8_t *Xc, const uint8_t *Xe, const uint8_t *Wp,
                              const float *bp, int64_t M, int64_t N, int64_t K, uint16_t *Y,
-                             hipStream_t st);
-// The tiles; whether their count fits a launch, and the one that is picked.
-hipError_t launch_mx4_gemm(const uint8_t *Xc, const uint8_t *Xe, const uint8_t *Wp,
-                           const float *bp, int64_t M, int64_t N, int64_t K, uint16_t *Y,
-                           hipStream_t st);
-bool mx4_gemm_fits(int64_t M, int64_t N);
+                             void *ws, hipStream_t st);
+size_t mx4_linear_workspace_bytes(int64_t M, int64_t N, int64_t K);
+void describe_mx4_linear(int64_t M, int64_t N, int64_t K, bool with_workspace, char *buf,
+                         size_t len);
 // A mixture-of-experts layer; workspace of at least moe_mx4_workspace_bytes.
 size_t moe_mx4_workspace_bytes(int64_t M, int64_t F, int64_t E, int64_t top_k);
 hipError_t launch_moe_mx4(const uint8_t *Xc, const uint8_t *Xe, const uint16_t *logits,

@@ -9,6 +9,8 @@
 // weights': there the wave copies its K tile of all tokens into LDS of its own,
 // whole 128-byte row pieces at a time, and takes the fragments from there.  No
 // wave waits for another before the sums meet.
+#include <stdio.h>
+
 #include "ot_mx4_stream.h"
 #include "ot_mx4_tiles.h"
 
@@ -205,33 +207,67 @@ hipError_t launch_decode_lds(const uint8_t *Xc, const uint8_t *Xe, const uint8_t
 
 using namespace detail;
 
-// Which kernel: 16 rows to a workgroup where that is at most one of them per CU
-// (more, and they read the tokens too often), or where the whole launch is
-// latency; else 32.  From 33 tokens on, with more 32-row workgroups than CUs,
-// the tiles of ot_mx4_gemm.hip, which read the tokens once per 64 or 128 rows.
-// Measured on MI355X, 16 and 32 rows (us):
-//   up to 16 tokens  9 x 3466, K = 24416 12.0 and 15.6; 16 x 5120, K = 20480
-//                    20.2 and 15.2; 8 x 20480, K = 5120 14.0 and 12.2;
-//                    2 x 4352, K = 1024 3.0 and 3.2
-//   17 .. 32         24 x 3840, K = 22528 12.5 and 15.8; 32 x 20480, K = 5120
-//                    17.5 and 14.1
-//   33 .. 64         40 x 3840, K = 22528 15.9 and 19.5; 45 x 5888, K = 14336
-//                    20.0 and 14.6 (64 x 64 tiles 22.8); 64 x 20480, K = 5120
-//                    23.8 and 21.7 (128 x 64 tiles 15.2)
-enum class DecodePlan { kRows16, kRows32, kTiles };
-static DecodePlan decode_plan(int64_t M, int64_t N, int64_t K) {
+// Which kernel.  Up to 16 tokens 16 rows to a workgroup where that is at most one
+// of them per CU (more, and they read the tokens too often), or where the whole
+// launch is latency; else 32.  On MI355X, 16 and 32 rows: 9 x 3466, K = 24416 12.0
+// and 15.6 us; 16 x 5120, K = 20480 20.2 and 15.2; 8 x 20480, K = 5120 14.0 and
+// 12.2; 2 x 4352, K = 1024 3.0 and 3.2; over 50 random launches 0.6 % over the
+// faster one.
+// From 17 on whichever of these and the tiles of ot_mx4_gemm.hip (which read the
+// tokens once per 64 or 128 rows) is estimated to be the fastest.  Fitted to 110
+// random launches, where the choice is 0.9 % over the fastest (15 % at worst); 32 x
+// 5120, K = 20480: 16 rows 21, 32 rows 16.1, tiles 25.2 or, in 3 parts, 16.7; 64 x
+// 20480, K = 5120: 23.8, 21.7 and 15.2; 54 x 4736, K = 1248: 4.3, 4.4 and 4.8.
+static constexpr Mx4Time kDecodeTime[2][2] = {  // [17 .. 32, 33 .. 64][16, 32 rows]
+    {{2.779, 0.041, 0.112, 0.004}, {2.959, 0.221, 0.134, 0.045}},
+    {{2.418, 0.304, 0.140, 0.043}, {2.523, 1.034, 0.150, 0.119}},
+};
+
+// rows: of a workgroup, or 0 for the tiles.
+struct LinearPlan {
+  int rows;
+  Mx4Plan tiles;
+};
+static LinearPlan linear_plan(int64_t M, int64_t N, int64_t K, bool with_workspace) {
   const int64_t cus = device_cus();
-  if (N <= 16 * cus) return DecodePlan::kRows16;
-  if (M <= 16) return N * K < (int64_t(1) << 24) ? DecodePlan::kRows16 : DecodePlan::kRows32;
-  return M <= 32 || N <= 32 * cus ? DecodePlan::kRows32 : DecodePlan::kTiles;
+  if (M <= 16)
+    return {N <= 16 * cus || N * K < (int64_t(1) << 24) ? 16 : 32, Mx4Plan{}};
+  LinearPlan plan{0, mx4_gemm_plan(M, N, K, with_workspace)};
+  if (M > 64) return plan;
+  double least = plan.tiles.us;
+  for (int i = 0; i < 2; ++i) {
+    const int rows = 16 << i;
+    const double us = kDecodeTime[M > 32][i].us((N + rows - 1) / rows, mx4_tiles(K), cus);
+    if (us < least) {
+      plan.rows = rows;
+      least = us;
+    }
+  }
+  return plan;
+}
+
+size_t mx4_linear_workspace_bytes(int64_t M, int64_t N, int64_t K) {
+  const LinearPlan plan = linear_plan(M, N, K, true);
+  return plan.rows ? 0 : plan.tiles.bytes;
+}
+
+void describe_mx4_linear(int64_t M, int64_t N, int64_t K, bool with_workspace, char *buf,
+                         size_t len) {
+  const LinearPlan plan = linear_plan(M, N, K, with_workspace);
+  if (plan.rows)
+    snprintf(buf, len, "decode %d rows", plan.rows);
+  else if (plan.tiles.parts > 1)
+    snprintf(buf, len, "tiles %dx%d split-K %d", plan.tiles.bn, plan.tiles.bm, plan.tiles.parts);
+  else
+    snprintf(buf, len, "tiles %dx%d", plan.tiles.bn, plan.tiles.bm);
 }
 
 hipError_t launch_mx4_linear(const uint8_t *Xc, const uint8_t *Xe, const uint8_t *Wp,
                              const float *bp, int64_t M, int64_t N, int64_t K, uint16_t *Y,
-                             hipStream_t st) {
-  const DecodePlan plan = M <= 64 ? decode_plan(M, N, K) : DecodePlan::kTiles;
-  if (plan == DecodePlan::kTiles) return launch_mx4_gemm(Xc, Xe, Wp, bp, M, N, K, Y, st);
-  const bool narrow = plan == DecodePlan::kRows16;
+                             void *ws, hipStream_t st) {
+  const LinearPlan plan = linear_plan(M, N, K, ws != nullptr);
+  if (plan.rows == 0) return launch_mx4_gemm(plan.tiles, Xc, Xe, Wp, bp, M, N, K, Y, ws, st);
+  const bool narrow = plan.rows == 16;
   if (M <= 16)
     return narrow ? launch_decode<1, 16>(Xc, Xe, Wp, bp, M, N, K, Y, st)
                   : launch_decode<2, 8>(Xc, Xe, Wp, bp, M, N, K, Y, st);

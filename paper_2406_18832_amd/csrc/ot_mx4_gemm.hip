@@ -1,4 +1,4 @@
-// The MX4 linear above 64 tokens:  Y = fp16(sum_k x w + b'), both operands in
+// The MX4 linear above 64 tokens, and below where it is the faster:  Y = fp16(sum_k x w + b'), both operands in
 // MX4 (ot_mx4.h), products and scales on v_mfma_scale_f32_32x32x64_f8f6f4, sums
 // in fp32.
 //
@@ -42,18 +42,22 @@ struct Mx4Cfg {
   static_assert(kSmem <= 160 * 1024, "LDS");
 };
 
-template <int BN, int BM, int WN, int WM, int S>
+// PARTS false: all of K, to Y.  PARTS true: workgroups of `parts` equal shares of
+// the K tiles, whose fp32 sums go to `sums` as mx4_join_kernel reads them.
+template <int BN, int BM, int WN, int WM, int S, bool PARTS>
 __device__ __forceinline__ void mx4_gemm_body(
     uint8_t *smem, const uint8_t *__restrict__ Xc, const uint8_t *__restrict__ Xe,
     const uint8_t *__restrict__ Wp, const float *__restrict__ bp, int M, int N, int K,
-    uint16_t *__restrict__ Y, int tiles_m, int tiles_n) {
+    uint16_t *__restrict__ Y, int tiles_m, int tiles_n, int parts, v4f *__restrict__ sums) {
   using C = Mx4Cfg<BN, BM, WN, WM, S>;
   const int KB = K / 2;                      // bytes of a token row
   const int KT = (K + kMx4Tile - 1) / kMx4Tile;
   const int NB = (N + 31) / 32;              // 32-row blocks of the packed weights
 
-  const TilePlace place(tiles_m, tiles_n);
+  const TilePlace place(tiles_m, tiles_n, PARTS);
   const int tm = place.tm, tn = place.tn;
+  const int kt0 = PARTS ? place.part * KT / parts : 0;               // its K tiles
+  const int kn = PARTS ? (place.part + 1) * KT / parts - kt0 : KT;
   const int n0 = tn * BN, m0 = tm * BM;
 
   const int lane = threadIdx.x & 63;
@@ -86,29 +90,29 @@ __device__ __forceinline__ void mx4_gemm_body(
     ck_b[j] = ((lane & 7) ^ swz_mx4(row)) * 16;
     off_b[j] = (uint32_t)row * (uint32_t)KB + ck_b[j];
   }
-  // Load j of K tile kt into its stage.  Tiles past the end of K load zeros
-  // (out of range) into stages that nobody reads, so that every iteration has
-  // the same number of loads in flight.
+  // Load j of its K tile kt into its stage.  Tiles past the end load zeros (out
+  // of range) into stages that nobody reads, so that every iteration has the
+  // same number of loads in flight.
   auto issue_one = [&](int kt, int j) {
     uint8_t *st = smem + (kt % S) * C::kStage;
     if (j < C::kLoadsA) {
       const int ja = j < C::kLoadsA ? j : 0;
       __builtin_amdgcn_raw_ptr_buffer_load_lds(
           rsrc_a, (lds_void *)(st + (wave * C::kLoadsA + ja) * 1024), 16,
-          kt < KT ? off_a[ja] + (uint32_t)kt * kMx4PackedTile : kOobOffset, 0, 0, 0);
+          kt < kn ? off_a[ja] + (uint32_t)(kt0 + kt) * kMx4PackedTile : kOobOffset, 0, 0, 0);
     } else if (j < C::kLoadsA + C::kLoadsB) {
       const int jb = j >= C::kLoadsA && j < C::kLoadsA + C::kLoadsB ? j - C::kLoadsA : 0;
-      const int k0 = kt * kMx4TileBytes;
+      const int k0 = (kt0 + kt) * kMx4TileBytes;
       __builtin_amdgcn_raw_ptr_buffer_load_lds(
           rsrc_b, (lds_void *)(st + C::kABytes + (wave * C::kLoadsB + jb) * 1024), 16,
-          k0 + ck_b[jb] < KB ? off_b[jb] + (uint32_t)k0 : kOobOffset, 0, 0, 0);
+          kt < kn && k0 + ck_b[jb] < KB ? off_b[jb] + (uint32_t)k0 : kOobOffset, 0, 0, 0);
     } else {
       // Scales: 256-byte piece q, of 32 weight rows or 32 token rows (waves left
       // over load the last one once more).  By 4 bytes a lane, since an odd number
       // of token rows leaves no wider alignment.  Fewer waves copying a KiB each
       // saved loads and cost more (OPT-66B fc2, 8192 tokens: 1229 us, and 1260 so).
       const int q = min(wave * C::kLoadsE + (j - C::kLoadsA - C::kLoadsB), C::kPieces - 1);
-      const int t = min(kt, KT - 1);
+      const int t = kt0 + min(kt, kn - 1);
       if (q < BN / 32) {
         const __amdgpu_buffer_rsrc_t r =
             make_rsrc(scales_w + (int64_t)t * NB * 256, (uint32_t)blocks_a * 256);
@@ -209,14 +213,14 @@ __device__ __forceinline__ void mx4_gemm_body(
     fb[0][g] = *reinterpret_cast<const v4i *>(smem + b_base + g * 32 * 128 + off_f[0]);
     eb[g] = *reinterpret_cast<const int *>(smem + eb_base + g * 256);
   }
-  for (int kt = 0; kt < KT; ++kt) {
+  for (int kt = 0; kt < kn; ++kt) {
     const uint8_t *st = smem + (kt % S) * C::kStage;
     kstep(IntC<0>{}, st, kt + S - 1, C::kMfma);
     kstep(IntC<1>{}, st, kt + S - 1, 2 * C::kMfma);
     kstep(IntC<2>{}, st, kt + S - 1, 3 * C::kMfma);
     // This wave's reads of tile kt are done once lgkmcnt drains, tile kt+1 has
     // landed once at most S-2 younger tiles are in flight; after the barrier
-    // tile kt's stage takes tile kt+S.  At kt = KT-1 the reads of "tile KT" are
+    // tile kt's stage takes tile kt+S.  At kt = kn-1 the reads of "tile kn" are
     // unused.
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
@@ -232,76 +236,125 @@ __device__ __forceinline__ void mx4_gemm_body(
   wait_vmcnt<0>();                     // the trailing out-of-range tiles
   __builtin_amdgcn_s_waitcnt(0xC07F);  // this wave's last reads
   lds_barrier();                       // every wave is done with the ring
-  mx4_epilogue<C::kFN, C::kFM>(smem, acc, bp, M, N, Y, n0 + wn * C::kTN, m0 + wm * C::kTM, wave, lane);
+  if constexpr (PARTS) {
+    v4f *dst = sums + (((int64_t)place.part * tiles_m + tm) * tiles_n + tn) * (BN * BM / 4) +
+               wave * (C::kMfma * 256) + lane;
+#pragma unroll
+    for (int f = 0; f < C::kFN; ++f)
+#pragma unroll
+      for (int g = 0; g < C::kFM; ++g)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          dst[((f * C::kFM + g) * 4 + j) * 64] = v4f{acc[f][g][4 * j], acc[f][g][4 * j + 1],
+                                                     acc[f][g][4 * j + 2], acc[f][g][4 * j + 3]};
+  } else {
+    mx4_epilogue<C::kFN, C::kFM>(smem, acc, bp, M, N, Y, n0 + wn * C::kTN,
+                                 (int64_t)m0 + wm * C::kTM, wave, lane);
+  }
 }
 
-template <int BN, int BM, int WN, int WM, int S>
+template <int BN, int BM, int WN, int WM, int S, bool PARTS>
 __global__ __launch_bounds__(64 * WN * WM, 1) void mx4_gemm_kernel(
     const uint8_t *__restrict__ Xc, const uint8_t *__restrict__ Xe, const uint8_t *__restrict__ Wp,
     const float *__restrict__ bp, int M, int N, int K, uint16_t *__restrict__ Y, int tiles_m,
-    int tiles_n) {
+    int tiles_n, int parts, v4f *__restrict__ sums) {
   __shared__ __attribute__((aligned(1024))) uint8_t smem[Mx4Cfg<BN, BM, WN, WM, S>::kSmem];
-  mx4_gemm_body<BN, BM, WN, WM, S>(smem, Xc, Xe, Wp, bp, M, N, K, Y, tiles_m, tiles_n);
+  mx4_gemm_body<BN, BM, WN, WM, S, PARTS>(smem, Xc, Xe, Wp, bp, M, N, K, Y, tiles_m, tiles_n, parts,
+                                          sums);
 }
 
+// Adds the parts' sums in their order and writes the outputs: the workgroup of a
+// tile, its waves and their registers as in the kernel that made them.
 template <int BN, int BM, int WN, int WM, int S>
+__global__ __launch_bounds__(64 * WN * WM, 1) void mx4_join_kernel(
+    const v4f *__restrict__ sums, const float *__restrict__ bp, int M, int N,
+    uint16_t *__restrict__ Y, int tiles_m, int tiles_n, int parts) {
+  using C = Mx4Cfg<BN, BM, WN, WM, S>;
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[C::kOut];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int tm = blockIdx.x / tiles_n, tn = blockIdx.x % tiles_n;
+  const v4f *src = sums + (int64_t)blockIdx.x * (BN * BM / 4) + wave * (C::kMfma * 256) + lane;
+  const int64_t step = (int64_t)tiles_m * tiles_n * (BN * BM / 4);
+  v16f acc[C::kFN][C::kFM];
+#pragma unroll
+  for (int f = 0; f < C::kFN; ++f)
+#pragma unroll
+    for (int g = 0; g < C::kFM; ++g) acc[f][g] = v16f{};
+  for (int p = 0; p < parts; ++p, src += step)
+#pragma unroll
+    for (int f = 0; f < C::kFN; ++f)
+#pragma unroll
+      for (int g = 0; g < C::kFM; ++g)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const v4f v = src[((f * C::kFM + g) * 4 + j) * 64];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[f][g][4 * j + i] += v[i];
+        }
+  mx4_epilogue<C::kFN, C::kFM>(smem, acc, bp, M, N, Y, tn * BN + (wave % WN) * C::kTN,
+                               (int64_t)tm * BM + (wave / WN) * C::kTM, wave, lane);
+}
+
+template <int BN, int BM, int WN, int WM, int S, bool SPLITS>
 hipError_t launch_mx4_tile(const uint8_t *Xc, const uint8_t *Xe, const uint8_t *Wp,
                            const float *bp, int64_t M, int64_t N, int64_t K, uint16_t *Y,
-                           hipStream_t st) {
+                           int parts, void *workspace, hipStream_t st) {
   const int tiles_m = (int)((M + BM - 1) / BM), tiles_n = (int)((N + BN - 1) / BN);
-  mx4_gemm_kernel<BN, BM, WN, WM, S><<<(unsigned)(tiles_m * tiles_n), 64 * WN * WM, 0, st>>>(
-      Xc, Xe, Wp, bp, (int)M, (int)N, (int)K, Y, tiles_m, tiles_n);
+  const unsigned tiles = (unsigned)(tiles_m * tiles_n);
+  if constexpr (SPLITS) {
+    if (parts > 1) {
+      v4f *sums = static_cast<v4f *>(workspace);
+      mx4_gemm_kernel<BN, BM, WN, WM, S, true><<<tiles * parts, 64 * WN * WM, 0, st>>>(
+          Xc, Xe, Wp, bp, (int)M, (int)N, (int)K, Y, tiles_m, tiles_n, parts, sums);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+      mx4_join_kernel<BN, BM, WN, WM, S><<<tiles, 64 * WN * WM, 0, st>>>(
+          sums, bp, (int)M, (int)N, Y, tiles_m, tiles_n, parts);
+      return hipGetLastError();
+    }
+  }
+  mx4_gemm_kernel<BN, BM, WN, WM, S, false><<<tiles, 64 * WN * WM, 0, st>>>(
+      Xc, Xe, Wp, bp, (int)M, (int)N, (int)K, Y, tiles_m, tiles_n, 1, nullptr);
   return hipGetLastError();
 }
 
-// The tiles and the launch's estimated time in microseconds: passes over the
-// CUs, each of `pass` and `per_k` per K tile, plus `share` per K tile for the
-// workgroups' mean number per CU (what they take from each other), plus `once`.
-// Fitted to 360 random launches on MI355X (33 .. 8192 tokens, 512 .. 28672
-// channels, K = 512 .. 36864) whose weights come from HBM: the tile it picks is
-// 0.6 % over the fastest of these (52 % at worst, on a 4 us launch), 1.3 % over
-// the fastest of nine shapes tried.
+// The tiles.  Their times are fitted to 360 random launches on MI355X (33 .. 8192
+// tokens, 512 .. 28672 channels, K = 512 .. 36864) whose weights come from HBM:
+// the tile they pick is 0.6 % over the fastest of these (52 % at worst, on a 4 us
+// launch), 1.3 % over the fastest of nine shapes tried.
+//
+// `splits`: with a workspace, few tiles share K between up to 16 workgroups each
+// (not more than one of them per CU), whose sums a second launch adds: 3.4 us more
+// and 0.535 us per MB of sums (fitted likewise).  512 tokens x 9216, K = 36864 104
+// us in 3 parts and 167 without; 128 x 9216 45 and 67; 256 x 5120, K = 20480 31
+// and 38; 64 x 5120 17.4 and 22.1; where it would not pay it is not picked (128 x
+// 4096, K = 4096 7.9 and, in 2 parts, 10.7).
 struct Mx4Tile {
   int bn, bm, threads;
-  double once, pass, per_k, share;
+  bool splits;
+  Mx4Time time;
 };
 constexpr Mx4Tile kTiles[] = {
-    {256, 256, 512, -0.485, 9.442, 1.175, 0.631},
-    {192, 256, 512, -0.814, 10.617, 1.014, 0.377},
-    {256, 128, 512, -0.314, 5.946, 0.929, 0.334},
-    {128, 128, 512, 1.111, 4.042, 0.422, 0.205},
-    {64, 128, 256, 1.034, 3.509, 0.343, 0.105},
-    {128, 64, 512, 1.126, 2.890, 0.352, 0.141},
-    {64, 64, 256, 2.539, 1.251, 0.295, -0.004},
+    {256, 256, 512, true, {-0.485, 9.442, 1.175, 0.631}},
+    {192, 256, 512, false, {-0.814, 10.617, 1.014, 0.377}},
+    {256, 128, 512, false, {-0.314, 5.946, 0.929, 0.334}},
+    {128, 128, 512, true, {1.111, 4.042, 0.422, 0.205}},
+    {64, 128, 256, false, {1.034, 3.509, 0.343, 0.105}},
+    {128, 64, 512, true, {1.126, 2.890, 0.352, 0.141}},
+    {64, 64, 256, true, {2.539, 1.251, 0.295, -0.004}},
 };
 constexpr int kTileCount = sizeof(kTiles) / sizeof(kTiles[0]);
+constexpr int kMaxParts = 16;
+constexpr double kJoin = 3.39, kJoinPerByte = 0.535e-6;
 
-// A launch takes fewer than 2^32 work-items: a tile whose grid does not fit is
-// left out.  256 x 256 has the fewest and is always there.
 int64_t tiles_of(const Mx4Tile &t, int64_t M, int64_t N) {
   return ((M + t.bm - 1) / t.bm) * ((N + t.bn - 1) / t.bn);
 }
+// A launch takes fewer than 2^32 work-items: a tile whose grid does not fit is
+// left out.  256 x 256 has the fewest and is always there.
 bool fits(const Mx4Tile &t, int64_t M, int64_t N) {
   return tiles_of(t, M, N) * t.threads <= (int64_t)UINT32_MAX;
-}
-
-int pick_tile(int64_t M, int64_t N, int64_t K) {
-  const int64_t cus = device_cus();
-  const double kt = (double)mx4_tiles(K);
-  int best = 0;
-  double least = 0.0;
-  for (int i = 0; i < kTileCount; ++i) {
-    const Mx4Tile &t = kTiles[i];
-    if (i > 0 && !fits(t, M, N)) continue;
-    const int64_t tiles = tiles_of(t, M, N);
-    const double passes = (double)((tiles + cus - 1) / cus);
-    const double us = t.once + passes * (t.pass + t.per_k * kt) + t.share * kt * tiles / cus;
-    if (i == 0 || us < least) {
-      best = i;
-      least = us;
-    }
-  }
-  return best;
 }
 
 }  // namespace detail
@@ -310,17 +363,36 @@ using namespace detail;
 
 bool mx4_gemm_fits(int64_t M, int64_t N) { return fits(kTiles[0], M, N); }
 
-hipError_t launch_mx4_gemm(const uint8_t *Xc, const uint8_t *Xe, const uint8_t *Wp,
-                           const float *bp, int64_t M, int64_t N, int64_t K, uint16_t *Y,
-                           hipStream_t st) {
-  switch (pick_tile(M, N, K)) {
-    case 0: return launch_mx4_tile<256, 256, 4, 2, 2>(Xc, Xe, Wp, bp, M, N, K, Y, st);
-    case 1: return launch_mx4_tile<192, 256, 2, 4, 2>(Xc, Xe, Wp, bp, M, N, K, Y, st);
-    case 2: return launch_mx4_tile<256, 128, 4, 2, 2>(Xc, Xe, Wp, bp, M, N, K, Y, st);
-    case 3: return launch_mx4_tile<128, 128, 4, 2, 4>(Xc, Xe, Wp, bp, M, N, K, Y, st);
-    case 4: return launch_mx4_tile<64, 128, 2, 2, 4>(Xc, Xe, Wp, bp, M, N, K, Y, st);
-    case 5: return launch_mx4_tile<128, 64, 4, 2, 4>(Xc, Xe, Wp, bp, M, N, K, Y, st);
-    default: return launch_mx4_tile<64, 64, 2, 2, 4>(Xc, Xe, Wp, bp, M, N, K, Y, st);
+Mx4Plan mx4_gemm_plan(int64_t M, int64_t N, int64_t K, bool with_workspace) {
+  const int64_t cus = device_cus(), kt = mx4_tiles(K);
+  Mx4Plan best{};
+  for (int i = 0; i < kTileCount; ++i) {
+    const Mx4Tile &t = kTiles[i];
+    if (i > 0 && !fits(t, M, N)) continue;
+    const int64_t tiles = tiles_of(t, M, N);
+    for (int64_t parts = 1; parts <= kMaxParts; ++parts) {
+      if (parts > 1 && (!with_workspace || !t.splits || tiles * parts > cus || kt < 2 * parts)) break;
+      const int64_t bytes = parts > 1 ? tiles * parts * t.bn * t.bm * 4 : 0;
+      double us = t.time.us(tiles * parts, (kt + parts - 1) / parts, cus);
+      if (parts > 1) us += kJoin + kJoinPerByte * (double)bytes;
+      if ((i == 0 && parts == 1) || us < best.us) best = Mx4Plan{i, t.bn, t.bm, (int)parts, (size_t)bytes, us};
+    }
+  }
+  return best;
+}
+
+hipError_t launch_mx4_gemm(const Mx4Plan &plan, const uint8_t *Xc, const uint8_t *Xe,
+                           const uint8_t *Wp, const float *bp, int64_t M, int64_t N, int64_t K,
+                           uint16_t *Y, void *ws, hipStream_t st) {
+  const int n = plan.parts;
+  switch (plan.tile) {
+    case 0: return launch_mx4_tile<256, 256, 4, 2, 2, true>(Xc, Xe, Wp, bp, M, N, K, Y, n, ws, st);
+    case 1: return launch_mx4_tile<192, 256, 2, 4, 2, false>(Xc, Xe, Wp, bp, M, N, K, Y, n, ws, st);
+    case 2: return launch_mx4_tile<256, 128, 4, 2, 2, false>(Xc, Xe, Wp, bp, M, N, K, Y, n, ws, st);
+    case 3: return launch_mx4_tile<128, 128, 4, 2, 4, true>(Xc, Xe, Wp, bp, M, N, K, Y, n, ws, st);
+    case 4: return launch_mx4_tile<64, 128, 2, 2, 4, false>(Xc, Xe, Wp, bp, M, N, K, Y, n, ws, st);
+    case 5: return launch_mx4_tile<128, 64, 4, 2, 4, true>(Xc, Xe, Wp, bp, M, N, K, Y, n, ws, st);
+    default: return launch_mx4_tile<64, 64, 2, 2, 4, true>(Xc, Xe, Wp, bp, M, N, K, Y, n, ws, st);
   }
 }
 

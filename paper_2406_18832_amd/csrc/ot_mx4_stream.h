@@ -19,7 +19,6 @@
 namespace ot {
 namespace detail {
 
-typedef float v4f __attribute__((ext_vector_type(4)));
 
 template <int kByte>
 __device__ __forceinline__ v4f mfma_mx4_16(v4i a, v4i b, v4f c, uint32_t ea, uint32_t eb) {

@@ -10,14 +10,20 @@ namespace detail {
 // The token and channel tile of this workgroup: each XCD a contiguous range of
 // tiles, walked in groups of 8 token tiles, so that concurrent tiles share
 // operand rows in the XCD's L2 (as the int8 prefill).
+// Several of these per tile (parts of K) follow one another as whole launches.
 struct TilePlace {
-  int tm, tn;
-  __device__ __forceinline__ TilePlace(int tiles_m, int tiles_n) {
+  int tm, tn, part;
+  __device__ __forceinline__ TilePlace(int tiles_m, int tiles_n, bool parts) {
     constexpr int kGroupM = 8;
     const int nwg = gridDim.x, bid = blockIdx.x;
     const int xcd = bid & 7, local = bid >> 3;
     const int per = nwg >> 3, rem = nwg & 7;
-    const int lid = (xcd < rem ? xcd * (per + 1) : rem * (per + 1) + (xcd - rem) * per) + local;
+    int lid = (xcd < rem ? xcd * (per + 1) : rem * (per + 1) + (xcd - rem) * per) + local;
+    part = 0;
+    if (parts) {
+      part = lid / (tiles_m * tiles_n);
+      lid %= tiles_m * tiles_n;
+    }
     const int group_size = kGroupM * tiles_n;
     const int first_m = (lid / group_size) * kGroupM;
     const int gm = min(tiles_m - first_m, kGroupM);
@@ -46,8 +52,8 @@ struct IntC {
 template <int kFN, int kFM>
 __device__ __forceinline__ void mx4_epilogue(uint8_t *smem, const v16f (&acc)[kFN][kFM],
                                              const float *__restrict__ bp, int M, int N,
-                                             uint16_t *__restrict__ Y, int nw0, int mw0, int wave,
-                                             int lane) {
+                                             uint16_t *__restrict__ Y, int nw0, int64_t mw0,
+                                             int wave, int lane) {
   constexpr int kTN = 32 * kFN, kTM = 32 * kFM;
   const int fr = lane & 31, fh = lane >> 5;
   // Lane l of a 32x32 block holds token l mod 32 and, in registers 4j..4j+3,

@@ -168,6 +168,8 @@ def lib() -> ctypes.CDLL:
         L.ot_qlinear_mx4.argtypes = [vp, vp, vp, vp, i64, i64, i64, vp, vp, vp]
         L.ot_qlinear_mx4_workspace_size.restype = ctypes.c_size_t
         L.ot_qlinear_mx4_workspace_size.argtypes = [i64, i64, i64]
+        L.ot_qlinear_mx4_plan.restype = c_int
+        L.ot_qlinear_mx4_plan.argtypes = [i64, i64, i64, c_int, ctypes.c_char_p, ctypes.c_size_t]
         L.ot_moe_mx4.restype = c_int
         L.ot_moe_mx4.argtypes = [vp, vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, i64, c_int, vp, vp,
                                  vp]
@@ -730,6 +732,15 @@ def ot_pack_weights_mx4(Wc, We, Wp, stream=None):
 
 def ot_qlinear_mx4_workspace_size(M: int, N: int, K: int) -> int:
     return int(lib().ot_qlinear_mx4_workspace_size(M, N, K))
+
+
+def ot_qlinear_mx4_plan(M: int, N: int, K: int, with_workspace=False) -> str:
+    """The kernel configuration ot_qlinear_mx4 launches for these sizes on the
+    current device (text; no device work)."""
+    buf = ctypes.create_string_buffer(96)
+    _check(lib().ot_qlinear_mx4_plan(M, N, K, int(bool(with_workspace)), buf, len(buf)),
+           "ot_qlinear_mx4_plan")
+    return buf.value.decode()
 
 
 def _scratch(workspace, need):

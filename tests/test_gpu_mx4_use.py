@@ -1,0 +1,336 @@
+"""The MX4 operators as they are used: one after another, in captured graphs, on
+other streams, with shared and split K, in buffers with neighbours."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import mx4_oracle as X
+from paper_2406_18832_amd import ot, quality, synth
+from tests.test_gpu_mx4 import (dev, draw_activations, draw_moe, draw_mx4, host, moe_expected,
+                                y_tolerance)
+
+pytestmark = pytest.mark.gpu
+
+NAN16 = float("nan")
+
+
+def guarded(rows, cols, dtype, extra=64):
+    """A contiguous [rows, cols] view of a buffer of a fixed byte, and a check that
+    the buffer's rest still holds it."""
+    size = torch.empty((), dtype=dtype).element_size()
+    raw = torch.full((rows * cols * size + 2 * extra,), 0x7B, dtype=torch.uint8, device="cuda")
+    view = raw[extra:extra + rows * cols * size].view(dtype).reshape(rows, cols)
+
+    def untouched():
+        return bool((raw[:extra] == 0x7B).all()) and bool((raw[extra + rows * cols * size:] == 0x7B).all())
+    return view, untouched
+
+
+def linear_operands(r, M, N, K, spread=3):
+    x, w = draw_mx4(r, M, K, spread), draw_mx4(r, N, K, spread)
+    return x, w, r.standard_normal(N).astype(np.float32)
+
+
+# Shared K: each tile that shares it, ragged in tokens, channels and K; parts of
+# unequal length; fewer tokens than the tile has
+SPLITS = [(33, 100, 16416), (60, 512, 20512), (200, 130, 9248), (17, 67, 13088), (65, 2727, 12448), (40, 4200, 24544),
+          (65, 4161, 20928)]
+
+
+@pytest.mark.parametrize("M,N,K", SPLITS)
+def test_linear_with_shared_k(M, N, K):
+    assert "split-K" in ot.ot_qlinear_mx4_plan(M, N, K, True)
+    r = np.random.default_rng([M, N, K])
+    x, w, bias = linear_operands(r, M, N, K)
+    some = np.unique(np.r_[r.integers(0, N, 300), 0, N - 1])
+    y, mags = X.linear(X.values(*x), X.values(w[0][some], w[1][:, some]), bias[some])
+    Wp = ot.pack_weights_mx4(*map(dev, w))
+    need = ot.ot_qlinear_mx4_workspace_size(M, N, K)
+    ws, ws_ok = guarded(1, need, torch.uint8)
+    Y, y_ok = guarded(M, N, torch.float16)
+    for _ in range(2):
+        ws.fill_(0xFF)  # NaNs
+        Y.fill_(NAN16)
+        ot.ot_qlinear_mx4(*map(dev, x), Wp, N, dev(bias), Y, ws.reshape(-1))
+        got = host(Y).astype(np.float64)
+        assert np.all(np.abs(got[:, some] - y) <= y_tolerance(y, mags, K))
+        assert ws_ok() and y_ok()
+    # without a workspace: the same sums in another order
+    alone = host(ot.qlinear_mx4(*map(dev, x), Wp, N, dev(bias), False)).astype(np.float64)
+    assert np.all(np.abs(alone[:, some] - y) <= y_tolerance(y, mags, K))
+    assert not np.isnan(got).any()
+
+
+def test_linear_with_shared_k_on_the_widest_tile():
+    M, N, K = 200, 8332, 36352
+    assert ot.ot_qlinear_mx4_plan(M, N, K, True) == "tiles 256x256 split-K 6"
+    r = np.random.default_rng(3)
+    x, w, bias = linear_operands(r, M, N, K)
+    some = np.unique(np.r_[r.integers(0, N, 200), 0, N - 1])
+    y, mags = X.linear(X.values(*x), X.values(w[0][some], w[1][:, some]), bias[some])
+    got = ot.qlinear_mx4(*map(dev, x), ot.pack_weights_mx4(*map(dev, w)), N, dev(bias), True)
+    assert not bool(got.isnan().any())
+    assert np.all(np.abs(host(got)[:, some].astype(np.float64) - y) <= y_tolerance(y, mags, K))
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 65, 96), (7, 33, 288), (30, 70, 544), (50, 100, 1056),
+                                   (70, 65, 96), (130, 257, 544), (300, 1000, 1056), (65, 70, 3488)])
+def test_linear_neighbours_and_rows_of_nan(M, N, K):
+    """Nothing is written outside Y; a NaN block of a token is its row's alone, one
+    of a weight row its channel's, an infinite bias its own."""
+    r = np.random.default_rng([M, N, K])
+    (xc, xe), (wc, we), bias = linear_operands(r, M, N, K)
+    clean, c_ok = guarded(M, N, torch.float16)
+    Y, y_ok = guarded(M, N, torch.float16)
+    ws = ot.qlinear_mx4_workspace_for(M, N, K)
+    ot.ot_qlinear_mx4(dev(xc), dev(xe), ot.pack_weights_mx4(dev(wc), dev(we)), N, dev(bias), clean, ws)
+    m, n, inf = M // 2, N // 3, N - 1
+    last = K // 32 - 1
+    xe[last // 8, m, last % 8] = 255
+    we[0, n, 0] = 255
+    bias[inf] = np.inf
+    ot.ot_qlinear_mx4(dev(xc), dev(xe), ot.pack_weights_mx4(dev(wc), dev(we)), N, dev(bias), Y, ws)
+    a, b = host(clean), host(Y)
+    assert not np.isnan(a).any() and c_ok() and y_ok()
+    assert np.isnan(b[m]).all() and np.isnan(b[:, n]).all()
+    rows, cols = np.arange(M) != m, (np.arange(N) != n) & (np.arange(N) != inf)
+    assert np.array_equal(a[rows][:, cols], b[rows][:, cols])
+    assert (b[rows, inf] == np.inf).all()
+
+
+@pytest.mark.parametrize("M,K", [(1, 32), (5, 544), (130, 2080)])
+def test_quantizers_write_their_outputs_alone(M, K):
+    r = np.random.default_rng([M, K])
+    x, z, inv_s = draw_activations(r, M, K)
+    g, b = (r.standard_normal(K).astype(np.float16) for _ in range(2))
+    tiles = -(-K // 256)
+    Xc, c_ok = guarded(M, K // 2, torch.uint8)
+    Xe, e_ok = guarded(tiles * M, 8, torch.uint8)
+    y, y_ok = guarded(M, K, torch.float32)
+    Wp, p_ok = guarded(1, ot.ot_packed_weights_mx4_size(M, K), torch.uint8)
+    bp, b_ok = guarded(1, M, torch.float32)
+    e3 = Xe.view(tiles, M, 8)
+    ot.ot_quantize_act_mx4(dev(x), dev(z), dev(inv_s), Xc, e3)
+    ot.ot_dequantize_mx4(Xc, e3, y)
+    ot.ot_pack_weights_mx4(Xc, e3, Wp.reshape(-1))
+    assert np.array_equal(host(Wp)[0], X.pack(host(Xc), host(e3)))
+    ot.ot_ln_quantize_act_mx4(dev(x), dev(g), dev(b), 1e-5, dev(z), dev(inv_s), Xc, e3)
+    ot.ot_fold_weights_mx4(dev(x), None, dev(z), dev(inv_s), Xc, e3, bp.reshape(-1))
+    assert all(ok() for ok in (c_ok, e_ok, y_ok, p_ok, b_ok))
+
+
+def test_fold_of_more_rows_than_a_launch_has_workgroups():
+    """Beyond 2^21 rows the workgroups take several pairs of rows each."""
+    N, K = (1 << 21) + 3, 32
+    g = torch.Generator(device="cuda").manual_seed(1)
+    W = torch.randn(N, K, device="cuda", generator=g).half()
+    z = torch.randn(K, device="cuda", generator=g)
+    Wc, We, bp = ot.fold_weights_mx4(W, None, z, None)
+    for part in (slice(0, 1000), slice(N - 1000, N), slice((1 << 21) - 500, (1 << 21) + 3)):
+        c, e, b = X.fold(host(W[part]), None, host(z), None)
+        assert np.array_equal(host(Wc[part]), c) and np.array_equal(host(We[:, part]), e)
+        # one rounding of the fp64 sum, itself off by far less
+        assert np.all(np.abs(host(bp[part]) - b) <= np.abs(b) * 2.0 ** -23 + 1e-30)
+    # every row: the largest level of a block is 4 or 6 and its scale is the row's
+    y = ot.dequantize_mx4(Wc, We)
+    assert bool(((y - W.float()).abs().amax(1) <= W.float().abs().amax(1) / 4).all())
+    assert bool((bp - W.double() @ z.double()).abs().max() < 1e-4)
+
+
+# --- one after another ----------------------------------------------------------
+
+def layer(r, N, K):
+    W = (r.standard_normal((N, K)) * K ** -0.5).astype(np.float16)
+    b = r.standard_normal(N).astype(np.float16)
+    return W, b
+
+
+def fold(W, b, z, s):
+    Wc, We, bp = ot.fold_weights_mx4(dev(W), dev(b), dev(z), dev(s))
+    return ot.pack_weights_mx4(Wc, We), bp
+
+
+@pytest.mark.parametrize("M", [1, 9, 40, 150])
+def test_a_block_of_layers(M):
+    """LayerNorm and quantizer, a linear, a quantizer, a linear, and a mixture of
+    experts behind a LayerNorm: each output against the plain form of what went
+    in (a code apart would be a step of the next operator, so each is checked by
+    itself on the values that the GPU handed on)."""
+    r = np.random.default_rng(M)
+    H, F, E, top = 288, 1056, 6, 2
+    h, z, inv_s = draw_activations(r, M, H)
+    gamma, beta = (r.standard_normal(H).astype(np.float16) for _ in range(2))
+    (W1, b1), (W2, b2) = layer(r, F, H), layer(r, H, F)
+    P1, p1 = fold(W1, b1, z, 1 / inv_s)
+    Xc, Xe = ot.ln_quantize_act_mx4(dev(h), dev(gamma), dev(beta), 1e-5, dev(z), dev(inv_s))
+    Y1 = ot.qlinear_mx4(Xc, Xe, P1, F, p1, True)
+    c, e, bias = X.fold(W1, b1, z, 1 / inv_s)
+    y, mags = X.linear(X.values(host(Xc), host(Xe)), X.values(c, e), bias)
+    # bprime is rounded to fp32 once
+    tol = y_tolerance(y, mags, H) + np.abs(bias) * 2.0 ** -24
+    assert np.all(np.abs(host(Y1).astype(np.float64) - y) <= tol)
+
+    z2, s2 = np.zeros(F, np.float32) + 0.25, r.uniform(0.5, 2, F).astype(np.float32)
+    P2, p2 = fold(W2, b2, z2, s2)
+    A = Y1.relu()
+    Ac, Ae = ot.quantize_act_mx4(A, dev(z2), dev((1 / s2).astype(np.float32)))
+    Y2 = ot.qlinear_mx4(Ac, Ae, P2, H, p2, True)
+    c, e = X.to_mx4(X.activations(host(A), z2, (1 / s2).astype(np.float32)))
+    assert np.array_equal(host(Ac), c) and np.array_equal(host(Ae), e)
+    wc, we, bias = X.fold(W2, b2, z2, s2)
+    y, mags = X.linear(X.values(c, e), X.values(wc, we), bias)
+    tol = y_tolerance(y, mags, F) + np.abs(bias) * 2.0 ** -24
+    assert np.all(np.abs(host(Y2).astype(np.float64) - y) <= tol)
+
+    if M > 64:
+        return
+    Bc, Be = ot.ln_quantize_act_mx4(Y2, dev(gamma), dev(beta), 1e-5, dev(z * 0), dev(inv_s * 0 + 1))
+    _, logits, w1, b1, w2, b2 = draw_moe(r, M, H, 96, E, "swiglu")
+    P1, P2 = (ot.pack_weights_mx4(*map(dev, w)) for w in (w1, w2))
+    out = ot.moe_mx4(Bc, Be, dev(logits), top, P1, dev(b1), P2, dev(b2), 96, "swiglu")
+    x = (host(Bc), host(Be))
+    y, tol = moe_expected(x, logits, top, w1, b1, w2, b2, 96, "swiglu")
+    assert np.all(np.abs(host(out).astype(np.float64) - y) <= tol)
+
+
+# --- graphs and streams -----------------------------------------------------------
+
+class Step:
+    """A decode step on buffers of its own: LayerNorm, quantizers, a wide linear, one
+    with shared K and a mixture of experts."""
+    M, H, N, E, F, TOP = 40, 2080, 24544, 5, 160, 2
+
+    def __init__(self, seed):
+        r = np.random.default_rng(seed)
+        self.h = dev(draw_activations(r, self.M, self.H)[0])
+        one = torch.ones(self.H, device="cuda")
+        self.norm = (one.half(), (one * 0.5).half(), 1e-5, one * 0.25, one * 0.5)
+        self.fc1 = ot.pack_weights_mx4(*map(dev, draw_mx4(r, self.N, self.H, 1)))
+        self.fc2 = ot.pack_weights_mx4(*map(dev, draw_mx4(r, self.H, self.N, 1)))
+        self.b1, self.b2 = torch.randn(self.N, device="cuda"), torch.randn(self.H, device="cuda")
+        _, logits, w1, _, w2, _ = draw_moe(r, self.M, self.H, self.F, self.E, "relu")
+        self.logits, self.w1, self.w2 = dev(logits), *(ot.pack_weights_mx4(*map(dev, w)) for w in (w1, w2))
+        codes = lambda k: ot._mx4_empty(self.M, k, "cuda")
+        half = lambda k: torch.empty(self.M, k, dtype=torch.float16, device="cuda")
+        self.x, self.a, self.c = codes(self.H), codes(self.N), codes(self.H)
+        self.y1, self.y2, self.out = half(self.N), half(self.H), half(self.H)
+        assert "split-K" in ot.ot_qlinear_mx4_plan(self.M, self.H, self.N, True)
+        self.ws1 = ot.qlinear_mx4_workspace_for(self.M, self.N, self.H)
+        self.ws2 = ot.qlinear_mx4_workspace_for(self.M, self.H, self.N)
+        self.ws = ot.moe_mx4_workspace_for(self.M, self.H, self.F, self.E, self.TOP)
+
+    def run(self):
+        ot.ot_ln_quantize_act_mx4(self.h, *self.norm, *self.x)
+        ot.ot_qlinear_mx4(*self.x, self.fc1, self.N, self.b1, self.y1, self.ws1)
+        ot.ot_quantize_act_mx4(self.y1, None, None, *self.a)
+        ot.ot_qlinear_mx4(*self.a, self.fc2, self.H, self.b2, self.y2, self.ws2)
+        ot.ot_ln_quantize_act_mx4(self.y2, *self.norm, *self.c)
+        ot.ot_moe_mx4(*self.c, self.logits, self.TOP, self.w1, None, self.w2, None, self.F, "relu",
+                      self.out, self.ws)
+
+    def clear(self):
+        for t in (*self.x, *self.a, *self.c, self.y1, self.y2, self.out, self.ws):
+            t.zero_()
+
+    def outputs(self):
+        return [t.clone() for t in (self.y1, self.y2, self.out)]
+
+
+def equal(a, b):
+    return all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+def test_captured_and_replayed():
+    step = Step(1)
+    step.run()
+    torch.cuda.synchronize()
+    eager = step.outputs()
+    assert all(bool(t.isfinite().all()) and bool(t.abs().max() > 0) for t in eager)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step.run()
+    other = dev(draw_activations(np.random.default_rng(9), Step.M, Step.H)[0])
+    first = step.h.clone()
+    for i in range(4):
+        step.clear()
+        step.h.copy_(first)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert equal(step.outputs(), eager), i
+        # other inputs through the same graph, and eagerly between the replays
+        step.clear()
+        step.h.copy_(other)
+        graph.replay()
+        replayed = step.outputs()
+        step.clear()
+        step.run()
+        torch.cuda.synchronize()
+        assert equal(replayed, step.outputs()) and not equal(replayed, eager), i
+
+
+def test_two_graphs_at_once_on_streams_of_their_own():
+    steps, streams = [Step(2), Step(3)], [torch.cuda.Stream() for _ in range(2)]
+    wanted, graphs = [], []
+    for step, s in zip(steps, streams):
+        step.run()
+        torch.cuda.synchronize()
+        wanted.append(step.outputs())
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            step.run()
+        graphs.append(g)
+    for _ in range(3):
+        for step in steps:
+            step.clear()
+        torch.cuda.synchronize()
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                for _ in range(5):
+                    g.replay()
+        torch.cuda.synchronize()
+        assert all(equal(step.outputs(), w) for step, w in zip(steps, wanted))
+
+
+def test_eager_on_two_streams_and_by_handle():
+    steps, streams = [Step(4), Step(5)], [torch.cuda.Stream() for _ in range(2)]
+    wanted = []
+    for step in steps:
+        step.run()
+        torch.cuda.synchronize()
+        wanted.append(step.outputs())
+        step.clear()
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for step, s in zip(steps, streams):
+            with torch.cuda.stream(s):
+                step.run()
+    torch.cuda.synchronize()
+    assert all(equal(step.outputs(), w) for step, w in zip(steps, wanted))
+    # the stream as an argument, the current one another
+    step, s = steps[0], streams[0]
+    y = torch.empty_like(step.y1)
+    torch.cuda.synchronize()
+    ot.ot_qlinear_mx4(*step.x, step.fc1, step.N, step.b1, y, step.ws1, s.cuda_stream)
+    s.synchronize()
+    assert torch.equal(y, wanted[0][0])
+
+
+# --- the method on the format -------------------------------------------------------
+
+def test_symmetrization_helps_where_channels_are_offset():
+    """One linear of the workload that shifts every channel: the MX4 product with
+    the shift and scale of the channels taken out first, with the scale alone and
+    with neither."""
+    wl = synth.WORKLOADS["opt13b_w6a6"]
+    Xh, W, b, minmax = quality.layer_inputs(wl, 0, 64, 64, 2)
+    ref = torch.matmul(Xh.double(), W.double().t()) + b.double()
+    errs = {label: quality.errors(quality.run_config(Xh, W, b, minmax, *how), ref)["rel_fro"]
+            for label, *how in quality.MX4_CONFIGS}
+    assert errs["MX4"] < errs["MX4 no-sym"] and errs["MX4"] < errs["MX4 plain"], errs
+    # and the configuration is the plain form's product
+    c, e = X.to_mx4(X.activations(host(Xh)))
+    some = np.random.default_rng(1).integers(0, W.shape[0], 500)
+    wc, we, bias = X.fold(host(W)[some], host(b)[some], None, None)
+    y, mags = X.linear(X.values(c, e), X.values(wc, we), bias)
+    got = host(quality.run_config(Xh, W, b, minmax, 4, 4, "mx4-plain")).astype(np.float64)[:, some]
+    assert np.all(np.abs(got - y) <= y_tolerance(y, mags, W.shape[1]))

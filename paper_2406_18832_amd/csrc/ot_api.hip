@@ -507,7 +507,7 @@ static bool moe_shape_ok(int64_t M, int64_t H, int64_t F, int64_t E, int64_t top
 
 size_t ot_moe_mx4_workspace_size(int64_t M, int64_t H, int64_t F, int64_t E, int64_t top_k) {
   if (M <= 0 || !moe_shape_ok(M, H, F, E, top_k)) return 0;
-  return ot::moe_mx4_workspace_bytes(M, F, E, top_k);
+  return ot::moe_mx4_workspace_bytes(M, H, F, E, top_k);
 }
 
 ot_status ot_moe_mx4(const uint8_t *Xc, const uint8_t *Xe, const uint16_t *logits,

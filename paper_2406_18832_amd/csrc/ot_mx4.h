@@ -156,7 +156,7 @@ size_t mx4_linear_workspace_bytes(int64_t M, int64_t N, int64_t K);
 void describe_mx4_linear(int64_t M, int64_t N, int64_t K, bool with_workspace, char *buf,
                          size_t len);
 // A mixture-of-experts layer; workspace of at least moe_mx4_workspace_bytes.
-size_t moe_mx4_workspace_bytes(int64_t M, int64_t F, int64_t E, int64_t top_k);
+size_t moe_mx4_workspace_bytes(int64_t M, int64_t H, int64_t F, int64_t E, int64_t top_k);
 hipError_t launch_moe_mx4(const uint8_t *Xc, const uint8_t *Xe, const uint16_t *logits,
                           const uint8_t *W1, const float *b1, const uint8_t *W2, const float *b2,
                           int64_t M, int64_t H, int64_t F, int64_t E, int64_t top_k, bool glu,

@@ -1,5 +1,5 @@
 // A mixture-of-experts layer on MX4 weights for at most 64 tokens, in two
-// launches.
+// launches, or three where there are few output channels.
 //
 //   p    = softmax over a token's top_k largest logits (ties to the lower expert)
 //   g_j  = W1_e x + b1_e for its j-th expert e
@@ -20,13 +20,21 @@
 // Kernel 2: a workgroup takes 16 output channels and all tokens.  Its waves
 // share out the K tiles of all chosen experts in one row, add p_j times each
 // expert's product to their own fp32 sums in LDS, and the waves' sums meet in
-// wave order: no atomics, so the result does not vary.
+// wave order: no atomics, so the result does not vary.  Where H / 16 workgroups
+// leave CUs idle, several share that row of K tiles, and kernel 3 adds their sums.
 #include "ot_mx4_stream.h"
 
 namespace ot {
 namespace detail {
 
 constexpr int kMoeWaves1 = 4, kMoeWaves2 = 16;
+
+__device__ __forceinline__ uint2 half4(v4f s) {
+  uint2 h;
+  h.x = (uint32_t)float_to_half_bits(s[0]) | ((uint32_t)float_to_half_bits(s[1]) << 16);
+  h.y = (uint32_t)float_to_half_bits(s[2]) | ((uint32_t)float_to_half_bits(s[3]) << 16);
+  return h;
+}
 
 // A token's logit for expert e as an integer that orders as the choice does:
 // larger comes first, the lower expert first among equals, -0 equal to 0, NaN
@@ -84,6 +92,7 @@ struct MoeWs {
   uint8_t *codes, *scales;
   int *expert;              // [M top_k], -1: none
   float *weight;            // [M top_k]
+  float *sums;              // [parts][M][H], with more than one part
 };
 
 struct MoeArgs {
@@ -374,8 +383,15 @@ __global__ __launch_bounds__(64 * kMoeWaves2) void moe_mx4_out_kernel(MoeArgs a)
   // ---- this wave's share of the groups' K tiles, as one row of steps ------------------
   const int tiles = (a.F + kMx4Tile - 1) / kMx4Tile;
   const int total = __builtin_amdgcn_readfirstlane(ngroups) * tiles;
-  const int i0 = (int)((int64_t)total * wave / kMoeWaves2);
-  const int i1 = (int)((int64_t)total * (wave + 1) / kMoeWaves2);
+  // (at most 320 groups of 256 K tiles, and 2048 shares: 32 bits)
+  int i0 = 0, i1 = total;
+  if (gridDim.y > 1) {
+    i0 = (int)((unsigned)total * blockIdx.y / gridDim.y);
+    i1 = (int)((unsigned)total * (blockIdx.y + 1) / gridDim.y);
+  }
+  const int mine = i1 - i0;
+  i1 = i0 + mine * (wave + 1) / kMoeWaves2;
+  i0 += mine * wave / kMoeWaves2;
   const int64_t blocks = (int64_t)a.E * a.H / 32;
   float *own = sums + wave * a.M * 16;
   // Loads run kDepth steps ahead, over the groups' borders.
@@ -446,7 +462,7 @@ __global__ __launch_bounds__(64 * kMoeWaves2) void moe_mx4_out_kernel(MoeArgs a)
   for (int i = threadIdx.x; i < a.M * 4; i += blockDim.x) {
     const int m = i >> 2;
     v4f s = v4f{0.f, 0.f, 0.f, 0.f};
-    if (a.b2)
+    if (a.b2 && blockIdx.y == 0)
       for (int j = 0; j < a.top_k; ++j) {
         const int e = expert[m * a.top_k + j];
         if (e >= 0)
@@ -478,11 +494,36 @@ __global__ __launch_bounds__(64 * kMoeWaves2) void moe_mx4_out_kernel(MoeArgs a)
     const int64_t n = (int64_t)blockIdx.x * 16 + 4 * (i & 3);
     v4f s = lds[m * 4 + (i & 3)];
     for (int v = 1; v <= kMoeWaves2; ++v) s += lds[(v * a.M + m) * 4 + (i & 3)];
-    uint2 h;
-    h.x = (uint32_t)float_to_half_bits(s[0]) | ((uint32_t)float_to_half_bits(s[1]) << 16);
-    h.y = (uint32_t)float_to_half_bits(s[2]) | ((uint32_t)float_to_half_bits(s[3]) << 16);
-    *reinterpret_cast<uint2 *>(a.Y + (int64_t)m * a.H + n) = h;
+    if (gridDim.y > 1)
+      *reinterpret_cast<v4f *>(a.ws.sums + ((int64_t)blockIdx.y * a.M + m) * a.H + n) = s;
+    else
+      *reinterpret_cast<uint2 *>(a.Y + (int64_t)m * a.H + n) = half4(s);
   }
+}
+
+// Adds the parts' sums, in their order: four channels to a thread.
+__global__ __launch_bounds__(256) void moe_mx4_join_kernel(const float *__restrict__ sums,
+                                                           int64_t outputs, int parts,
+                                                           uint16_t *__restrict__ Y) {
+  const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (i >= outputs) return;
+  v4f s = *reinterpret_cast<const v4f *>(sums + i);
+#pragma unroll 4
+  for (int p = 1; p < parts; ++p) s += *reinterpret_cast<const v4f *>(sums + p * outputs + i);
+  *reinterpret_cast<uint2 *>(Y + i) = half4(s);
+}
+
+// Parts that the second kernel's work is shared out to: as many as give every CU a
+// workgroup, each wave at least two K tiles (counting one step of tokens per
+// expert).  On MI355X, whole layers with and without: 20 tokens, H = 768, 43 experts
+// of 9728 41 and 68 us; 57, 512, 13 of 9696 (top 7) 39 and 87; one token, 864, 9
+// gated of 12448 (top 6) 38 and 48; 3, 1888, 24 gated of 7872 54 and 60; at two K
+// tiles to a wave one token, 512, 20 of 2048 (top 8) 16.8 and 16.3.
+int moe_parts(int64_t M, int64_t H, int64_t F, int64_t E, int64_t top_k) {
+  const int64_t slots = M * top_k, steps = (E < slots ? E : slots) * mx4_tiles(F);
+  int64_t parts = device_cus() / (H / 16);
+  if (parts > steps / (2 * kMoeWaves2)) parts = steps / (2 * kMoeWaves2);
+  return parts < 2 ? 1 : (int)parts;
 }
 
 size_t moe_out_lds(int M, int E, int top_k) {
@@ -500,10 +541,11 @@ static size_t moe_code_bytes(int64_t M, int64_t F, int64_t E) {
   return (size_t)(E * ((M + 15) / 16)) * mx4_tiles(F) * 2048;
 }
 
-size_t moe_mx4_workspace_bytes(int64_t M, int64_t F, int64_t E, int64_t top_k) {
+size_t moe_mx4_workspace_bytes(int64_t M, int64_t H, int64_t F, int64_t E, int64_t top_k) {
   const size_t slots = (size_t)M * top_k;
+  const int parts = moe_parts(M, H, F, E, top_k);
   return moe_code_bytes(M, F, E) + moe_code_bytes(M, F, E) / 8 + align16(slots * sizeof(int)) +
-         align16(slots * sizeof(float));
+         align16(slots * sizeof(float)) + (parts > 1 ? (size_t)parts * M * H * sizeof(float) : 0);
 }
 
 hipError_t launch_moe_mx4(const uint8_t *Xc, const uint8_t *Xe, const uint16_t *logits,
@@ -520,6 +562,8 @@ hipError_t launch_moe_mx4(const uint8_t *Xc, const uint8_t *Xe, const uint16_t *
   a.ws.expert = reinterpret_cast<int *>(p);
   p += align16(slots * sizeof(int));
   a.ws.weight = reinterpret_cast<float *>(p);
+  p += align16(slots * sizeof(float));
+  a.ws.sums = reinterpret_cast<float *>(p);
   // Waves to a block of hidden channels: enough that a CU has some 70 KB of weights
   // in flight (4 waves of gate and value rows, 8 of one kind), as far as H has K
   // tiles for them.  One token through two experts of 16384, H = 4096: 18.6 us with
@@ -545,10 +589,19 @@ hipError_t launch_moe_mx4(const uint8_t *Xc, const uint8_t *Xe, const uint16_t *
   hipError_t err = hipGetLastError();
   if (err != hipSuccess) return err;
   const size_t lds = moe_out_lds((int)M, (int)E, (int)top_k);
+  const int out_parts = moe_parts(M, H, F, E, top_k);
+  const dim3 out_grid((unsigned)(H / 16), (unsigned)out_parts);
   // 32 tokens of an expert to a step where it has more than 12 on average: with
   // fewer, half of the token loads and products would be of nobody
-  if (M <= 16 || (int64_t)slots <= 12 * E) moe_mx4_out_kernel<1><<<(unsigned)(H / 16), 64 * kMoeWaves2, lds, st>>>(a);
-  else moe_mx4_out_kernel<2><<<(unsigned)(H / 16), 64 * kMoeWaves2, lds, st>>>(a);
+  if (M <= 16 || (int64_t)slots <= 12 * E)
+    moe_mx4_out_kernel<1><<<out_grid, 64 * kMoeWaves2, lds, st>>>(a);
+  else
+    moe_mx4_out_kernel<2><<<out_grid, 64 * kMoeWaves2, lds, st>>>(a);
+  err = hipGetLastError();
+  if (err != hipSuccess || out_parts == 1) return err;
+  const int64_t outputs = M * H;
+  moe_mx4_join_kernel<<<(unsigned)((outputs / 4 + 255) / 256), 256, 0, st>>>(a.ws.sums, outputs,
+                                                                             out_parts, Y);
   return hipGetLastError();
 }
 

@@ -137,6 +137,54 @@ def test_fold_of_more_rows_than_a_launch_has_workgroups():
     assert bool((bp - W.double() @ z.double()).abs().max() < 1e-4)
 
 
+def moe_call(x, logits, k, w1, b1, w2, b2, F, act, Y, ws):
+    ot.ot_moe_mx4(dev(x[0]), dev(x[1]), dev(logits), k, ot.pack_weights_mx4(*map(dev, w1)),
+                  dev(b1), ot.pack_weights_mx4(*map(dev, w2)), dev(b2), F, act, Y, ws)
+
+
+# the second kernel's K tiles shared between workgroups: few output channels, and
+# experts enough (the last one has one part all the same)
+@pytest.mark.parametrize("M,H,F,E,k", [(40, 96, 1056, 32, 2), (17, 512, 1312, 20, 2), (64, 32, 544, 70, 3),
+                                       (5, 256, 800, 30, 4), (1, 32, 4128, 16, 8), (9, 288, 96, 4, 2)])
+@pytest.mark.parametrize("act", ["relu", "swiglu"])
+def test_moe_with_shared_k(M, H, F, E, k, act):
+    r = np.random.default_rng([M, H, F, E, k])
+    x, logits, w1, b1, w2, b2 = draw_moe(r, M, H, F, E, act)
+    logits[M // 2] = -np.inf  # a token without an expert
+    y, tol = moe_expected(x, logits, k, w1, b1, w2, b2, F, act)
+    ws, ws_ok = guarded(1, ot.ot_moe_mx4_workspace_size(M, H, F, E, k), torch.uint8)
+    Y, y_ok = guarded(M, H, torch.float16)
+    outs = []
+    for fill in (0xFF, 0x00):
+        ws.fill_(fill)
+        Y.fill_(NAN16)
+        moe_call(x, logits, k, w1, b1, w2, b2, F, act, Y, ws.reshape(-1))
+        assert ws_ok() and y_ok()
+        outs.append(Y.clone())
+    assert torch.equal(outs[0], outs[1])
+    assert np.all(np.abs(host(outs[0]).astype(np.float64) - y) <= tol)
+    assert not host(outs[0])[M // 2].any()
+
+
+def test_moe_nan_blocks_stay_with_their_tokens_and_experts():
+    """A NaN block of a token reaches that token alone, one of an expert's weights
+    the tokens that chose it."""
+    M, H, F, E, k = 20, 128, 96, 6, 2
+    r = np.random.default_rng(8)
+    x, logits, w1, b1, w2, b2 = draw_moe(r, M, H, F, E, "relu")
+    ws = ot.moe_mx4_workspace_for(M, H, F, E, k)
+    clean, Y = (torch.empty(M, H, dtype=torch.float16, device="cuda") for _ in range(2))
+    moe_call(x, logits, k, w1, b1, w2, b2, F, "relu", clean, ws)
+    chosen = X.top_k(logits, k)
+    x[1][0, 3, 1] = 255
+    w2[1][0, 4 * H:5 * H, 0] = 255
+    moe_call(x, logits, k, w1, b1, w2, b2, F, "relu", Y, ws)
+    bad = (chosen == 4).any(1)
+    bad[3] = True
+    assert not clean.isnan().any() and 1 < bad.sum() < M
+    assert bool(Y[dev(bad)].isnan().all()) and torch.equal(Y[dev(~bad)], clean[dev(~bad)])
+
+
 # --- one after another ----------------------------------------------------------
 
 def layer(r, N, K):

@@ -499,8 +499,8 @@ size_t ot_qlinear_mx4_workspace_size(int64_t M, int64_t N, int64_t K);
  * these sizes on the current device, given a workspace or not; as
  * ot_qlinear_plan.  Writes "none" for M == 0, "decode <R> rows" (output channels
  * per workgroup: 16 or 32), or "tiles <R>x<T>" (output channels x tokens per
- * workgroup: 256x256, 192x256, 256x128, 128x128, 64x128, 128x64 or 64x64), with
- * " split-K <parts>" where K is shared between workgroups.
+ * workgroup: 256x256, 192x256, 256x128, 192x128, 128x128, 64x128, 128x64
+ * or 64x64), with " split-K <parts>" where K is shared between workgroups.
  */
 ot_status ot_qlinear_mx4_plan(int64_t M, int64_t N, int64_t K, int with_workspace,
                               char *buf, size_t len);

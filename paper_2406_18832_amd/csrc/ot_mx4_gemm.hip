@@ -322,7 +322,7 @@ hipError_t launch_mx4_tile(const uint8_t *Xc, const uint8_t *Xe, const uint8_t *
 // The tiles.  Their times are fitted to 360 random launches on MI355X (33 .. 8192
 // tokens, 512 .. 28672 channels, K = 512 .. 36864) whose weights come from HBM:
 // the tile they pick is 0.6 % over the fastest of these (52 % at worst, on a 4 us
-// launch), 1.3 % over the fastest of nine shapes tried.
+// launch), 1.0 % over the fastest of nine shapes tried.
 //
 // `splits`: with a workspace, few tiles share K between up to 16 workgroups each
 // (not more than one of them per CU), whose sums a second launch adds: 3.4 us more
@@ -339,6 +339,7 @@ constexpr Mx4Tile kTiles[] = {
     {256, 256, 512, true, {-0.485, 9.442, 1.175, 0.631}},
     {192, 256, 512, false, {-0.814, 10.617, 1.014, 0.377}},
     {256, 128, 512, false, {-0.314, 5.946, 0.929, 0.334}},
+    {192, 128, 512, false, {0.606, 5.894, 0.814, 0.190}},
     {128, 128, 512, true, {1.111, 4.042, 0.422, 0.205}},
     {64, 128, 256, false, {1.034, 3.509, 0.343, 0.105}},
     {128, 64, 512, true, {1.126, 2.890, 0.352, 0.141}},
@@ -389,9 +390,10 @@ hipError_t launch_mx4_gemm(const Mx4Plan &plan, const uint8_t *Xc, const uint8_t
     case 0: return launch_mx4_tile<256, 256, 4, 2, 2, true>(Xc, Xe, Wp, bp, M, N, K, Y, n, ws, st);
     case 1: return launch_mx4_tile<192, 256, 2, 4, 2, false>(Xc, Xe, Wp, bp, M, N, K, Y, n, ws, st);
     case 2: return launch_mx4_tile<256, 128, 4, 2, 2, false>(Xc, Xe, Wp, bp, M, N, K, Y, n, ws, st);
-    case 3: return launch_mx4_tile<128, 128, 4, 2, 4, true>(Xc, Xe, Wp, bp, M, N, K, Y, n, ws, st);
-    case 4: return launch_mx4_tile<64, 128, 2, 2, 4, false>(Xc, Xe, Wp, bp, M, N, K, Y, n, ws, st);
-    case 5: return launch_mx4_tile<128, 64, 4, 2, 4, true>(Xc, Xe, Wp, bp, M, N, K, Y, n, ws, st);
+    case 3: return launch_mx4_tile<192, 128, 2, 4, 2, false>(Xc, Xe, Wp, bp, M, N, K, Y, n, ws, st);
+    case 4: return launch_mx4_tile<128, 128, 4, 2, 4, true>(Xc, Xe, Wp, bp, M, N, K, Y, n, ws, st);
+    case 5: return launch_mx4_tile<64, 128, 2, 2, 4, false>(Xc, Xe, Wp, bp, M, N, K, Y, n, ws, st);
+    case 6: return launch_mx4_tile<128, 64, 4, 2, 4, true>(Xc, Xe, Wp, bp, M, N, K, Y, n, ws, st);
     default: return launch_mx4_tile<64, 64, 2, 2, 4, true>(Xc, Xe, Wp, bp, M, N, K, Y, n, ws, st);
   }
 }

@@ -183,9 +183,19 @@ LINEARS = [(1, 1, 32), (1, 33, 64), (2, 16, 96), (16, 768, 768), (17, 100, 288),
            # 32 rows to a workgroup: more than 16 x 256 channels
            (1, 4128, 4352), (16, 4100, 5120), (17, 4100, 288), (32, 4097, 2304), (40, 4100, 544),
            (64, 4099, 2080), (40, 8300, 96), (64, 8193, 800),
-           # each tile's own sizes, ragged: 256 x 256, 192 x 256, 256 x 128, 128 x 128, 64 x 128
+           # each tile's own sizes, ragged (TILES)
            (4000, 8000, 320), (2000, 12250, 96), (1100, 7700, 160), (500, 5100, 1056),
-           (128, 9000, 96)]
+           (128, 9000, 96), (2830, 5637, 288), (906, 8330, 800), (1628, 1167, 64), (264, 6535, 64),
+           (1035, 7173, 64), (407, 8425, 64), (69, 8347, 64)]
+
+TILES = {(2000, 12250, 96): "256x128", (906, 8330, 800): "192x256", (1035, 7173, 64): "256x256",
+         (2830, 5637, 288): "192x128", (264, 6535, 64): "128x128", (1628, 1167, 64): "64x128",
+         (69, 8347, 64): "128x64", (300, 1000, 1056): "64x64"}
+
+
+def test_each_tile_has_its_sizes():
+    for sizes, tile in TILES.items():
+        assert sizes in LINEARS and ot.ot_qlinear_mx4_plan(*sizes) == "tiles " + tile
 
 
 @pytest.mark.parametrize("M,N,K", LINEARS)

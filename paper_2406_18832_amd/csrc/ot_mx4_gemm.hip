@@ -326,9 +326,9 @@ hipError_t launch_mx4_tile(const uint8_t *Xc, const uint8_t *Xe, const uint8_t *
 //
 // `splits`: with a workspace, few tiles share K between up to 16 workgroups each
 // (not more than one of them per CU), whose sums a second launch adds: 3.4 us more
-// and 0.535 us per MB of sums (fitted likewise).  512 tokens x 9216, K = 36864 104
-// us in 3 parts and 167 without; 128 x 9216 45 and 67; 256 x 5120, K = 20480 31
-// and 38; 64 x 5120 17.4 and 22.1; where it would not pay it is not picked (128 x
+// and 0.535 us per MB of sums (fitted likewise).  512 tokens x 9216, K = 36864 120
+// us in 3 parts and 156 without; 128 x 9216 47 and 68; 256 x 5120, K = 20480 32
+// and 39; 64 x 5120 17.2 and 22.1; where it would not pay it is not picked (128 x
 // 4096, K = 4096 7.9 and, in 2 parts, 10.7).
 struct Mx4Tile {
   int bn, bm, threads;

@@ -166,7 +166,7 @@ def test_linear_plans():
     assert plan(8, 20480, 5120) == "decode 32 rows"
     assert plan(64, 20480, 5120) == plan(64, 20480, 5120, True) == "tiles 128x64"
     assert plan(65, 64, 32) == "tiles 64x64"
-    assert plan(512, 9216, 36864) == "tiles 128x128"
+    assert plan(512, 9216, 36864) == "tiles 192x128"
     assert plan(512, 9216, 36864, True) == "tiles 256x256 split-K 3"
     # the most tokens and channels: fewer than 2^32 work-items
     for M, N in (((1 << 31) - 256, 16), (1 << 24, 30000), (1 << 30, 256), (65, (1 << 26) - 1)):

@@ -185,6 +185,117 @@ def test_moe_nan_blocks_stay_with_their_tokens_and_experts():
     assert bool(Y[dev(bad)].isnan().all()) and torch.equal(Y[dev(~bad)], clean[dev(~bad)])
 
 
+# --- the largest sizes: element numbers past 32 bits --------------------------------
+
+def random_mx4(rows, K, seed):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    c = torch.randint(0, 256, (rows, K // 2), dtype=torch.uint8, device="cuda", generator=g)
+    e = torch.randint(122, 127, ((K + 255) // 256, rows, 8), dtype=torch.uint8, device="cuda", generator=g)
+    if K % 256:
+        e[-1, :, K % 256 // 32:] = 0
+    return c, e
+
+
+@pytest.mark.parametrize("M", [1, 20, 65])
+def test_linear_of_the_most_channels(M):
+    N, K = (1 << 26) - 1, 32
+    w, x = random_mx4(N, K, 1), random_mx4(M, K, 2)
+    bias = torch.randn(N, device="cuda")
+    Wp = ot.pack_weights_mx4(*w)
+    Y = ot.qlinear_mx4(*x, Wp, N, bias, True)
+    some = np.unique(np.r_[0:40, N // 2:N // 2 + 40, (1 << 25) - 20:(1 << 25) + 20, N - 300:N])
+    at = torch.from_numpy(some).cuda()
+    y, mags = X.linear(X.values(*map(host, x)), X.values(host(w[0][at]), host(w[1][:, at])),
+                       host(bias[at]))
+    assert np.all(np.abs(host(Y[:, at]).astype(np.float64) - y) <= y_tolerance(y, mags, K))
+    del Wp, w
+    assert not bool(Y[-1].isnan().any())
+
+
+def test_linear_of_the_most_tokens():
+    """The last rows that a launch takes, whose byte numbers pass 2^35."""
+    M, N, K = (1 << 31) - 256, 1, 32
+    assert ot.ot_qlinear_mx4_plan(M, N, K) != "none"
+    w = random_mx4(N, K, 1)
+    x = (torch.empty(M, K // 2, dtype=torch.uint8, device="cuda"),
+         torch.zeros(1, M, 8, dtype=torch.uint8, device="cuda"))
+    some = np.unique(np.r_[0:300, (1 << 30) - 200:(1 << 30) + 200, M - 600:M])
+    at = torch.from_numpy(some).cuda()
+    part = random_mx4(some.size, K, 3)
+    x[0][at], x[1][:, at] = part
+    bias = torch.randn(N, device="cuda")
+    Y, y_ok = guarded(M, N, torch.float16, 512)
+    ot.ot_qlinear_mx4(*x, ot.pack_weights_mx4(*w), N, bias, Y, ot.qlinear_mx4_workspace_for(M, N, K))
+    y, mags = X.linear(X.values(*map(host, part)), X.values(*map(host, w)), host(bias))
+    assert np.all(np.abs(host(Y[at]).astype(np.float64) - y) <= y_tolerance(y, mags, K))
+    assert y_ok()
+
+
+def test_linear_of_the_longest_rows():
+    """With one scale each, of 1/2 and 1, the products are multiples of 1/8, and the
+    sums (of random signs: far below 2^21) multiples of 1/8 that fp32 holds: exact in
+    any order. What remains is the bias, half a step of fp32, and half one of fp16."""
+    N, K = 64, 1 << 22
+    for M in (3, 40, 70):
+        x, w = random_mx4(M, K, 4), random_mx4(N, K, 5)
+        x[1].fill_(126)
+        w[1].fill_(127)
+        bias = torch.randn(N, device="cuda")
+        Y = ot.qlinear_mx4(*x, ot.pack_weights_mx4(*w), N, bias, True)
+        xv, wv = (ot.dequantize_mx4(*t).double() for t in (x, w))
+        y = host(xv @ wv.t() + bias.double())
+        assert 2000 < np.abs(y).max() < 65000
+        assert np.all(np.abs(host(Y).astype(np.float64) - y) <= np.abs(y) * (2.0 ** -11 + 2.0 ** -23)
+                      + 2.0 ** -22)
+
+
+def test_quantizers_past_32_bits():
+    M, K = (1 << 27) + 5, 32  # 2^32 + 160 elements
+    part = np.r_[0:100, M // 2:M // 2 + 100, M - 100:M]
+    at = torch.from_numpy(part).cuda()
+    r = np.random.default_rng(6)
+    h, z, inv_s = draw_activations(r, part.size, K)
+    x = torch.zeros(M, K, dtype=torch.float16, device="cuda")
+    x[at] = dev(h)
+    c, e = ot.quantize_act_mx4(x, dev(z), dev(inv_s))
+    wc, we = X.to_mx4(X.activations(h, z, inv_s))
+    assert np.array_equal(host(c[at]), wc) and np.array_equal(host(e[:, at]), we)
+    wc, we, bp = X.fold(h, None, z, inv_s)
+    c, e, b = ot.fold_weights_mx4(x, None, dev(z), dev(inv_s))
+    assert np.array_equal(host(c[at]), wc) and np.array_equal(host(e[:, at]), we)
+    assert np.all(np.abs(host(b[at]) - bp) <= np.abs(bp) * 2.0 ** -23 + 1e-30)
+    del x
+    y = ot.dequantize_mx4(c, e)
+    assert np.array_equal(host(y[at]), X.values(wc, we).astype(np.float32))
+
+
+def test_moe_of_many_wide_experts():
+    """Weights whose byte numbers pass 32 bits: the last experts' are the right ones
+    (the plain form has the chosen experts alone)."""
+    M, H, F, E, k = 5, 32768, 1024, 256, 2
+    r = np.random.default_rng(7)
+    some = [0, 131, 254, 255]
+    x, small, _, b1, _, b2 = draw_moe(r, M, H, F, len(some), "relu")
+    logits = np.full((M, E), -np.inf, np.float16)
+    logits[:, some] = small
+    parts, packed = [], []
+    for rows, K in ((F, H), (H, F)):
+        c, e = random_mx4(E * rows, K, rows)
+        e[:] = 123 + (e & 1)
+        packed.append(ot.pack_weights_mx4(c, e))
+        at = torch.cat([torch.arange(i * rows, (i + 1) * rows) for i in some]).cuda()
+        parts.append((host(c[at]), host(e[:, at])))
+        del c, e
+    bias = [np.zeros((E, v.shape[1]), np.float32) for v in (b1, b2)]
+    for v, small_v in zip(bias, (b1, b2)):
+        v[some] = small_v
+    got = ot.moe_mx4(*map(dev, x), dev(logits), k, packed[0], dev(bias[0]), packed[1], dev(bias[1]),
+                     F, "relu")
+    y, tol = moe_expected(x, small, k, parts[0], b1, parts[1], b2, F, "relu")
+    assert np.median(tol) <= 0.05 * np.sqrt(np.mean(y * y))
+    assert np.all(np.abs(host(got).astype(np.float64) - y) <= tol)
+
+
 # --- one after another ----------------------------------------------------------
 
 def layer(r, N, K):

@@ -8,6 +8,7 @@
 // ot_status, or None where any argument is not exactly what it expects
 // (another type, dtype, device, layout or shape): ot.py then runs its own
 // checks, which name the fault or convert the argument.
+#include <ATen/detail/CUDAHooksInterface.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <Python.h>
@@ -23,7 +24,9 @@ PyObject *g_current_stream = nullptr;
 // One call's arguments; ok turns false at the first that does not fit.
 struct Args {
   PyObject *const *a;
+  bool here = false;  // only tensors of the current device fit
   bool ok = true;
+  int64_t device = -1;
 
   // Plain tensors (and parameters) only, by their type: an object can claim to
   // be a tensor (its __class__) without a tensor's memory, and a subclass may
@@ -32,6 +35,10 @@ struct Args {
     if (!ok || !THPVariable_CheckExact(a[i])) return fail();
     const at::Tensor &t = THPVariable_Unpack(a[i]);
     if (t.scalar_type() != type || !t.is_cuda() || !t.is_contiguous()) return fail();
+    if (here) {
+      if (device < 0) device = at::detail::getCUDAHooks().current_device();
+      if (t.get_device() != device) return fail();
+    }
     return &t;
   }
   // A matrix that defines its two sizes.
@@ -164,9 +171,9 @@ constexpr at::ScalarType kCode = at::kChar, kF32 = at::kFloat, kF16 = at::kHalf,
 
 // Runs body(args) -> ot_status; None where an argument did not fit.
 template <class Body>
-PyObject *run(PyObject *const *a, Py_ssize_t n, Py_ssize_t want, Body body) {
+PyObject *run(PyObject *const *a, Py_ssize_t n, Py_ssize_t want, Body body, bool here = false) {
   if (n != want) Py_RETURN_NONE;
-  Args args{a};
+  Args args{a, here};
   int rc = 0;
   try {
     rc = body(args);
@@ -335,7 +342,7 @@ PyObject *quantize_act_mx4(PyObject *, PyObject *const *a, Py_ssize_t n) {
     auto *e = g.mx4_scales(5, M, K);
     auto *st = g.stream(6);
     return g.call([&] { return fn(x, M, K, z, is, c, e, st); });
-  });
+  }, true);
 }
 
 // (fn, h, gamma, beta, eps, z, inv_s, Xc, Xe, stream)
@@ -352,7 +359,7 @@ PyObject *ln_quantize_act_mx4(PyObject *, PyObject *const *a, Py_ssize_t n) {
     auto *e = g.mx4_scales(8, M, K);
     auto *st = g.stream(9);
     return g.call([&] { return fn(h, M, K, ga, be, eps, z, is, c, e, st); });
-  });
+  }, true);
 }
 
 // (fn, c, e, y, stream)
@@ -365,7 +372,7 @@ PyObject *dequantize_mx4(PyObject *, PyObject *const *a, Py_ssize_t n) {
     auto *y = g.sized<float>(3, kF32, M, K);
     auto *st = g.stream(4);
     return g.call([&] { return fn(c, e, M, K, y, st); });
-  });
+  }, true);
 }
 
 using PackedFn = size_t (*)(int64_t, int64_t);
@@ -386,7 +393,7 @@ PyObject *qlinear_mx4(PyObject *, PyObject *const *a, Py_ssize_t n) {
     auto *ws = g.scratch(9, [&] { return ws_size(M, N, K); });
     auto *st = g.stream(10);
     return g.call([&] { return fn(c, e, w, b, M, N, K, y, ws, st); });
-  });
+  }, true);
 }
 
 using MoeWsFn = size_t (*)(int64_t, int64_t, int64_t, int64_t, int64_t);
@@ -415,7 +422,7 @@ PyObject *moe_mx4(PyObject *, PyObject *const *a, Py_ssize_t n) {
     auto *ws = g.scratch(14, [&] { return ws_size(M, H, F, E, k); });
     auto *st = g.stream(15);
     return g.call([&] { return fn(c, e, l, w1, b1, w2, b2, M, H, F, E, k, (int)act, y, ws, st); });
-  });
+  }, true);
 }
 
 // (fn): the function that returns the current stream's handle

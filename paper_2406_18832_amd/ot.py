@@ -646,6 +646,14 @@ def qlinear_asym(Xq, Wq, sW, zW, bprime, a_bits, w_bits, want_acc=False, workspa
 # MX4: microscaled 4-bit floating point.  A matrix [rows, K] is a pair of
 # tensors: codes [rows, K / 2] uint8 and scales [ceil(K / 256), rows, 8] uint8.
 # ---------------------------------------------------------------------------
+def _mx4_dev(t, dtype, name, shape=None):
+    """_dev, for tensors of the current device alone: the launch goes there."""
+    p = _dev(t, dtype, name, shape)
+    if p is not None and _current_device is not None and t.get_device() != _current_device():
+        raise ValueError(f"{name} must be on the current device {_current_device()}, not {t.device}")
+    return p
+
+
 def _mx4_pair(c, e, name, shape=None):
     """(rows, K, codes pointer, scales pointer) of a matrix in MX4, checked
     against the [rows, K] it should be."""
@@ -656,8 +664,8 @@ def _mx4_pair(c, e, name, shape=None):
     rows, K = shape
     if K % 32:
         raise ValueError(f"{name} must have a multiple of 32 channels, got {K}")
-    return (rows, K, _dev(c, torch.uint8, f"{name}'s codes", (rows, K // 2)),
-            _dev(e, torch.uint8, f"{name}'s scales", ((K + 255) // 256, rows, 8)))
+    return (rows, K, _mx4_dev(c, torch.uint8, f"{name}'s codes", (rows, K // 2)),
+            _mx4_dev(e, torch.uint8, f"{name}'s scales", ((K + 255) // 256, rows, 8)))
 
 
 def ot_quantize_act_mx4(x, z, inv_s, Xc, Xe, stream=None):
@@ -668,9 +676,9 @@ def ot_quantize_act_mx4(x, z, inv_s, Xc, Xe, stream=None):
         return _check(rc, "ot_quantize_act_mx4")
     M, K = x.shape
     _, _, pc, pe = _mx4_pair(Xc, Xe, "X", (M, K))
-    rc = lib().ot_quantize_act_mx4(_dev(x, torch.float16, "x"), M, K,
-                                   _dev(z, torch.float32, "z", (K,)),
-                                   _dev(inv_s, torch.float32, "inv_s", (K,)), pc, pe,
+    rc = lib().ot_quantize_act_mx4(_mx4_dev(x, torch.float16, "x"), M, K,
+                                   _mx4_dev(z, torch.float32, "z", (K,)),
+                                   _mx4_dev(inv_s, torch.float32, "inv_s", (K,)), pc, pe,
                                    _stream(stream))
     _check(rc, "ot_quantize_act_mx4")
 
@@ -683,11 +691,11 @@ def ot_ln_quantize_act_mx4(h, gamma, beta, eps, z, inv_s, Xc, Xe, stream=None):
         return _check(rc, "ot_ln_quantize_act_mx4")
     M, K = h.shape
     _, _, pc, pe = _mx4_pair(Xc, Xe, "X", (M, K))
-    rc = lib().ot_ln_quantize_act_mx4(_dev(h, torch.float16, "h"), M, K,
-                                      _dev(gamma, torch.float16, "gamma", (K,)),
-                                      _dev(beta, torch.float16, "beta", (K,)), float(eps),
-                                      _dev(z, torch.float32, "z", (K,)),
-                                      _dev(inv_s, torch.float32, "inv_s", (K,)), pc, pe,
+    rc = lib().ot_ln_quantize_act_mx4(_mx4_dev(h, torch.float16, "h"), M, K,
+                                      _mx4_dev(gamma, torch.float16, "gamma", (K,)),
+                                      _mx4_dev(beta, torch.float16, "beta", (K,)), float(eps),
+                                      _mx4_dev(z, torch.float32, "z", (K,)),
+                                      _mx4_dev(inv_s, torch.float32, "inv_s", (K,)), pc, pe,
                                       _stream(stream))
     _check(rc, "ot_ln_quantize_act_mx4")
 
@@ -697,10 +705,10 @@ def ot_fold_weights_mx4(W, b, z, s, Wc, We, bprime, stream=None):
     and scales of W diag(s), bprime [N] fp32.  Synchronous."""
     N, K = W.shape
     _, _, pc, pe = _mx4_pair(Wc, We, "W", (N, K))
-    rc = lib().ot_fold_weights_mx4(_dev(W, torch.float16, "W"), _dev(b, torch.float16, "b", (N,)),
-                                   N, K, _dev(z, torch.float32, "z", (K,)),
-                                   _dev(s, torch.float32, "s", (K,)), pc, pe,
-                                   _dev(bprime, torch.float32, "bprime", (N,)), _stream(stream))
+    rc = lib().ot_fold_weights_mx4(_mx4_dev(W, torch.float16, "W"), _mx4_dev(b, torch.float16, "b", (N,)),
+                                   N, K, _mx4_dev(z, torch.float32, "z", (K,)),
+                                   _mx4_dev(s, torch.float32, "s", (K,)), pc, pe,
+                                   _mx4_dev(bprime, torch.float32, "bprime", (N,)), _stream(stream))
     _check(rc, "ot_fold_weights_mx4")
 
 
@@ -711,7 +719,7 @@ def ot_dequantize_mx4(c, e, y, stream=None):
     if rc is not None:
         return _check(rc, "ot_dequantize_mx4")
     rows, K, pc, pe = _mx4_pair(c, e, "the matrix")
-    rc = lib().ot_dequantize_mx4(pc, pe, rows, K, _dev(y, torch.float32, "y", (rows, K)),
+    rc = lib().ot_dequantize_mx4(pc, pe, rows, K, _mx4_dev(y, torch.float32, "y", (rows, K)),
                                  _stream(stream))
     _check(rc, "ot_dequantize_mx4")
 
@@ -725,7 +733,7 @@ def ot_pack_weights_mx4(Wc, We, Wp, stream=None):
     Asynchronous."""
     N, K, pc, pe = _mx4_pair(Wc, We, "W")
     rc = lib().ot_pack_weights_mx4(pc, pe, N, K,
-                                   _dev(Wp, torch.uint8, "Wp", (ot_packed_weights_mx4_size(N, K),)),
+                                   _mx4_dev(Wp, torch.uint8, "Wp", (ot_packed_weights_mx4_size(N, K),)),
                                    _stream(stream))
     _check(rc, "ot_pack_weights_mx4")
 
@@ -747,7 +755,7 @@ def _scratch(workspace, need):
     """Device pointer of an optional workspace of at least `need` bytes."""
     if workspace is None:
         return None
-    ptr = _dev(workspace, torch.uint8, "workspace")
+    ptr = _mx4_dev(workspace, torch.uint8, "workspace")
     if workspace.numel() < need:
         raise ValueError(f"workspace holds {workspace.numel()} bytes, the call needs {need}")
     return ptr
@@ -761,9 +769,9 @@ def ot_qlinear_mx4(Xc, Xe, Wp, N, bprime, Y, workspace=None, stream=None):
         return _check(rc, "ot_qlinear_mx4")
     M, K, pc, pe = _mx4_pair(Xc, Xe, "X")
     rc = lib().ot_qlinear_mx4(pc, pe,
-                              _dev(Wp, torch.uint8, "Wp", (ot_packed_weights_mx4_size(N, K),)),
-                              _dev(bprime, torch.float32, "bprime", (N,)), M, N, K,
-                              _dev(Y, torch.float16, "Y", (M, N)),
+                              _mx4_dev(Wp, torch.uint8, "Wp", (ot_packed_weights_mx4_size(N, K),)),
+                              _mx4_dev(bprime, torch.float32, "bprime", (N,)), M, N, K,
+                              _mx4_dev(Y, torch.float16, "Y", (M, N)),
                               _scratch(workspace, ot_qlinear_mx4_workspace_size(M, N, K)),
                               _stream(stream))
     _check(rc, "ot_qlinear_mx4")
@@ -795,12 +803,12 @@ def ot_moe_mx4(Xc, Xe, logits, top_k, W1p, b1, W2p, b2, F, act, Y, workspace, st
     E, F1 = logits.shape[1], (2 if act == "swiglu" else 1) * F
     if workspace is None and M:
         raise ValueError("ot_moe_mx4 needs a workspace")
-    rc = lib().ot_moe_mx4(pc, pe, _dev(logits, torch.float16, "logits", (M, E)),
-                          _dev(W1p, torch.uint8, "W1p", (ot_packed_weights_mx4_size(E * F1, H),)),
-                          _dev(b1, torch.float32, "b1", (E, F1)),
-                          _dev(W2p, torch.uint8, "W2p", (ot_packed_weights_mx4_size(E * H, F),)),
-                          _dev(b2, torch.float32, "b2", (E, H)), M, H, F, E, int(top_k),
-                          MOE_ACTIVATIONS[act], _dev(Y, torch.float16, "Y", (M, H)),
+    rc = lib().ot_moe_mx4(pc, pe, _mx4_dev(logits, torch.float16, "logits", (M, E)),
+                          _mx4_dev(W1p, torch.uint8, "W1p", (ot_packed_weights_mx4_size(E * F1, H),)),
+                          _mx4_dev(b1, torch.float32, "b1", (E, F1)),
+                          _mx4_dev(W2p, torch.uint8, "W2p", (ot_packed_weights_mx4_size(E * H, F),)),
+                          _mx4_dev(b2, torch.float32, "b2", (E, H)), M, H, F, E, int(top_k),
+                          MOE_ACTIVATIONS[act], _mx4_dev(Y, torch.float16, "Y", (M, H)),
                           _scratch(workspace, ot_moe_mx4_workspace_size(M, H, F, E, top_k)),
                           _stream(stream))
     _check(rc, "ot_moe_mx4")

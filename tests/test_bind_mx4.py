@@ -120,3 +120,16 @@ def test_native_and_python_marshalling_agree(name, monkeypatch):
     for i, (a, b) in enumerate(zip(first, second)):
         assert _same(a, b), (i, a, b)
     assert not isinstance(first[0], tuple)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name", NAMES)
+def test_tensors_of_another_device_are_refused(name, monkeypatch):
+    """The launch goes to the current device; here that is said to be another one
+    (the native side asks the runtime itself, and leaves such calls to this check)."""
+    ot.lib()
+    call, args = _calls("cuda")[name]
+    monkeypatch.setattr(ot, "_n_" + name, ot._unbound)
+    monkeypatch.setattr(ot, "_current_device", lambda: 1)
+    with pytest.raises(ValueError, match="current device 1, not cuda:0"):
+        call(*args)

@@ -1,6 +1,7 @@
 // The MX4 linear up to 64 tokens:  Y = fp16(sum_k x w + b').
 //
-// Bound by reading the weights.  A workgroup takes 16 RB weight rows and all
+// Bound by reading the weights (MI355X: 8 tokens x 20480, K = 5120 in 11.5 us, 4.9
+// TB/s; 14336 x 28928 with 3 tokens 34 us, 6.4).  A workgroup takes 16 RB weight rows and all
 // tokens; its waves share out the K tiles and add their fp32 sums through LDS
 // in wave order (ot_mx4_stream.h).
 //

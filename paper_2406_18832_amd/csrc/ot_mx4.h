@@ -90,9 +90,9 @@ __device__ __forceinline__ uint32_t row_scales(uint32_t b, int lane) {
 // Lane l of a wave holds eight consecutive channels from k0 = 8 (64 i + l) on,
 // zeros past K: their codes and scales to row `row` of [M x K].  All 64 lanes
 // take part.  The scale byte of the lane's block.
-__device__ __forceinline__ uint32_t mx4_store8(const float (&v)[8], int64_t row, int64_t M, int64_t K,
-                                           int64_t k0, int lane, uint8_t *__restrict__ Xc,
-                                           uint8_t *__restrict__ Xe) {
+__device__ __forceinline__ uint32_t mx4_store8(const float (&v)[8], int64_t row, int64_t M,
+                                               int64_t K, int64_t k0, int lane,
+                                               uint8_t *__restrict__ Xc, uint8_t *__restrict__ Xe) {
   uint32_t most = abs_bits(v[0]);
 #pragma unroll
   for (int i = 1; i < 8; ++i) most = max(most, abs_bits(v[i]));

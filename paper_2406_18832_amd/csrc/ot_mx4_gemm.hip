@@ -1,6 +1,7 @@
-// The MX4 linear above 64 tokens, and below where it is the faster:  Y = fp16(sum_k x w + b'), both operands in
-// MX4 (ot_mx4.h), products and scales on v_mfma_scale_f32_32x32x64_f8f6f4, sums
-// in fp32.
+// The MX4 linear above 64 tokens, and below where it is the faster:
+//   Y = fp16(sum_k x w + b')
+// with both operands in MX4 (ot_mx4.h), products and scales on
+// v_mfma_scale_f32_32x32x64_f8f6f4, sums in fp32.
 //
 // The matrix instruction takes 16 bytes of codes per lane (a block of 32
 // channels) and one scale byte per lane and operand, and does twice the work of
@@ -376,11 +377,14 @@ Mx4Plan mx4_gemm_plan(int64_t M, int64_t N, int64_t K, bool with_workspace) {
     if (i > 0 && !fits(t, M, N)) continue;
     const int64_t tiles = tiles_of(t, M, N);
     for (int64_t parts = 1; parts <= kMaxParts; ++parts) {
-      if (parts > 1 && (!with_workspace || !t.splits || tiles * parts > cus || kt < 2 * parts)) break;
+      if (parts > 1 &&
+          (!with_workspace || !t.splits || tiles * parts > cus || kt < 2 * parts))
+        break;
       const int64_t bytes = parts > 1 ? tiles * parts * t.bn * t.bm * 4 : 0;
       double us = t.time.us(tiles * parts, (kt + parts - 1) / parts, cus);
       if (parts > 1) us += kJoin + kJoinPerByte * (double)bytes;
-      if ((i == 0 && parts == 1) || us < best.us) best = Mx4Plan{i, t.bn, t.bm, (int)parts, (size_t)bytes, us};
+      if ((i == 0 && parts == 1) || us < best.us)
+        best = Mx4Plan{i, t.bn, t.bm, (int)parts, (size_t)bytes, us};
     }
   }
   return best;

@@ -114,7 +114,7 @@ hipError_t launch_ln_quantize_act_mx4(const uint16_t *h, int64_t M, int64_t K,
                                       const uint16_t *gamma, const uint16_t *beta, float eps,
                                       const float *z, const float *inv_s, uint8_t *Xc, uint8_t *Xe,
                                       hipStream_t st);
-// status as for launch_fold; z and s: both or neither.
+// status as for launch_fold; z and s: either may be NULL.
 hipError_t launch_fold_mx4(const uint16_t *W, const uint16_t *b, int64_t N, int64_t K,
                            const float *z, const float *s, uint8_t *Wc, uint8_t *We,
                            float *bprime, int *status, hipStream_t st);

@@ -19,7 +19,6 @@
 namespace ot {
 namespace detail {
 
-
 template <int kByte>
 __device__ __forceinline__ v4f mfma_mx4_16(v4i a, v4i b, v4f c, uint32_t ea, uint32_t eb) {
   const v8i a8 = __builtin_shufflevector(a, a, 0, 1, 2, 3, -1, -1, -1, -1);

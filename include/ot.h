@@ -425,8 +425,10 @@ ot_status ot_quantize_act_mx4(const uint16_t *x, int64_t M, int64_t K,
  * ot_ln_quantize_act_mx4 -- the LayerNorm fused with the MX4 quantizer:
  *   v[m,k] = ((((h - fp32(mean)) * fp32(rstd)) * gamma_k + (beta_k - z_k)) * inv_s_k)
  * in fp32 rounded to nearest even (no fused multiply-add), with mean and rstd
- * as defined for ot_ln_quantize_act.  Arguments as there (K <= 65536), outputs
- * as ot_quantize_act_mx4; M < 2^22 (OT_ESHAPE).  Asynchronous on stream.
+ * as defined for ot_ln_quantize_act.  A NaN or an infinity in a row of h makes
+ * every block of that row NaN (b = 255), and so do equal values with eps == 0.
+ * Arguments as there otherwise (K <= 65536), outputs as ot_quantize_act_mx4;
+ * M < 2^22 (OT_ESHAPE).  Asynchronous on stream.
  */
 ot_status ot_ln_quantize_act_mx4(const uint16_t *h, int64_t M, int64_t K,
                                  const uint16_t *gamma, const uint16_t *beta,

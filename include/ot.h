@@ -493,8 +493,15 @@ ot_status ot_qlinear_mx4(const uint8_t *Xc, const uint8_t *Xe, const uint8_t *Wp
                          const float *bprime, int64_t M, int64_t N, int64_t K,
                          uint16_t *Y, void *workspace, void *stream);
 /* Bytes of optional scratch that ot_qlinear_mx4 can use for these sizes on the
- * current device (0 if none, and for sizes it rejects).  No device work. */
+ * current device (0 if none, and for sizes it rejects).  No device work.
+ * They are of these sizes alone: more tokens may use fewer bytes, or none, so a
+ * buffer sized for the largest batch can be too small for a smaller one, and the
+ * call, which is not told a size, would write past it. */
 size_t ot_qlinear_mx4_workspace_size(int64_t M, int64_t N, int64_t K);
+/* The most that ot_qlinear_mx4_workspace_size gives for 1 to M tokens: the size
+ * of one buffer for calls of any of them (0 for sizes it rejects).  Host work of
+ * up to a millisecond; no device work. */
+size_t ot_qlinear_mx4_workspace_max(int64_t M, int64_t N, int64_t K);
 
 /*
  * ot_qlinear_mx4_plan -- which kernel configuration ot_qlinear_mx4 launches for

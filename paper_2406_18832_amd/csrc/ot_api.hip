@@ -487,6 +487,11 @@ size_t ot_qlinear_mx4_workspace_size(int64_t M, int64_t N, int64_t K) {
   return ot::mx4_linear_workspace_bytes(M, N, K);
 }
 
+size_t ot_qlinear_mx4_workspace_max(int64_t M, int64_t N, int64_t K) {
+  if (M <= 0 || !mx4_linear_ok(M, N, K)) return 0;
+  return ot::mx4_linear_workspace_max(M, N, K);
+}
+
 ot_status ot_qlinear_mx4_plan(int64_t M, int64_t N, int64_t K, int with_workspace, char *buf,
                               size_t len) {
   if (!buf || len == 0 || M < 0 || N < 0 || K < 0) return OT_EINVAL;

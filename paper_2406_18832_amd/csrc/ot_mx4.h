@@ -146,6 +146,8 @@ hipError_t launch_mx4_gemm(const Mx4Plan &plan, const uint8_t *Xc, const uint8_t
                            const uint8_t *Wp, const float *bp, int64_t M, int64_t N, int64_t K,
                            uint16_t *Y, void *ws, hipStream_t st);
 bool mx4_gemm_fits(int64_t M, int64_t N);  // whether some tile's grid does
+// Whether a launch of these sizes, or of more tokens, can share K at all.
+bool mx4_gemm_may_share(int64_t M, int64_t N, int64_t K);
 
 // The product: up to 64 tokens mostly by streaming the weights
 // (ot_mx4_decode.hip), else on tiles.  ws: NULL or mx4_linear_workspace_bytes.
@@ -153,6 +155,7 @@ hipError_t launch_mx4_linear(const uint8_t *Xc, const uint8_t *Xe, const uint8_t
                              const float *bp, int64_t M, int64_t N, int64_t K, uint16_t *Y,
                              void *ws, hipStream_t st);
 size_t mx4_linear_workspace_bytes(int64_t M, int64_t N, int64_t K);
+size_t mx4_linear_workspace_max(int64_t M, int64_t N, int64_t K);
 void describe_mx4_linear(int64_t M, int64_t N, int64_t K, bool with_workspace, char *buf,
                          size_t len);
 // A mixture-of-experts layer; workspace of at least moe_mx4_workspace_bytes.

@@ -252,6 +252,18 @@ size_t mx4_linear_workspace_bytes(int64_t M, int64_t N, int64_t K) {
   return plan.rows ? 0 : plan.tiles.bytes;
 }
 
+// The most that any call of 1 to M tokens uses: a plan is the same for all tokens
+// of one count of 64-row tiles, and for 17 to 32.
+size_t mx4_linear_workspace_max(int64_t M, int64_t N, int64_t K) {
+  size_t most = 0;
+  for (int64_t m = 32; mx4_gemm_may_share(m < M ? m : M, N, K); m += m < 64 ? 32 : 64) {
+    const size_t bytes = mx4_linear_workspace_bytes(m < M ? m : M, N, K);
+    if (bytes > most) most = bytes;
+    if (m >= M) break;
+  }
+  return most;
+}
+
 void describe_mx4_linear(int64_t M, int64_t N, int64_t K, bool with_workspace, char *buf,
                          size_t len) {
   const LinearPlan plan = linear_plan(M, N, K, with_workspace);

@@ -369,6 +369,10 @@ using namespace detail;
 
 bool mx4_gemm_fits(int64_t M, int64_t N) { return fits(kTiles[0], M, N); }
 
+bool mx4_gemm_may_share(int64_t M, int64_t N, int64_t K) {
+  return 2 * tiles_of(kTiles[0], M, N) <= device_cus() && mx4_tiles(K) >= 4;
+}
+
 Mx4Plan mx4_gemm_plan(int64_t M, int64_t N, int64_t K, bool with_workspace) {
   const int64_t cus = device_cus(), kt = mx4_tiles(K);
   Mx4Plan best{};

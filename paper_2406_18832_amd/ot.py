@@ -168,6 +168,8 @@ def lib() -> ctypes.CDLL:
         L.ot_qlinear_mx4.argtypes = [vp, vp, vp, vp, i64, i64, i64, vp, vp, vp]
         L.ot_qlinear_mx4_workspace_size.restype = ctypes.c_size_t
         L.ot_qlinear_mx4_workspace_size.argtypes = [i64, i64, i64]
+        L.ot_qlinear_mx4_workspace_max.restype = ctypes.c_size_t
+        L.ot_qlinear_mx4_workspace_max.argtypes = [i64, i64, i64]
         L.ot_qlinear_mx4_plan.restype = c_int
         L.ot_qlinear_mx4_plan.argtypes = [i64, i64, i64, c_int, ctypes.c_char_p, ctypes.c_size_t]
         L.ot_moe_mx4.restype = c_int
@@ -742,6 +744,11 @@ def ot_qlinear_mx4_workspace_size(M: int, N: int, K: int) -> int:
     return int(lib().ot_qlinear_mx4_workspace_size(M, N, K))
 
 
+def ot_qlinear_mx4_workspace_max(M: int, N: int, K: int) -> int:
+    """The most bytes that any call of 1 to M tokens uses."""
+    return int(lib().ot_qlinear_mx4_workspace_max(M, N, K))
+
+
 def ot_qlinear_mx4_plan(M: int, N: int, K: int, with_workspace=False) -> str:
     """The kernel configuration ot_qlinear_mx4 launches for these sizes on the
     current device (text; no device work)."""
@@ -855,10 +862,11 @@ def pack_weights_mx4(Wc, We):
     return Wp
 
 
-def qlinear_mx4_workspace_for(M: int, N: int, K: int, device=None):
+def qlinear_mx4_workspace_for(M: int, N: int, K: int, device=None, up_to=False):
     """A scratch buffer for ot_qlinear_mx4 at these sizes, or None when it uses
-    none."""
-    n = ot_qlinear_mx4_workspace_size(M, N, K)
+    none.  up_to: for batches of any number of tokens up to M (more tokens may need
+    less, so the buffer of the largest batch alone can be too small for others)."""
+    n = (ot_qlinear_mx4_workspace_max if up_to else ot_qlinear_mx4_workspace_size)(M, N, K)
     return torch.empty(n, dtype=torch.uint8, device=device or "cuda") if n else None
 
 

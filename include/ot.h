@@ -409,7 +409,8 @@ ot_status ot_qlinear_packed(const int8_t *Xq, const int8_t *Wp, const float *sW,
  * with outliers does not take its block's other channels' resolution.
  *
  * For all mx4 entry points: 32 <= K <= 2^22, K % 32 == 0 (OT_ESHAPE), rows
- * below 2^31, pointers 16-byte aligned (OT_EINVAL).
+ * below 2^31, pointers 16-byte aligned (ot_fold_weights_mx4's b and bprime: to
+ * their elements; OT_EINVAL).
  *
  * ot_quantize_act_mx4 -- runtime activations:
  *   v[m,k] = fp32(fp32(fp32(x[m,k]) - z_k) * inv_s_k), each rounded to nearest

@@ -435,6 +435,9 @@ ot_status ot_fold_weights_mx4(const uint16_t *W, const uint16_t *b, int64_t N, i
   if (!W || !Wc || !We || !bprime) return OT_EINVAL;
   if (!aligned16(W) || !aligned16(z) || !aligned16(s) || !aligned16(Wc) || !aligned16(We))
     return OT_EINVAL;
+  // b and b' go by single elements
+  if (reinterpret_cast<uintptr_t>(b) % sizeof(*b) || reinterpret_cast<uintptr_t>(bprime) % sizeof(*bprime))
+    return OT_EINVAL;
   hipStream_t st = static_cast<hipStream_t>(stream);
   StatusWord status(st);
   const hipError_t e = ot::launch_fold_mx4(W, b, N, K, z, s, Wc, We, bprime, status.word(), st);

@@ -75,18 +75,20 @@ def errors(Y, ref):
 
 
 def sweep(workloads=("opt6.7b_w8a8", "opt13b_w6a6", "opt66b_w8a8"), rows=256, calib_rows=None,
-          calib_batches=None, configs=CONFIGS + MX4_CONFIGS, device="cuda", log=None):
+          calib_batches=None, configs=None, device="cuda", log=None):
     """Errors of every configuration on every linear of the given workloads
-    (calibration: the workload's own batches unless given).  Returns a list
-    of dicts (workload, layer, config, a_bits, w_bits, path, rel_fro,
-    mean_abs, max_abs)."""
+    (calibration: the workload's own batches unless given).  Configurations:
+    CONFIGS, and MX4_CONFIGS where the linear's channels are whole blocks of 32,
+    unless given.  Returns a list of dicts (workload, layer, config, a_bits,
+    w_bits, path, rel_fro, mean_abs, max_abs)."""
     out = []
     for name in workloads:
         wl = synth.WORKLOADS[name]
         for li, lay in enumerate(wl.layers):
             X, W, b, minmax = layer_inputs(wl, li, rows, calib_rows, calib_batches, device)
             ref = torch.matmul(X.double(), W.double().t()) + b.double()
-            for label, a_bits, w_bits, path in configs:
+            mx4 = MX4_CONFIGS if X.shape[1] % 32 == 0 else []
+            for label, a_bits, w_bits, path in CONFIGS + mx4 if configs is None else configs:
                 Y = run_config(X, W, b, minmax, a_bits, w_bits, path)
                 rec = dict(workload=name, layer=lay.name, config=label, a_bits=a_bits,
                            w_bits=w_bits, path=path, **errors(Y, ref))

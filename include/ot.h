@@ -478,16 +478,18 @@ ot_status ot_pack_weights_mx4(const uint8_t *Wc, const uint8_t *We, int64_t N,
  * ot_qlinear_mx4 -- the linear on MX4 operands:
  *   Y[m,n] = fp16(fp32(sum_k x[m,k] w[n,k]) + bprime_n)
  * with the values that the codes stand for; their products are exact, the sum
- * is in fp32 (its order is fixed for given sizes, with or without a workspace,
- * and unspecified).
+ * is in fp32.  Its order is unspecified, but fixed for given sizes on one kind
+ * of device: the same call gives the same bits.  With a workspace the order is
+ * another one than without, where the call uses it (ot_qlinear_mx4_plan tells).
+ * Partial sums past fp32's largest value give an infinity or a NaN.
  *   Xc, Xe [M x K] and Wp of ot_pack_weights_mx4 for N x K, bprime [N] fp32
  *   (device).  M >= 0 (0 is a no-op), 1 <= N < 2^26 and
  *   ceil(M/256) ceil(N/256) < 2^23 (OT_ESHAPE).
  *   Y  [M x N] fp16 output (device).
  *   workspace  NULL, or at least ot_qlinear_mx4_workspace_size(M, N, K) bytes of
- *           scratch as for ot_qlinear, with which few tokens on a long K are
- *           faster (K is shared between workgroups).  Calls that overlap in time
- *           must not share one.
+ *           scratch as for ot_qlinear, with which few tokens (from 17 on) on a
+ *           long K are faster (K is shared between workgroups); up to 16 tokens
+ *           none is used.  Calls that overlap in time must not share one.
  * Asynchronous on stream; no synchronization, no allocation.
  */
 ot_status ot_qlinear_mx4(const uint8_t *Xc, const uint8_t *Xe, const uint8_t *Wp,

@@ -519,15 +519,18 @@ ot_status ot_qlinear_mx4_plan(int64_t M, int64_t N, int64_t K, int with_workspac
 
 /*
  * ot_moe_mx4 -- a whole mixture-of-experts layer for a few tokens on packed MX4
- * weights (a decode step; larger batches run an expert's linears through
- * ot_qlinear_mx4).  For token m, with its top_k largest logits (the lower expert
+ * weights (a decode step).  An expert's rows of W1p and W2p are no packed weights
+ * by themselves, since the scales of all experts lie behind all codes: larger
+ * batches through ot_qlinear_mx4 need each expert's linears packed apart, as
+ * copies of their own.  For token m, with its top_k largest logits (the lower expert
  * first among equals) and p the softmax over them,
  *   g_j  = W1_e x_m + b1_e             for its j-th expert e, in fp32
  *   h_j  = max(g_j, 0)                 OT_MOE_RELU, F1 = F
  *          silu(g_j[0..F)) g_j[F..2F)  OT_MOE_SWIGLU, F1 = 2F; silu(v) = v / (1 + e^-v)
  *   Y[m] = fp16(sum_j p_j (W2_e q(h_j) + b2_e)),  q: the values of h_j in MX4
  * A logit of -inf or NaN is never chosen: such a token takes fewer experts, and
- * one with no other logit gets Y = 0.
+ * one with no other logit gets Y = 0.  A NaN that the router should not have
+ * made is therefore not seen in Y; a caller who wants to know looks at the logits.
  *   Xc, Xe [M x H] in MX4; logits [M x E] fp16 (device).
  *   W1p  packed weights of all experts' fc1 as one matrix [E F1 x H] (an
  *        expert's rows together; the gate's rows before the others).

@@ -521,15 +521,16 @@ __global__ __launch_bounds__(256) void moe_mx4_join_kernel(const float *__restri
 // workgroup, each wave at least two K tiles (counting one step of tokens per
 // expert).  On MI355X, whole layers with and without: 20 tokens, H = 768, 43 experts
 // of 9728 41 and 68 us; 57, 512, 13 of 9696 (top 7) 39 and 87; one token, 864, 9
-// gated of 12448 (top 6) 38 and 48; 18, 768, 12 gated of 2496 (three parts) 18.5 and
-// 21.1.  Two parts save less than the third launch takes unless a wave has 16 K tiles:
-// 3 tokens, 1888, 24 gated of 7872 54 and 60; one, 512, 20 of 2048 (top 8) 16.8 and
-// 16.3; 64, 2048, 32 gated of 1408 42.0 and 41.4.
+// gated of 12448 (top 6) 38 and 48.  Two parts, weights from HBM, medians of 12 turns
+// that differ by 0.5 %: over 43 random layers 0.78 to 1.006 of the time with one, the
+// less the more K tiles a wave has; 48 tokens, 1696, 63 of 4160 (top 6) 105 and 134 us;
+// 64, 2048, 32 gated of 1408 (top 4) 37.9 and 41.6; at the least, of four to five K tiles
+// to a wave, one, 512, 20 of 2048 (top 8) 17.06 and 17.02; 3, 1792, 21 of 1952 (top 3)
+// 17.06 and 16.97.
 int moe_parts(int64_t M, int64_t H, int64_t F, int64_t E, int64_t top_k) {
   const int64_t slots = M * top_k, steps = (E < slots ? E : slots) * mx4_tiles(F);
   int64_t parts = device_cus() / (H / 16);
   if (parts > steps / (2 * kMoeWaves2)) parts = steps / (2 * kMoeWaves2);
-  if (parts == 2 && steps < 16 * kMoeWaves2) return 1;
   return parts < 2 ? 1 : (int)parts;
 }
 

@@ -5,7 +5,7 @@ import torch
 
 from oracle import mx4_oracle as X
 from paper_2406_18832_amd import ot
-from tests.test_gpu_mx4 import dev, draw_mx4, host, y_tolerance
+from tests.test_gpu_mx4 import dev, draw_moe, draw_mx4, host, moe_expected, run_moe, y_tolerance
 
 
 def test_one_workspace_for_all_batches_up_to_the_largest():
@@ -47,6 +47,30 @@ def test_moe_workspace_grows_with_the_tokens():
         k = int(r.integers(1, min(E, 16) + 1))
         sizes = [ot.ot_moe_mx4_workspace_size(M, H, F, E, k) for M in range(1, 65)]
         assert all(a <= b for a, b in zip(sizes, sizes[1:])), (H, F, E, k)
+
+
+TWO_PARTS = (17, 1600, 704, 24, 3)  # 100 workgroups of 16 channels, 72 K tiles
+
+
+def test_moe_shares_its_second_linear_between_two_workgroups():
+    """Where that fills the CUs (256 without a GPU) and leaves each wave two K tiles:
+    the workspace has two fp32 sums of every output behind the hidden values."""
+    for M, H, F, E, k in (TWO_PARTS, (64, 2048, 1408, 32, 4), (1, 512, 2048, 20, 8)):
+        hidden = E * -(-M // 16) * -(-F // 256) * 2048 * 9 // 8
+        slots = 2 * (-(-M * k * 4 // 16) * 16)
+        assert ot.ot_moe_mx4_workspace_size(M, H, F, E, k) == hidden + slots + 2 * M * H * 4
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("act", ["relu", "swiglu"])
+def test_moe_of_two_parts(act):
+    M, H, F, E, k = TWO_PARTS
+    r = np.random.default_rng(7)
+    x, logits, w1, b1, w2, b2 = draw_moe(r, M, H, F, E, act)
+    y, tol = moe_expected(x, logits, k, w1, b1, w2, b2, F, act)
+    assert np.median(tol) <= 0.05 * np.sqrt(np.mean(y * y))
+    got = host(run_moe(x, logits, k, w1, b1, w2, b2, F, act)).astype(np.float64)
+    assert np.all(np.abs(got - y) <= tol)
 
 
 @pytest.mark.gpu

@@ -203,16 +203,6 @@ __global__ __launch_bounds__(MAXT) void ln_quantize_kernel(
       s1 += red[0][w][r];
       s2 += red[1][w][r];
     }
-    if constexpr (MX4) {
-      // A NaN or an infinity in the row (finite fp16 values have a finite sum of
-      // squares): the LayerNorm of such a row is NaN, and so is each of its blocks.
-      // The exact sums below know finite values only.
-      if (!(s2 < __builtin_inf())) {
-        mu32[r] = r32[r] = __builtin_nanf("");
-        exact[r] = false;
-        continue;
-      }
-    }
     // the fast path only has to land within the bound below of the exact
     // procedure, so it takes the cheap operations: products with a rounded
     // 1/K and a refined reciprocal square root
@@ -236,6 +226,10 @@ __global__ __launch_bounds__(MAXT) void ln_quantize_kernel(
     const double e_rstd = rstd * (0.55 * (e_var * rstd * rstd + 3.0 * kU) + 20.0 * kU);
     exact[r] = row0 + r < M &&
                (near_fp32_boundary(mean, e_mean) || near_fp32_boundary(rstd, e_rstd));
+    // A NaN or an infinity in the row (finite fp16 values have a finite sum of
+    // squares) leaves none of s1, the mean and any h - mean finite, and so each
+    // block of the row NaN.  The exact sums know finite values only.
+    if constexpr (MX4) exact[r] = exact[r] && s2 < __builtin_inf();
     any_exact |= exact[r];
   }
 

@@ -129,10 +129,12 @@ __device__ inline u128 wave_sum_u128(u128 v) {
 }
 
 // MX4 false: int8 codes in Xq.  MX4 true: u = y * inv_s_k in blocks of 32, codes
-// and scales in Xq and Xe (qa unused).  On MI355X the MX4 form takes 2-17 % more than
-// the int8 one over 25 shapes, most on short launches (2048 x 7168 18.1 and 17.5 us,
-// 8192 x 7168 51.1 and 45.6, 8 x 5120 4.9 and 3.9), and the rules on sizes below pick
-// its fastest variant or one within 6 % as well.
+// and scales in Xq and Xe (qa unused).  On MI355X the MX4 form takes 4-25 % more than
+// the int8 one, most on short launches (kernel trace, input in the last-level cache,
+// and where it differs evicted from it: 2048 x 7168 20.4 and 18.7 us, evicted 21.8 and
+// 21.0; 8192 x 7168 52.5 and 46.1, evicted 56.8 and 50.9; 8 x 5120 5.3 and 4.3), and
+// over 25 shapes the rules on sizes below pick its fastest variant or one within 6 %
+// as well.
 template <int CPT, int R, int MAXT, bool MX4>
 __global__ __launch_bounds__(MAXT) void ln_quantize_kernel(
     const uint16_t *__restrict__ h, int64_t M, int K, const uint16_t *__restrict__ gamma,

@@ -87,8 +87,10 @@ struct MoeKeys {
 //   scales [e G + g][T][64 lanes][4 bytes]  (bytes 0 and 2: instructions 0 and 1)
 // as v_mfma_scale_f32_16x16x128_f8f6f4 takes them (ot_mx4_stream.h), so that the
 // other kernel's loads are whole KiB.  Row by row, those loads (32 bytes from each
-// of 16 rows) took longer than its weights'.  Most of it is never touched; it is
-// M / 2H of the experts' weights at most.
+// of 16 rows) took longer than its weights'.  Most of it is never touched.  It is
+// 2304 G T bytes an expert: for F a multiple of 256 8.5 G / H of the weights of ReLU
+// experts (0.2 % of them at H = 4096 and up to 16 tokens) and two thirds of that of
+// gated ones, else more.
 struct MoeWs {
   uint8_t *codes, *scales;
   int *expert;              // [M top_k], -1: none
@@ -331,8 +333,8 @@ __global__ __launch_bounds__(64 * kMoeWaves1, 2) void moe_mx4_hidden_kernel(MoeA
 }
 
 // MB column blocks of 16 tokens to a step (an expert's further tokens are steps
-// of their own, which read its weights again).  MI355X, as above: 16.6 us (4.3 TB/s)
-// and 17.5 (2.8 TB/s, 128 workgroups).
+// of their own, which read its weights again).  MI355X, as above: 15.9 us (4.5 TB/s),
+// and 14.8 in two parts of 128 workgroups (3.3 TB/s), whose sums take 4.5 more.
 template <int MB>
 __global__ __launch_bounds__(64 * kMoeWaves2) void moe_mx4_out_kernel(MoeArgs a) {
   // LDS: the waves' sums and the biases' [waves + 1][M][16], the slots' weights and experts, each

@@ -186,7 +186,9 @@ __global__ __launch_bounds__(64 * kWaves) void dequantize_mx4_kernel(
 }
 
 // Row-major codes and scales to the packed layout: one 16-byte block of codes
-// or one word of scales per thread.
+// or one word of scales per thread; a wave reads 16 bytes from each of 32 rows and
+// writes 1 KiB.  MI355X: 20480 x 5120 17.8 us (111 MB in and out, in the last-level
+// cache: 6.3 TB/s), 9216 x 36864 81 us (361 MB: 4.5 TB/s).
 __global__ __launch_bounds__(256) void pack_weights_mx4_kernel(
     const uint8_t *__restrict__ Wc, const uint8_t *__restrict__ We, int64_t N, int64_t K,
     int64_t blocks, int64_t tiles, uint8_t *__restrict__ Wp) {

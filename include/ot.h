@@ -560,6 +560,130 @@ ot_status ot_moe_mx4(const uint8_t *Xc, const uint8_t *Xe,
 size_t ot_moe_mx4_workspace_size(int64_t M, int64_t H, int64_t F, int64_t E,
                                  int64_t top_k);
 
+/*
+ * KV8: a key/value cache in 8 bits, for the attention between the quantized qkv and
+ * out linears.
+ *
+ * The cache is a pool of pages, each of OT_KV8_PAGE tokens of one sequence, for all
+ * H key heads.  A page of a head holds one byte per value, b, worth (b - 128) s with
+ * the page and head's fp32 scale s, for keys and for values apart:
+ *   Kc  [num_pages x H x 64 x Dp] uint8     Ks  [num_pages x H] fp32
+ *   Vc  [num_pages x H x Dp x 64] uint8     Vs  [num_pages x H] fp32
+ * with Dp = ot_kv8_row_size(D): D rounded up to 64, 96, 128, 192 or 256.  Bytes past D
+ * and past a page's tokens are unspecified and never seen.
+ *
+ * A batch is B sequences of a call's T rows and a page table:
+ *   cu      [B + 1] int32: rows cu[b] .. cu[b+1] - 1 are sequence b's, in order (none
+ *           where they are equal).  Rows from cu[B] on are padding: they are neither
+ *           read nor written.
+ *   kv_len  [B] int32: tokens that sequence b has once the call's are in the cache.
+ *           Its n = cu[b+1] - cu[b] rows are its last n tokens, positions
+ *           kv_len[b] - n .. kv_len[b] - 1.
+ *   table   [B x max_pages] int32: token j of sequence b is in page
+ *           table[b][j / 64], place j mod 64.  Entries past its tokens are not read.
+ * All of them are in device memory, so that a captured graph can be replayed with
+ * others.  They are not checked on the host; no value of them makes a call read or
+ * write outside its tensors: what ot_kv8_append says of a page that is not in
+ * 0 .. num_pages - 1, and what the others say, holds for positions past the table
+ * (max_pages) too.  A cu that falls, or exceeds T, gives unspecified rows.
+ *
+ * For all kv8 entry points: 16 <= D <= 256, D % 16 == 0; 1 <= H <= 1024;
+ * 0 <= B <= 65535; 0 <= T <= 2^24; 1 <= max_pages <= 2^24; 1 <= num_pages < 2^31
+ * (OT_ESHAPE, as for calls too large for a launch).  B == 0 or T == 0 is a no-op.
+ * fp16 tensors and codes 16-byte aligned, the others to their elements (OT_EINVAL).
+ *
+ * ot_kv8_row_size -- Dp (0 for a D that the calls reject).
+ *
+ * ot_kv8_append -- quantizes new tokens into their pages.  Per page and head, for keys
+ * and for values apart, with a the largest magnitude of the call's tokens in it:
+ *   s    = fp32(a / 127)   if the sequence has no earlier token in the page, or the
+ *                          page's scale is 0
+ *   s    = s_old 2^k       else, k >= 0 the least with a <= fp32(127.5 s_old) 2^k; where
+ *                          k > 0 the earlier tokens' codes c become rne(c 2^-k)
+ *   code = clip(rne(fp32(x fp32(1 / s))), -127, 127)   (0 where s is 0)
+ * A token's error is at most s / 2 when written and below s ever after.  A NaN or an
+ * infinity makes s, and with it all of the head's keys (or values) in the page, NaN
+ * until a sequence begins the page anew.
+ *   k, v   [T x H x D] fp16, token rows ldk and ldv elements apart (>= H D, multiples
+ *          of 8: a qkv linear's output serves as it is).
+ * Tokens of a page that the pool does not have (and of a position below 0) are left
+ * out.  Two sequences of one call must not write to one page (pages of a shared prefix
+ * are full ones, which are only read).  A call with the same tokens again changes
+ * nothing.  Asynchronous on stream.
+ */
+#define OT_KV8_PAGE 64
+int64_t ot_kv8_row_size(int64_t D);
+ot_status ot_kv8_append(const uint16_t *k, int64_t ldk, const uint16_t *v,
+                        int64_t ldv, int64_t T, int64_t B, int64_t H, int64_t D,
+                        const int32_t *cu, const int32_t *kv_len,
+                        const int32_t *table, int64_t max_pages,
+                        int64_t num_pages, uint8_t *Kc, uint8_t *Vc, float *Ks,
+                        float *Vs, void *stream);
+
+/*
+ * ot_kv8_read -- tokens of the cache as fp16(fp32(code s)), dense: rows cu[b] ..
+ * cu[b+1] - 1 of k and v receive sequence b's tokens from position start[b] ([B]
+ * int32) on.  Rows of a page that the pool does not have, and of positions below 0,
+ * are NaN.
+ *   k, v   [T x H x D] fp16 outputs (device).
+ * Asynchronous on stream.
+ */
+ot_status ot_kv8_read(const uint8_t *Kc, const uint8_t *Vc, const float *Ks,
+                      const float *Vs, int64_t num_pages, const int32_t *cu,
+                      const int32_t *start, const int32_t *table,
+                      int64_t max_pages, int64_t T, int64_t B, int64_t H,
+                      int64_t D, uint16_t *k, uint16_t *v, void *stream);
+
+/*
+ * ot_attn_kv8 -- attention over the cache.  Query row i of sequence b (with
+ * n = cu[b+1] - cu[b] of them) stands at position p = kv_len[b] - n + i; head g of Hq
+ * goes with key head g / (Hq / Hkv).  With K_j and V_j the values that codes stand for,
+ *   x_j = scale q . K_j     for j < kv_len[b], where causal != 0 only j <= p, and where
+ *                           window > 0 (causal calls) only j > p - window
+ *   Y   = sum_j e^x_j V_j / sum_j e^x_j,    lse = log sum_j e^x_j
+ * A row without a key gets Y = 0 and lse = -inf.  Products are exact, sums and the
+ * softmax's statistics in fp32; its weights are rounded to fp16 for the second product,
+ * whose sum is in fp32, and Y once at the end.  Keys behind the mask are never seen,
+ * also where they are NaN.  A NaN that a row sees, among keys or values, makes its Y and
+ * its lse NaN; a page that the pool does not have counts as NaN, and a kv_len past the
+ * table makes all of its sequence's rows NaN.
+ *   q      [T x Hq x D] fp16, rows ldq elements apart (>= Hq D, a multiple of 8).
+ *   Hq     1 .. 16384, a multiple of Hkv.
+ *   scale  finite.   window  >= 0; 0: all keys (OT_EINVAL for others, and for a window
+ *          without causal).
+ *   max_q  1 .. T: no sequence has more rows than this (1 for decode).  Up to 32 rows to
+ *          a key head (max_q Hq / Hkv) a kernel for few rows runs, which reads the cache
+ *          at memory speed; rows of a sequence past max_q may be left as they were.
+ *   Y      [T x Hq x D] fp16 output, lse [T x Hq] fp32 output or NULL (device).
+ *   workspace  NULL, or at least ot_attn_kv8_workspace_size(T, B, Hq, Hkv, D, max_q)
+ *          bytes of 16-byte aligned scratch (device), with which a sequence's keys are
+ *          shared between workgroups.  It needs no initialization; calls that overlap in
+ *          time must not share one.
+ * The order of the sums is fixed by the sizes, the lengths and whether there is a
+ * workspace: the same call gives the same bits.  Asynchronous on stream; no
+ * synchronization, no allocation.
+ */
+ot_status ot_attn_kv8(const uint16_t *q, int64_t ldq, int64_t T, int64_t B,
+                      int64_t Hq, int64_t Hkv, int64_t D, const int32_t *cu,
+                      const int32_t *kv_len, const int32_t *table,
+                      int64_t max_pages, int64_t num_pages, const uint8_t *Kc,
+                      const uint8_t *Vc, const float *Ks, const float *Vs,
+                      float scale, int causal, int64_t window, int64_t max_q,
+                      uint16_t *Y, float *lse, void *workspace, void *stream);
+/* Bytes of optional scratch that ot_attn_kv8 can use for these sizes on the current
+ * device (0 if none, and for sizes it rejects).  No device work. */
+size_t ot_attn_kv8_workspace_size(int64_t T, int64_t B, int64_t Hq, int64_t Hkv,
+                                  int64_t D, int64_t max_q);
+/*
+ * ot_attn_kv8_plan -- which kernel configuration ot_attn_kv8 launches for these sizes
+ * on the current device, as ot_qlinear_plan: "none" (T or B == 0), "few <rows> rows"
+ * (16 or 32 at a time), with ", <items> items" where keys are shared between
+ * workgroups, or "tiles <rows>".
+ */
+ot_status ot_attn_kv8_plan(int64_t T, int64_t B, int64_t Hq, int64_t Hkv,
+                           int64_t D, int64_t max_q, int with_workspace,
+                           char *buf, size_t len);
+
 #ifdef __cplusplus
 }
 #endif

@@ -9,6 +9,7 @@
 #include <mutex>
 #include <vector>
 
+#include "ot_kv8.h"
 #include "ot_mx4.h"
 
 namespace {
@@ -28,6 +29,15 @@ bool grid_ok(int64_t M, int64_t N) { return (M + 127) / 128 * ((N + 255) / 256) 
 constexpr int64_t kMaxLnMx4Rows = (int64_t(1) << 22) - 1;
 constexpr int64_t kMaxMx4N = (int64_t(1) << 26) - 1;
 bool mx4_k_ok(int64_t K) { return K >= 32 && K % 32 == 0 && K <= ot::kMx4MaxK; }
+
+// KV8: heads, sequences, tokens of a call and pages of a sequence (positions stay
+// below 2^30, rows of all query heads of a key head below 2^30).
+constexpr int64_t kMaxKv8Heads = 1024, kMaxKv8Queries = 16384, kMaxKv8Batch = 65535;
+constexpr int64_t kMaxKv8Tokens = int64_t(1) << 24, kMaxKv8Pages = int64_t(1) << 24;
+// Rows of H D elements so far apart, 16-byte aligned each; the last one's offset fits.
+bool kv8_ld_ok(int64_t ld, int64_t width) {
+  return ld >= width && ld % 8 == 0 && ld < (int64_t(1) << 32);
+}
 
 bool bits_ok(int bits) { return bits >= 2 && bits <= 8; }
 int qmax(int bits) { return (1 << (bits - 1)) - 1; }
@@ -534,6 +544,123 @@ ot_status ot_moe_mx4(const uint8_t *Xc, const uint8_t *Xe, const uint16_t *logit
   return hip_status(ot::launch_moe_mx4(Xc, Xe, logits, W1p, b1, W2p, b2, M, H, F, E, top_k,
                                        act == OT_MOE_SWIGLU, Y, workspace,
                                        static_cast<hipStream_t>(stream)));
+}
+
+// Sizes of an 8-bit cache and a batch over it.
+static bool kv8_ok(int64_t T, int64_t B, int64_t H, int64_t D, int64_t max_pages,
+                   int64_t num_pages) {
+  return D >= 16 && D <= 256 && D % 16 == 0 && H >= 1 && H <= kMaxKv8Heads && B <= kMaxKv8Batch &&
+         T <= kMaxKv8Tokens && max_pages >= 1 && max_pages <= kMaxKv8Pages && num_pages >= 1 &&
+         num_pages <= kMaxRows;
+}
+// A wave to a page, a head and keys or values fits a launch (fewer than 2^32 work-items).
+static bool kv8_pages_fit(int64_t T, int64_t B, int64_t H) {
+  return ot::kv8_page_slots(T, B) * ((2 * H + 3) / 4) * 256 < (int64_t(1) << 32);
+}
+static bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+int64_t ot_kv8_row_size(int64_t D) {
+  return D >= 16 && D <= 256 && D % 16 == 0 ? ot::kv8_width(D) : 0;
+}
+
+ot_status ot_kv8_append(const uint16_t *k, int64_t ldk, const uint16_t *v, int64_t ldv, int64_t T,
+                        int64_t B, int64_t H, int64_t D, const int32_t *cu, const int32_t *kv_len,
+                        const int32_t *table, int64_t max_pages, int64_t num_pages, uint8_t *Kc,
+                        uint8_t *Vc, float *Ks, float *Vs, void *stream) {
+  if (T < 0 || B < 0 || H < 0 || D < 0 || max_pages < 0 || num_pages < 0) return OT_EINVAL;
+  if (!kv8_ok(T, B, H, D, max_pages, num_pages) || !kv8_pages_fit(T, B, H)) return OT_ESHAPE;
+  if (T == 0 || B == 0) return OT_OK;
+  if (!kv8_ld_ok(ldk, H * D) || !kv8_ld_ok(ldv, H * D)) return OT_EINVAL;
+  if (!k || !v || !cu || !kv_len || !table || !Kc || !Vc || !Ks || !Vs) return OT_EINVAL;
+  if (!aligned16(k) || !aligned16(v) || !aligned16(Kc) || !aligned16(Vc) || !aligned4(cu) ||
+      !aligned4(kv_len) || !aligned4(table) || !aligned4(Ks) || !aligned4(Vs))
+    return OT_EINVAL;
+  const ot::Kv8Cache cache{Kc, Vc, Ks, Vs, table, max_pages, num_pages};
+  return hip_status(ot::launch_kv8_append(k, ldk, v, ldv, T, B, H, D, cu, kv_len, cache,
+                                          static_cast<hipStream_t>(stream)));
+}
+
+ot_status ot_kv8_read(const uint8_t *Kc, const uint8_t *Vc, const float *Ks, const float *Vs,
+                      int64_t num_pages, const int32_t *cu, const int32_t *start,
+                      const int32_t *table, int64_t max_pages, int64_t T, int64_t B, int64_t H,
+                      int64_t D, uint16_t *k, uint16_t *v, void *stream) {
+  if (T < 0 || B < 0 || H < 0 || D < 0 || max_pages < 0 || num_pages < 0) return OT_EINVAL;
+  if (!kv8_ok(T, B, H, D, max_pages, num_pages) || !kv8_pages_fit(T, B, H)) return OT_ESHAPE;
+  if (T == 0 || B == 0) return OT_OK;
+  if (!k || !v || !cu || !start || !table || !Kc || !Vc || !Ks || !Vs) return OT_EINVAL;
+  if (!aligned16(k) || !aligned16(v) || !aligned16(Kc) || !aligned16(Vc) || !aligned4(cu) ||
+      !aligned4(start) || !aligned4(table) || !aligned4(Ks) || !aligned4(Vs))
+    return OT_EINVAL;
+  const ot::Kv8Cache cache{const_cast<uint8_t *>(Kc), const_cast<uint8_t *>(Vc),
+                           const_cast<float *>(Ks), const_cast<float *>(Vs), table, max_pages,
+                           num_pages};
+  return hip_status(ot::launch_kv8_read(cache, H, D, cu, start, T, B, k, v,
+                                        static_cast<hipStream_t>(stream)));
+}
+
+static bool attn_kv8_ok(int64_t T, int64_t B, int64_t Hq, int64_t Hkv, int64_t D, int64_t max_pages,
+                        int64_t num_pages) {
+  return kv8_ok(T, B, Hkv, D, max_pages, num_pages) && Hq >= Hkv && Hq <= kMaxKv8Queries &&
+         Hq % Hkv == 0 && ot::attn_kv8_fits(T, B, Hq, Hkv);
+}
+
+ot_status ot_attn_kv8(const uint16_t *q, int64_t ldq, int64_t T, int64_t B, int64_t Hq, int64_t Hkv,
+                      int64_t D, const int32_t *cu, const int32_t *kv_len, const int32_t *table,
+                      int64_t max_pages, int64_t num_pages, const uint8_t *Kc, const uint8_t *Vc,
+                      const float *Ks, const float *Vs, float scale, int causal, int64_t window,
+                      int64_t max_q, uint16_t *Y, float *lse, void *workspace, void *stream) {
+  if (T < 0 || B < 0 || Hq < 0 || Hkv < 0 || D < 0 || max_pages < 0 || num_pages < 0)
+    return OT_EINVAL;
+  if (!isfinite(scale) || window < 0 || (window > 0 && !causal)) return OT_EINVAL;
+  if (!attn_kv8_ok(T, B, Hq, Hkv, D, max_pages, num_pages)) return OT_ESHAPE;
+  if (T == 0 || B == 0) return OT_OK;
+  if (max_q < 1 || max_q > T || !kv8_ld_ok(ldq, Hq * D)) return OT_EINVAL;
+  if (!q || !cu || !kv_len || !table || !Kc || !Vc || !Ks || !Vs || !Y) return OT_EINVAL;
+  if (!aligned16(q) || !aligned16(Kc) || !aligned16(Vc) || !aligned16(Y) || !aligned16(workspace) ||
+      !aligned4(cu) || !aligned4(kv_len) || !aligned4(table) || !aligned4(Ks) || !aligned4(Vs) ||
+      !aligned4(lse))
+    return OT_EINVAL;
+  ot::Kv8Attn a{};
+  a.q = q;
+  a.ldq = ldq;
+  a.T = (int)T;
+  a.B = (int)B;
+  a.Hq = (int)Hq;
+  a.Hkv = (int)Hkv;
+  a.D = (int)D;
+  a.max_q = (int)max_q;
+  a.cu = cu;
+  a.kv_len = kv_len;
+  a.cache = ot::Kv8Cache{const_cast<uint8_t *>(Kc), const_cast<uint8_t *>(Vc),
+                         const_cast<float *>(Ks), const_cast<float *>(Vs), table, max_pages,
+                         num_pages};
+  a.scale = scale;
+  a.causal = causal != 0;
+  a.window = window;
+  a.Y = Y;
+  a.lse = lse;
+  return hip_status(ot::launch_attn_kv8(a, workspace, static_cast<hipStream_t>(stream)));
+}
+
+size_t ot_attn_kv8_workspace_size(int64_t T, int64_t B, int64_t Hq, int64_t Hkv, int64_t D,
+                                  int64_t max_q) {
+  if (T <= 0 || B <= 0 || Hq <= 0 || Hkv <= 0 || max_q < 1 || max_q > T ||
+      !attn_kv8_ok(T, B, Hq, Hkv, D, 1, 1))
+    return 0;
+  return ot::attn_kv8_workspace_bytes(T, B, Hq, Hkv, D, max_q);
+}
+
+ot_status ot_attn_kv8_plan(int64_t T, int64_t B, int64_t Hq, int64_t Hkv, int64_t D, int64_t max_q,
+                           int with_workspace, char *buf, size_t len) {
+  if (!buf || len == 0 || T < 0 || B < 0 || Hq < 0 || Hkv < 0 || D < 0) return OT_EINVAL;
+  if (!attn_kv8_ok(T, B, Hq, Hkv, D, 1, 1)) return OT_ESHAPE;
+  if (T == 0 || B == 0) {
+    snprintf(buf, len, "none");
+    return OT_OK;
+  }
+  if (max_q < 1 || max_q > T) return OT_EINVAL;
+  ot::describe_attn_kv8(T, B, Hq, Hkv, D, max_q, with_workspace != 0, buf, len);
+  return OT_OK;
 }
 
 }  // extern "C"

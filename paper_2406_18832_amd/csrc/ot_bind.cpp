@@ -94,6 +94,49 @@ struct Args {
     if (ok) K *= 2;
     return p;
   }
+  // A tensor of known sizes.
+  template <class T, int N>
+  T *shaped(int i, at::ScalarType type, const int64_t (&size)[N], bool none = false) {
+    if (ok && none && a[i] == Py_None) return nullptr;
+    const at::Tensor *t = tensor(i, type);
+    if (t == nullptr || t->dim() != N) return static_cast<T *>(miss());
+    for (int d = 0; d < N; ++d)
+      if (t->size(d) != size[d]) return static_cast<T *>(miss());
+    return static_cast<T *>(t->data_ptr());
+  }
+  // fp16 rows [T][heads][D], dense by themselves and ld elements apart, that define
+  // their sizes (or have those given).
+  const uint16_t *rows3(int i, int64_t &T, int64_t &H, int64_t &D, int64_t &ld, bool given = false) {
+    if (!ok || !THPVariable_CheckExact(a[i])) return static_cast<const uint16_t *>(miss());
+    const at::Tensor &t = THPVariable_Unpack(a[i]);
+    if (t.scalar_type() != at::kHalf || !t.is_cuda() || t.dim() != 3) return static_cast<const uint16_t *>(miss());
+    if (device < 0) device = at::detail::getCUDAHooks().current_device();
+    if (t.get_device() != device) return static_cast<const uint16_t *>(miss());
+    if (given ? t.size(0) != T || t.size(1) != H || t.size(2) != D : false)
+      return static_cast<const uint16_t *>(miss());
+    T = t.size(0);
+    H = t.size(1);
+    D = t.size(2);
+    if (t.numel() == 0 || (D > 1 && t.stride(2) != 1) || (H > 1 && t.stride(1) != D))
+      return static_cast<const uint16_t *>(miss());
+    ld = T > 1 ? t.stride(0) : H * D;
+    return static_cast<const uint16_t *>(t.data_ptr());
+  }
+  // The cache's tensors from argument i on, for D channels; they define the pages and
+  // heads.
+  void kv8_cache(int i, int64_t D, int64_t (*row_size)(int64_t), int64_t &pages, int64_t &H,
+                 uint8_t *&Kc, uint8_t *&Vc, float *&Ks, float *&Vs) {
+    Ks = const_cast<float *>(matrix<float>(i + 2, at::kFloat, pages, H));
+    if (!ok) return;
+    const int64_t Dp = row_size(D);
+    if (Dp == 0) {
+      ok = false;
+      return;
+    }
+    Kc = shaped<uint8_t, 4>(i, at::kByte, {pages, H, OT_KV8_PAGE, Dp});
+    Vc = shaped<uint8_t, 4>(i + 1, at::kByte, {pages, H, Dp, OT_KV8_PAGE});
+    Vs = sized<float>(i + 3, at::kFloat, pages, H);
+  }
   float real(int i) {
     if (ok && !PyFloat_CheckExact(a[i])) ok = false;
     return ok ? (float)PyFloat_AS_DOUBLE(a[i]) : 0.f;
@@ -425,6 +468,88 @@ PyObject *moe_mx4(PyObject *, PyObject *const *a, Py_ssize_t n) {
   }, true);
 }
 
+using RowFn = int64_t (*)(int64_t);
+
+// (fn, row_size, k, v, cu, kv_len, table, Kc, Vc, Ks, Vs, stream)
+PyObject *kv8_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return run(a, n, 12, [](Args &g) -> int {
+    int64_t T, H, D, ldk, ldv, B, most, pages, heads;
+    uint8_t *Kc, *Vc;
+    float *Ks, *Vs;
+    auto fn = g.address<decltype(&ot_kv8_append)>(0);
+    auto row_size = g.address<RowFn>(1);
+    auto *k = g.rows3(2, T, H, D, ldk);
+    auto *v = g.ok ? g.rows3(3, T, H, D, ldv, true) : nullptr;
+    auto *table = g.matrix<int32_t>(6, kI32, B, most);
+    if (!g.ok) return 0;
+    auto *cu = g.vec<int32_t>(4, kI32, B + 1), *len = g.vec<int32_t>(5, kI32, B);
+    g.kv8_cache(7, D, row_size, pages, heads, Kc, Vc, Ks, Vs);
+    if (g.ok && heads != H) g.ok = false;
+    auto *st = g.stream(11);
+    return g.call([&] {
+      return fn(k, ldk, v, ldv, T, B, H, D, cu, len, table, most, pages, Kc, Vc, Ks, Vs, st);
+    });
+  }, true);
+}
+
+// (fn, row_size, Kc, Vc, Ks, Vs, cu, start, table, k, v, stream)
+PyObject *kv8_read(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return run(a, n, 12, [](Args &g) -> int {
+    int64_t T, H, D, ld, B, most, pages, heads;
+    uint8_t *Kc, *Vc;
+    float *Ks, *Vs;
+    auto fn = g.address<decltype(&ot_kv8_read)>(0);
+    auto row_size = g.address<RowFn>(1);
+    g.rows3(9, T, H, D, ld);
+    if (!g.ok) return 0;
+    auto *k = g.shaped<uint16_t, 3>(9, kF16, {T, H, D}), *v = g.shaped<uint16_t, 3>(10, kF16, {T, H, D});
+    auto *table = g.matrix<int32_t>(8, kI32, B, most);
+    if (!g.ok) return 0;
+    auto *cu = g.vec<int32_t>(6, kI32, B + 1), *start = g.vec<int32_t>(7, kI32, B);
+    g.kv8_cache(2, D, row_size, pages, heads, Kc, Vc, Ks, Vs);
+    if (g.ok && heads != H) g.ok = false;
+    auto *st = g.stream(11);
+    return g.call([&] {
+      return fn(Kc, Vc, Ks, Vs, pages, cu, start, table, most, T, B, H, D, k, v, st);
+    });
+  }, true);
+}
+
+using AttnWsFn = size_t (*)(int64_t, int64_t, int64_t, int64_t, int64_t, int64_t);
+
+// (fn, ws_size, row_size, q, cu, kv_len, table, Kc, Vc, Ks, Vs, scale, causal, window,
+//  max_q, Y, lse, workspace, stream)
+PyObject *attn_kv8(PyObject *, PyObject *const *a, Py_ssize_t n) {
+  return run(a, n, 19, [](Args &g) -> int {
+    int64_t T, Hq, D, ldq, B, most, pages, Hkv;
+    uint8_t *Kc, *Vc;
+    float *Ks, *Vs;
+    auto fn = g.address<decltype(&ot_attn_kv8)>(0);
+    auto ws_size = g.address<AttnWsFn>(1);
+    auto row_size = g.address<RowFn>(2);
+    auto *q = g.rows3(3, T, Hq, D, ldq);
+    auto *table = g.matrix<int32_t>(6, kI32, B, most);
+    if (!g.ok) return 0;
+    auto *cu = g.vec<int32_t>(4, kI32, B + 1), *len = g.vec<int32_t>(5, kI32, B);
+    g.kv8_cache(7, D, row_size, pages, Hkv, Kc, Vc, Ks, Vs);
+    const float scale = g.real(11);
+    if (!g.ok || (g.a[12] != Py_True && g.a[12] != Py_False)) {
+      g.ok = false;
+      return 0;
+    }
+    const int causal = g.a[12] == Py_True;
+    const int64_t window = g.integer(13), max_q = g.integer(14);
+    auto *y = g.shaped<uint16_t, 3>(15, kF16, {T, Hq, D});
+    auto *lse = g.sized<float>(16, kF32, T, Hq, true);
+    auto *ws = g.scratch(17, [&] { return ws_size(T, B, Hq, Hkv, D, max_q); });
+    auto *st = g.stream(18);
+    return g.call([&] {
+      return fn(q, ldq, T, B, Hq, Hkv, D, cu, len, table, most, pages, Kc, Vc, Ks, Vs, scale,
+                causal, window, max_q, y, lse, ws, st);
+    });
+  }, true);
+}
+
 // (fn): the function that returns the current stream's handle
 PyObject *set_current_stream(PyObject *, PyObject *const *a, Py_ssize_t n) {
   if (n != 1 || !PyCallable_Check(a[0])) {
@@ -443,7 +568,8 @@ PyMethodDef kMethods[] = {
     OT_DEF(qlinear), OT_DEF(qlinear_noalloc), OT_DEF(qlinear_packed),
     OT_DEF(qlinear_per_token), OT_DEF(qlinear_asym),
     OT_DEF(quantize_act_mx4), OT_DEF(ln_quantize_act_mx4), OT_DEF(dequantize_mx4),
-    OT_DEF(qlinear_mx4), OT_DEF(moe_mx4), {nullptr, nullptr, 0, nullptr}};
+    OT_DEF(qlinear_mx4), OT_DEF(moe_mx4),
+    OT_DEF(kv8_append), OT_DEF(kv8_read), OT_DEF(attn_kv8), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_otbind", nullptr, -1, kMethods,
                        nullptr, nullptr, nullptr, nullptr};
 

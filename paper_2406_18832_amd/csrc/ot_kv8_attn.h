@@ -1,0 +1,138 @@
+// What the two attention kernels over the 8-bit cache share.
+//
+// The softmax in one pass.  With x_j = log2(e) scale q.K_j, a row keeps a
+// reference m, L = sum_j 2^(x_j + l_j - m) 2^(-l_j) and O = sum_j 2^(x_j + l_j - m) c_j,
+// where a value V_j = 2^(l_j) c_j is a code c_j times its page's scale 2^(l_j): the
+// value scale costs nothing there, as x_j + l_j is one fused multiply-add from the
+// product of codes and queries.  O / L is the row's result; m and L are fp32.
+//
+// The weights 2^(x_j + l_j - m) are an operand of the matrix cores in fp16 (half a
+// step is 2^-11 of a weight); m lies kHeadroom binades under the largest weight, so
+// that fp16's normal numbers reach 2^-29 of it and what is lost below is under
+// 2^-29 of the largest term.  L sums the fp32 weights.
+//
+// Which weight belongs to which token.  S^T = K Q^T has tokens as the MFMA's rows
+// and queries as its columns, and leaves a lane with weights of one query alone,
+// which are, in this order, the operand of O^T = V^T P^T as long as K's row r stands
+// for the right token: no weight changes its lane.
+#pragma once
+
+#include "ot_kv8.h"
+
+namespace ot {
+namespace detail {
+
+constexpr float kHeadroom = 15.f;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kNegInf = -__builtin_inff();
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// A value scale's exponent and what undoes it: a page of zeros (scale 0) counts as
+// scale 1.  A NaN goes by the exponent alone, which reaches the rows that see the page
+// and no others.
+__device__ __forceinline__ void value_scale(float s, float &lg, float &inv) {
+  const float v = s == 0.f ? 1.f : s;
+  lg = __builtin_amdgcn_logf(v);  // log2
+  inv = v == v ? 1.f / v : 1.f;
+}
+
+__device__ __forceinline__ v2h pack_half(float a, float b) {
+  return v2h{(_Float16)a, (_Float16)b};  // each to nearest even
+}
+
+// How the pages of a batch are shared out between workgroups.  An item is a run of
+// at most `chunk` pages of one sequence; every workgroup works out from the lengths
+// how many there are (their sizes are even whatever the lengths: a long sequence
+// among short ones has many) and which one is its own.
+struct Kv8Item {
+  int b, index, chunk;  // sequence (-1: none), which of its items, pages per item
+  int first, count;     // its sequence's first item and their number
+};
+
+// Sequence b's pages and rows, by one lane.
+struct Kv8Seq {
+  Kv8Rows rows;
+  int64_t len;
+  Kv8Span span;
+  bool bad;  // more keys than its table has pages for
+};
+__device__ __forceinline__ Kv8Seq kv8_seq(const Kv8Attn &a, int b) {
+  Kv8Seq s;
+  s.rows = kv8_rows(a.cu[b], a.cu[b + 1], a.T);
+  const int64_t len = a.kv_len[b];
+  s.len = kv8_len(len, a.cache.max_pages);
+  s.bad = len > s.len;
+  s.span = kv8_span(s.len, s.rows.n, 0, s.rows.n, a.causal, a.window);
+  return s;
+}
+// Pages that count in the sharing: at least one, which writes the rows that see no key.
+__device__ __forceinline__ int kv8_shared_pages(const Kv8Seq &s) {
+  return s.rows.n == 0 ? 0 : max(s.span.p1 - s.span.p0, 1);
+}
+
+__device__ __forceinline__ int wave_sum(int v) {
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off);
+  return v;
+}
+
+// chunk: the smallest that makes at most `wanted` items and one more per sequence,
+// but `least`; wanted 0: every sequence is one item.
+__device__ __forceinline__ int kv8_chunk(const Kv8Attn &a, int lane, int wanted, int least) {
+  if (wanted == 0) return 1 << 30;
+  int64_t total = 0;
+  for (int b0 = 0; b0 < a.B; b0 += 64) {
+    const int b = b0 + lane;
+    total += wave_sum(b < a.B ? kv8_shared_pages(kv8_seq(a, b)) : 0);
+  }
+  return (int)kv8_max(least, (total + wanted - 1) / wanted);
+}
+
+__device__ __forceinline__ Kv8Item kv8_item(const Kv8Attn &a, int lane, int x, int wanted,
+                                            int least) {
+  const int chunk = kv8_chunk(a, lane, wanted, least);
+  int before = 0;
+  for (int b0 = 0; b0 < a.B; b0 += 64) {
+    const int b = b0 + lane;
+    const int own = b < a.B ? (kv8_shared_pages(kv8_seq(a, b)) + chunk - 1) / chunk : 0;
+    int upto = own;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      const int o = __shfl_up(upto, off);
+      if (lane >= off) upto += o;
+    }
+    const uint64_t past = __ballot(before + upto > x);
+    if (past != 0) {
+      const int at = __builtin_ctzll(past);
+      const int count = __shfl(own, at), first = before + __shfl(upto, at) - count;
+      return {b0 + at, x - first, chunk, first, count};
+    }
+    before += __shfl(upto, 63);
+  }
+  return {-1, 0, chunk, 0, 0};
+}
+
+// A row's partial result in the workspace: m, L and O[D] (fp32).
+__device__ __forceinline__ int64_t kv8_partial(int64_t item, int64_t h, int64_t row, int64_t Hkv,
+                                               int64_t rows) {
+  return (item * Hkv + h) * rows + row;
+}
+
+}  // namespace detail
+
+// Partial results of a split launch: `items` runs of pages, `rows` rows to each key
+// head.  spans [B] says which items a sequence has.
+struct Kv8Split {
+  int wanted, least;  // as kv8_chunk; wanted 0: no split
+  int64_t items, rows;
+  float *m, *l, *o;
+  int2 *spans;
+};
+
+hipError_t launch_kv8_decode(const Kv8Attn &a, const Kv8Split &s, hipStream_t st);
+hipError_t launch_kv8_combine(const Kv8Attn &a, const Kv8Split &s, hipStream_t st);
+hipError_t launch_kv8_tiles(const Kv8Attn &a, hipStream_t st);
+
+}  // namespace ot

@@ -1,0 +1,343 @@
+// Attention over the 8-bit cache for few query rows: decode, and drafts of a few
+// tokens.  It reads every code once and is bound by that.
+//
+// A workgroup takes one key head and a run of a sequence's pages; its four waves
+// take the pages in turn, each with a running maximum, sum and output of its own
+// (no barrier until they meet at the end).  Up to 16 query rows (tokens times the
+// query heads of the key head) are the 16 columns of v_mfma_f32_16x16x32_f16, 32
+// those of two; with a single row 15/16 of the matrix cores' work is for nothing,
+// which costs less than the loads take.
+//
+// Lane l has query row l mod 16 and, with g = l / 16, tokens 16 g .. 16 g + 15 of a
+// page: K's row 4 g' + i of the s-th of four products is token 16 g' + 4 s + i.
+// V^T's rows are channels, its 16 bytes of a lane are tokens 16 g .. of one channel.
+#include <math.h>
+
+#include "ot_kv8_attn.h"
+
+namespace ot {
+namespace detail {
+
+constexpr int kDecodeWaves = 4;
+
+template <int DP, int RT>
+__global__ __launch_bounds__(64 * kDecodeWaves) void kv8_decode_kernel(Kv8Attn a, Kv8Split s) {
+  constexpr int kChunks = DP / 64, kTail = DP % 64 / 32;  // of a key's row
+  constexpr int kSteps = DP / 32, kOut = DP / 16;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int col = lane & 15, g = lane >> 4;
+  const int h = blockIdx.y;
+  const int G = a.Hq / a.Hkv;
+
+  const Kv8Item item = kv8_item(a, lane, blockIdx.x, s.wanted, s.least);
+  if (item.b < 0) return;
+  const Kv8Seq seq = kv8_seq(a, item.b);
+  const int rows = min(seq.rows.n, a.max_q) * G, row_base = blockIdx.z * (16 * RT);
+  if (blockIdx.z == 0 && h == 0 && item.index == 0 && threadIdx.x == 0 && s.wanted != 0)
+    s.spans[item.b] = make_int2(item.first, item.count);
+  if (row_base >= rows) return;
+  const int64_t p0 = seq.span.p0 + (int64_t)item.index * item.chunk;
+  const int64_t p1 = kv8_min(p0 + item.chunk, seq.span.p1);
+
+  // this lane's query rows, and the positions of the keys that they see
+  v8h q[RT][kSteps];
+  int key_lo[RT], key_hi[RT];  // [lo, hi]
+  int all_lo = 0, all_hi = 0x7fffffff;
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    const int row = row_base + 16 * r + col;
+    const bool in = row < rows;
+    const int i = in ? row / G : 0;
+    const uint16_t *p = a.q + (seq.rows.row0 + i) * a.ldq + (h * G + (in ? row % G : 0)) * a.D;
+#pragma unroll
+    for (int st = 0; st < kSteps; ++st) {
+      const int d = st < 2 * kChunks ? 64 * (st >> 1) + 16 * g + 8 * (st & 1) : 64 * kChunks + 8 * g;
+      v4u w = {0u, 0u, 0u, 0u};
+      if (in && d < a.D) w = *reinterpret_cast<const v4u *>(p + d);
+      q[r][st] = __builtin_bit_cast(v8h, w);
+    }
+    const int pos = (int)(seq.len - seq.rows.n + i);
+    key_hi[r] = a.causal ? pos : (int)seq.len - 1;
+    key_lo[r] = a.window > 0 ? (int)kv8_max(0, pos - a.window + 1) : 0;
+  }
+  // keys that every row sees: those after the last row's first and up to the first
+  // row's last
+  if (a.causal) all_hi = (int)(seq.len - seq.rows.n);
+  all_hi = min(all_hi, (int)seq.len - 1);
+  if (a.window > 0) all_lo = (int)kv8_max(0, seq.len - a.window);
+
+  float m[RT], l[RT];
+  v4f o[RT][kOut];
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    m[r] = kNegInf;
+    l[r] = 0.f;
+#pragma unroll
+    for (int t = 0; t < kOut; ++t) o[r][t] = v4f{0.f, 0.f, 0.f, 0.f};
+  }
+  const float fac = a.scale * kLog2e;
+
+  // 64 of this wave's pages at a time: lane i has the i-th one's number and scales
+  for (int64_t batch = p0 + wave; batch < p1; batch += 64 * kDecodeWaves) {
+    const int64_t mine = batch + kDecodeWaves * lane;
+    int64_t page = -1;
+    float ks = __builtin_nanf(""), vs = 0.f;
+    if (mine < p1) {
+      page = kv8_page(a.cache.table, item.b, mine, a.cache.max_pages, a.cache.num_pages);
+      if (page >= 0) {
+        ks = a.cache.Ks[page * a.Hkv + h];
+        vs = a.cache.Vs[page * a.Hkv + h];
+      }
+    }
+    if (page < 0) page = 0;  // its scale is NaN: what sees it is
+    float lg, inv;
+    value_scale(vs, lg, inv);
+    ks = seq.bad ? __builtin_nanf("") : ks * fac;
+    const int todo = (int)kv8_min(64, (p1 - batch + kDecodeWaves - 1) / kDecodeWaves);
+    for (int n = 0; n < todo; ++n) {
+      const int64_t ph = (int64_t)__builtin_amdgcn_readlane((int)page, n) * a.Hkv + h;
+      const float f = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, ks), n));
+      const float lgv = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, lg), n));
+      const float iv = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, inv), n));
+      const uint8_t *kp = a.cache.Kc + ph * (DP * kKv8Page);
+      const uint8_t *vp = a.cache.Vc + ph * (DP * kKv8Page);
+      v4u kc[4][kChunks > 0 ? kChunks : 1];
+      v2u kt[4];
+      v4u vc[kOut];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const uint8_t *p = kp + (16 * (col >> 2) + 4 * t + (col & 3)) * DP;
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) kc[t][c] = *reinterpret_cast<const v4u *>(p + 64 * c + 16 * g);
+        if constexpr (kTail) kt[t] = *reinterpret_cast<const v2u *>(p + 64 * kChunks + 8 * g);
+      }
+#pragma unroll
+      for (int t = 0; t < kOut; ++t)
+        vc[t] = *reinterpret_cast<const v4u *>(vp + (16 * t + col) * kKv8Page + 16 * g);
+
+      v4f x[RT][4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+#pragma unroll
+        for (int r = 0; r < RT; ++r) x[r][t] = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int st = 0; st < kSteps; ++st) {
+          v8h k;
+          if (st < 2 * kChunks) {
+            const v4u w = kc[t][st >> 1];
+            k = (st & 1) ? kv8_halves(w[2], w[3]) : kv8_halves(w[0], w[1]);
+          } else {
+            k = kv8_halves(kt[t][0], kt[t][1]);
+          }
+#pragma unroll
+          for (int r = 0; r < RT; ++r)
+            x[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[r][st], x[r][t], 0, 0, 0);
+        }
+      }
+      const int token = (int)((batch + kDecodeWaves * n) * kKv8Page);
+      const bool cut = token < all_lo || token + kKv8Page - 1 > all_hi;
+      v8h p[RT][2];
+#pragma unroll
+      for (int r = 0; r < RT; ++r) {
+        float most = kNegInf;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float v = __builtin_fmaf(x[r][t][i], f, lgv);
+            const int key = token + 16 * g + 4 * t + i;
+            if (cut && (key < key_lo[r] || key > key_hi[r])) v = kNegInf;
+            x[r][t][i] = v;
+            most = fmaxf(most, v);
+          }
+        }
+        most = fmaxf(most, __shfl_xor(most, 16));
+        most = fmaxf(most, __shfl_xor(most, 32));
+        const float now = fmaxf(m[r], most - kHeadroom);
+        const float ref = now == kNegInf ? 0.f : now;  // no key yet
+        const float keep = exp2_fast(m[r] - ref);
+        m[r] = now;
+        float sum = 0.f;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          float w[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            w[i] = exp2_fast(x[r][t][i] - ref);
+            sum += w[i];
+          }
+          const v2h lo = pack_half(w[0], w[1]), hi = pack_half(w[2], w[3]);
+          p[r][t >> 1][4 * (t & 1) + 0] = lo[0];
+          p[r][t >> 1][4 * (t & 1) + 1] = lo[1];
+          p[r][t >> 1][4 * (t & 1) + 2] = hi[0];
+          p[r][t >> 1][4 * (t & 1) + 3] = hi[1];
+        }
+        l[r] = __builtin_fmaf(l[r], keep, sum * iv);
+#pragma unroll
+        for (int t = 0; t < kOut; ++t) o[r][t] *= keep;
+      }
+#pragma unroll
+      for (int t = 0; t < kOut; ++t) {
+        const v8h v0 = kv8_halves(vc[t][0], vc[t][1]), v1 = kv8_halves(vc[t][2], vc[t][3]);
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+          o[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, p[r][0], o[r][t], 0, 0, 0);
+          o[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, p[r][1], o[r][t], 0, 0, 0);
+        }
+      }
+    }
+  }
+
+  // The waves' results meet, some channels at a time; only rows that exist are written.
+  constexpr int kRows = 16 * RT;
+  constexpr int kGroups = (kOut * RT + 7) / 8, kPer = kOut / kGroups, kCols = 16 * kPer;
+  static_assert(kPer * kGroups == kOut, "whole groups");
+  __shared__ float meet_m[kDecodeWaves][kRows], meet_l[kDecodeWaves][kRows];
+  __shared__ __attribute__((aligned(16))) float meet_o[kDecodeWaves][kRows][kCols];
+  const int here = min(rows - row_base, kRows);
+#pragma unroll
+  for (int r = 0; r < RT; ++r) {
+    l[r] += __shfl_xor(l[r], 16);
+    l[r] += __shfl_xor(l[r], 32);
+    if (g == 0) {
+      meet_m[wave][16 * r + col] = m[r];
+      meet_l[wave][16 * r + col] = l[r];
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < kGroups; ++u) {
+    if (u > 0) __syncthreads();
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+      if (16 * r + col < here) {
+#pragma unroll
+        for (int t = 0; t < kPer; ++t)
+          *reinterpret_cast<v4f *>(&meet_o[wave][16 * r + col][16 * t + 4 * g]) = o[r][u * kPer + t];
+      }
+    __syncthreads();
+    for (int e = threadIdx.x; e < here * (kCols / 4); e += 64 * kDecodeWaves) {
+      const int row = e / (kCols / 4), c = e % (kCols / 4) * 4, d = u * kCols + c;
+      float top = kNegInf;
+#pragma unroll
+      for (int w = 0; w < kDecodeWaves; ++w) top = fmaxf(top, meet_m[w][row]);
+      const float ref = top == kNegInf ? 0.f : top;
+      float sum = 0.f;
+      v4f out = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < kDecodeWaves; ++w) {
+        const float part = exp2_fast(meet_m[w][row] - ref);
+        sum = __builtin_fmaf(part, meet_l[w][row], sum);
+        const v4f v = *reinterpret_cast<const v4f *>(&meet_o[w][row][c]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) out[i] = __builtin_fmaf(part, v[i], out[i]);
+      }
+      const int full = row_base + row;
+      if (item.count == 1) {
+        const int i = full / G, head = h * G + full % G;
+        const int64_t pos = seq.len - seq.rows.n + i;
+        // a row that sees no key: as its position says, not as its sum does
+        const bool empty = seq.len == 0 || (a.causal && pos < 0);
+        const int64_t at = (int64_t)(seq.rows.row0 + i) * a.Hq + head;
+        const float scale = 1.f / sum;
+        if (d < a.D) {
+          v2u y;
+          y[0] = __builtin_bit_cast(uint32_t, pack_half(out[0] * scale, out[1] * scale));
+          y[1] = __builtin_bit_cast(uint32_t, pack_half(out[2] * scale, out[3] * scale));
+          if (empty) y = v2u{0u, 0u};
+          *reinterpret_cast<v2u *>(a.Y + at * a.D + d) = y;
+        }
+        if (d == 0 && a.lse != nullptr)
+          a.lse[at] = empty ? kNegInf : (top + log2f(sum)) * kLn2;
+      } else {
+        const int64_t at = kv8_partial(blockIdx.x, h, full, a.Hkv, s.rows);
+        if (d == 0) {
+          s.m[at] = top;
+          s.l[at] = sum;
+        }
+        *reinterpret_cast<v4f *>(s.o + at * DP + d) = out;
+      }
+    }
+  }
+}
+
+// The items of a sequence joined: a wave to a query row.
+template <int DP>
+__global__ __launch_bounds__(256) void kv8_combine_kernel(Kv8Attn a, Kv8Split s) {
+  const int lane = threadIdx.x & 63, b = blockIdx.y;
+  const int G = a.Hq / a.Hkv;
+  const Kv8Rows rows = kv8_rows(a.cu[b], a.cu[b + 1], a.T);
+  const int which = blockIdx.x * 4 + (threadIdx.x >> 6);  // (key head, row)
+  const int h = which / (int)s.rows, row = which % (int)s.rows;
+  if (h >= a.Hkv || row >= min(rows.n, a.max_q) * G) return;
+  const int2 span = s.spans[b];
+  if (span.y <= 1) return;
+  float ref = kNegInf;
+  for (int c = lane; c < span.y; c += 64)
+    ref = fmaxf(ref, s.m[kv8_partial(span.x + c, h, row, a.Hkv, s.rows)]);
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) ref = fmaxf(ref, __shfl_xor(ref, off));
+  const float top = ref;
+  if (ref == kNegInf) ref = 0.f;
+  constexpr int kPer = (DP + 63) / 64;
+  float sum = 0.f, out[kPer];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) out[i] = 0.f;
+  for (int c = 0; c < span.y; ++c) {
+    const int64_t at = kv8_partial(span.x + c, h, row, a.Hkv, s.rows);
+    const float part = exp2_fast(s.m[at] - ref);
+    sum = __builtin_fmaf(part, s.l[at], sum);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      if (64 * i + lane < a.D) out[i] = __builtin_fmaf(part, s.o[at * DP + 64 * i + lane], out[i]);
+  }
+  const int i = row / G, head = h * G + row % G;
+  const int64_t len = kv8_len(a.kv_len[b], a.cache.max_pages);
+  const bool empty = len == 0 || (a.causal && len - rows.n + i < 0);
+  const int64_t at = (int64_t)(rows.row0 + i) * a.Hq + head;
+  const float scale = 1.f / sum;
+#pragma unroll
+  for (int j = 0; j < kPer; ++j)
+    if (64 * j + lane < a.D)
+      a.Y[at * a.D + 64 * j + lane] = empty ? 0 : float_to_half_bits(out[j] * scale);
+  if (lane == 0 && a.lse != nullptr) a.lse[at] = empty ? kNegInf : (top + log2f(sum)) * kLn2;
+}
+
+template <int DP, int RT>
+hipError_t decode_launch(const Kv8Attn &a, int64_t max_rows, const Kv8Split &s, hipStream_t st) {
+  const dim3 grid((unsigned)s.items, (unsigned)a.Hkv, (unsigned)((max_rows + 16 * RT - 1) / (16 * RT)));
+  kv8_decode_kernel<DP, RT><<<grid, 64 * kDecodeWaves, 0, st>>>(a, s);
+  return hipGetLastError();
+}
+
+template <int DP>
+hipError_t decode_width(const Kv8Attn &a, int64_t max_rows, const Kv8Split &s, hipStream_t st) {
+  return max_rows <= 16 ? decode_launch<DP, 1>(a, max_rows, s, st)
+                        : decode_launch<DP, 2>(a, max_rows, s, st);
+}
+
+}  // namespace detail
+
+hipError_t launch_kv8_decode(const Kv8Attn &a, const Kv8Split &s, hipStream_t st) {
+  const int64_t max_rows = (int64_t)a.max_q * (a.Hq / a.Hkv);
+  switch (kv8_width(a.D)) {
+    case 64: return detail::decode_width<64>(a, max_rows, s, st);
+    case 96: return detail::decode_width<96>(a, max_rows, s, st);
+    case 128: return detail::decode_width<128>(a, max_rows, s, st);
+    case 192: return detail::decode_width<192>(a, max_rows, s, st);
+    default: return detail::decode_width<256>(a, max_rows, s, st);
+  }
+}
+
+hipError_t launch_kv8_combine(const Kv8Attn &a, const Kv8Split &s, hipStream_t st) {
+  const dim3 grid((unsigned)((a.Hkv * s.rows + 3) / 4), (unsigned)a.B);
+  switch (kv8_width(a.D)) {
+    case 64: detail::kv8_combine_kernel<64><<<grid, 256, 0, st>>>(a, s); break;
+    case 96: detail::kv8_combine_kernel<96><<<grid, 256, 0, st>>>(a, s); break;
+    case 128: detail::kv8_combine_kernel<128><<<grid, 256, 0, st>>>(a, s); break;
+    case 192: detail::kv8_combine_kernel<192><<<grid, 256, 0, st>>>(a, s); break;
+    default: detail::kv8_combine_kernel<256><<<grid, 256, 0, st>>>(a, s); break;
+  }
+  return hipGetLastError();
+}
+
+}  // namespace ot

@@ -66,6 +66,13 @@ _BOUND_MX4 = {
 }
 _n_quantize_act_mx4 = _n_ln_quantize_act_mx4 = _n_dequantize_mx4 = _unbound
 _n_qlinear_mx4 = _n_moe_mx4 = _unbound
+# and for the 8-bit cache's
+_BOUND_KV8 = {
+    "kv8_append": ("ot_kv8_append", "ot_kv8_row_size"),
+    "kv8_read": ("ot_kv8_read", "ot_kv8_row_size"),
+    "attn_kv8": ("ot_attn_kv8", "ot_attn_kv8_workspace_size", "ot_kv8_row_size"),
+}
+_n_kv8_append = _n_kv8_read = _n_attn_kv8 = _unbound
 
 
 def _load_bind(L) -> None:
@@ -87,7 +94,7 @@ def _load_bind(L) -> None:
         return
     _bind = _otbind
     _otbind.set_current_stream(_current_stream)
-    for name, symbols in (*_BOUND.items(), *_BOUND_MX4.items()):
+    for name, symbols in (*_BOUND.items(), *_BOUND_MX4.items(), *_BOUND_KV8.items()):
         addresses = [ctypes.cast(getattr(L, s), ctypes.c_void_p).value for s in symbols]
         globals()["_n_" + name] = partial(getattr(_otbind, name), *addresses)
 
@@ -177,6 +184,22 @@ def lib() -> ctypes.CDLL:
                                  vp]
         L.ot_moe_mx4_workspace_size.restype = ctypes.c_size_t
         L.ot_moe_mx4_workspace_size.argtypes = [i64, i64, i64, i64, i64]
+        L.ot_kv8_row_size.restype = i64
+        L.ot_kv8_row_size.argtypes = [i64]
+        L.ot_kv8_append.restype = c_int
+        L.ot_kv8_append.argtypes = [vp, i64, vp, i64, i64, i64, i64, i64, vp, vp, vp, i64, i64, vp,
+                                    vp, vp, vp, vp]
+        L.ot_kv8_read.restype = c_int
+        L.ot_kv8_read.argtypes = [vp, vp, vp, vp, i64, vp, vp, vp, i64, i64, i64, i64, i64, vp, vp,
+                                  vp]
+        L.ot_attn_kv8.restype = c_int
+        L.ot_attn_kv8.argtypes = [vp, i64, i64, i64, i64, i64, i64, vp, vp, vp, i64, i64, vp, vp,
+                                  vp, vp, ctypes.c_float, c_int, i64, i64, vp, vp, vp, vp]
+        L.ot_attn_kv8_workspace_size.restype = ctypes.c_size_t
+        L.ot_attn_kv8_workspace_size.argtypes = [i64, i64, i64, i64, i64, i64]
+        L.ot_attn_kv8_plan.restype = c_int
+        L.ot_attn_kv8_plan.argtypes = [i64, i64, i64, i64, i64, i64, c_int, ctypes.c_char_p,
+                                       ctypes.c_size_t]
         _load_bind(L)
         _lib = L
     return _lib
@@ -892,3 +915,179 @@ def moe_mx4(Xc, Xe, logits, top_k, W1p, b1, W2p, b2, F, act, workspace=None):
     Y = torch.empty((M, H), dtype=torch.float16, device=Xc.device)
     ot_moe_mx4(Xc, Xe, logits, top_k, W1p, b1, W2p, b2, F, act, Y, workspace)
     return Y
+
+
+# ---------------------------------------------------------------------------
+# KV8: the key/value cache in 8 bits.  A cache is four tensors: codes Kc
+# [num_pages, H, 64, Dp] and Vc [num_pages, H, Dp, 64] uint8, scales Ks and Vs
+# [num_pages, H] fp32.
+# ---------------------------------------------------------------------------
+KV8_PAGE = 64
+
+
+def ot_kv8_row_size(D: int) -> int:
+    return int(lib().ot_kv8_row_size(D))
+
+
+def _kv8_rows(t, name, shape=None):
+    """(T, heads, D, elements between rows, pointer) of a tensor [T, heads, D] fp16 whose
+    rows are dense by themselves: what a slice of a fused linear's output is."""
+    if not isinstance(t, torch.Tensor) or t.dim() != 3:
+        raise ValueError(f"{name} must be a tensor [T, heads, D]")
+    T, H, D = t.shape
+    if t.numel() and ((D > 1 and t.stride(2) != 1) or (H > 1 and t.stride(1) != D)):
+        raise ValueError(f"{name} must have dense rows [heads, D]")
+    ld = t.stride(0) if T > 1 and t.numel() else H * D
+    if shape is not None and (T, H, D) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {(T, H, D)}")
+    if t.dtype != torch.float16:
+        raise TypeError(f"{name} must be {torch.float16}, got {t.dtype}")
+    if t.device.type != "cuda":
+        raise ValueError(f"{name} must be on the GPU")
+    if _current_device is not None and t.get_device() != _current_device():
+        raise ValueError(f"{name} must be on the current device {_current_device()}, not {t.device}")
+    return T, H, D, ld, t.data_ptr()
+
+
+def _kv8_cache(Kc, Vc, Ks, Vs, D):
+    """(pages, H, the four pointers) of a cache for D channels."""
+    if not isinstance(Ks, torch.Tensor) or Ks.dim() != 2:
+        raise ValueError("Ks must be a tensor [num_pages, H]")
+    pages, H = Ks.shape
+    Dp = ot_kv8_row_size(D)
+    if Dp == 0:
+        raise ValueError(f"the cache takes a multiple of 16 channels from 16 to 256, got {D}")
+    return (pages, H, _mx4_dev(Kc, torch.uint8, "Kc", (pages, H, KV8_PAGE, Dp)),
+            _mx4_dev(Vc, torch.uint8, "Vc", (pages, H, Dp, KV8_PAGE)),
+            _mx4_dev(Ks, torch.float32, "Ks"), _mx4_dev(Vs, torch.float32, "Vs", (pages, H)))
+
+
+def _kv8_batch(cu, lengths, table, name):
+    """(B, max_pages, the three pointers) of a batch."""
+    if not isinstance(table, torch.Tensor) or table.dim() != 2:
+        raise ValueError("table must be a tensor [B, max_pages]")
+    B, most = table.shape
+    return (B, most, _mx4_dev(cu, torch.int32, "cu", (B + 1,)),
+            _mx4_dev(lengths, torch.int32, name, (B,)), _mx4_dev(table, torch.int32, "table"))
+
+
+def ot_kv8_append(k, v, cu, kv_len, table, Kc, Vc, Ks, Vs, stream=None):
+    """Quantizes the new tokens k, v [T, H, D] fp16 (rows may lie apart: slices of a
+    fused linear's output serve) into the cache's pages: rows cu[b]..cu[b + 1] - 1 are
+    the last of sequence b's kv_len[b] tokens, token j in page table[b, j // 64].
+    Asynchronous."""
+    rc = _n_kv8_append(k, v, cu, kv_len, table, Kc, Vc, Ks, Vs, stream)
+    if rc is not None:
+        return _check(rc, "ot_kv8_append")
+    T, H, D, ldk, pk = _kv8_rows(k, "k")
+    _, _, _, ldv, pv = _kv8_rows(v, "v", (T, H, D))
+    pages, heads, pKc, pVc, pKs, pVs = _kv8_cache(Kc, Vc, Ks, Vs, D)
+    if heads != H:
+        raise ValueError(f"the cache has {heads} heads, k has {H}")
+    B, most, pcu, plen, ptable = _kv8_batch(cu, kv_len, table, "kv_len")
+    rc = lib().ot_kv8_append(pk, ldk, pv, ldv, T, B, H, D, pcu, plen, ptable, most, pages, pKc,
+                             pVc, pKs, pVs, _stream(stream))
+    _check(rc, "ot_kv8_append")
+
+
+def ot_kv8_read(Kc, Vc, Ks, Vs, cu, start, table, k, v, stream=None):
+    """Rows cu[b]..cu[b + 1] - 1 of k and v [T, H, D] fp16 receive sequence b's tokens
+    from position start[b] on.  Asynchronous."""
+    rc = _n_kv8_read(Kc, Vc, Ks, Vs, cu, start, table, k, v, stream)
+    if rc is not None:
+        return _check(rc, "ot_kv8_read")
+    if not isinstance(k, torch.Tensor) or k.dim() != 3:
+        raise ValueError("k must be a tensor [T, H, D]")
+    T, H, D = k.shape
+    pages, heads, pKc, pVc, pKs, pVs = _kv8_cache(Kc, Vc, Ks, Vs, D)
+    if heads != H:
+        raise ValueError(f"the cache has {heads} heads, k has {H}")
+    B, most, pcu, pstart, ptable = _kv8_batch(cu, start, table, "start")
+    rc = lib().ot_kv8_read(pKc, pVc, pKs, pVs, pages, pcu, pstart, ptable, most, T, B, H, D,
+                           _mx4_dev(k, torch.float16, "k"),
+                           _mx4_dev(v, torch.float16, "v", (T, H, D)), _stream(stream))
+    _check(rc, "ot_kv8_read")
+
+
+def ot_attn_kv8_workspace_size(T: int, B: int, Hq: int, Hkv: int, D: int, max_q: int) -> int:
+    return int(lib().ot_attn_kv8_workspace_size(T, B, Hq, Hkv, D, max_q))
+
+
+def ot_attn_kv8_plan(T: int, B: int, Hq: int, Hkv: int, D: int, max_q: int,
+                     with_workspace=False) -> str:
+    """The kernel configuration ot_attn_kv8 launches for these sizes on the current
+    device (text; no device work)."""
+    buf = ctypes.create_string_buffer(96)
+    _check(lib().ot_attn_kv8_plan(T, B, Hq, Hkv, D, max_q, int(bool(with_workspace)), buf,
+                                  len(buf)), "ot_attn_kv8_plan")
+    return buf.value.decode()
+
+
+def ot_attn_kv8(q, cu, kv_len, table, Kc, Vc, Ks, Vs, scale, causal, window, max_q, Y, lse=None,
+                workspace=None, stream=None):
+    """Attention of the queries q [T, Hq, D] fp16 (rows may lie apart) over the cache ->
+    Y [T, Hq, D] fp16 (and lse [T, Hq] fp32 if given).  Sequence b's rows are the last of
+    its kv_len[b] tokens; causal: a row sees the keys up to its own, of them the last
+    `window` where that is not 0.  max_q: the most rows that a sequence has.
+    workspace: ot_attn_kv8_workspace_size bytes (uint8) or None.  Asynchronous."""
+    rc = _n_attn_kv8(q, cu, kv_len, table, Kc, Vc, Ks, Vs, scale, causal, window, max_q, Y, lse,
+                     workspace, stream)
+    if rc is not None:
+        return _check(rc, "ot_attn_kv8")
+    T, Hq, D, ldq, pq = _kv8_rows(q, "q")
+    pages, Hkv, pKc, pVc, pKs, pVs = _kv8_cache(Kc, Vc, Ks, Vs, D)
+    B, most, pcu, plen, ptable = _kv8_batch(cu, kv_len, table, "kv_len")
+    rc = lib().ot_attn_kv8(pq, ldq, T, B, Hq, Hkv, D, pcu, plen, ptable, most, pages, pKc, pVc,
+                           pKs, pVs, float(scale), int(bool(causal)), int(window), int(max_q),
+                           _mx4_dev(Y, torch.float16, "Y", (T, Hq, D)),
+                           _mx4_dev(lse, torch.float32, "lse", (T, Hq)),
+                           _scratch(workspace,
+                                    ot_attn_kv8_workspace_size(T, B, Hq, Hkv, D, max_q)),
+                           _stream(stream))
+    _check(rc, "ot_attn_kv8")
+
+
+def kv8_cache(num_pages: int, H: int, D: int, device=None):
+    """An empty cache (Kc, Vc, Ks, Vs) of num_pages pages for H heads of D channels."""
+    Dp, device = ot_kv8_row_size(D), device or "cuda"
+    if Dp == 0:
+        raise ValueError(f"the cache takes a multiple of 16 channels from 16 to 256, got {D}")
+    return (torch.empty((num_pages, H, KV8_PAGE, Dp), dtype=torch.uint8, device=device),
+            torch.empty((num_pages, H, Dp, KV8_PAGE), dtype=torch.uint8, device=device),
+            torch.zeros((num_pages, H), dtype=torch.float32, device=device),
+            torch.zeros((num_pages, H), dtype=torch.float32, device=device))
+
+
+def kv8_append(k, v, cu, kv_len, table, cache):
+    ot_kv8_append(k, v, cu, kv_len, table, *cache)
+
+
+def kv8_read(cache, cu, start, table, T: int, D: int):
+    """Allocating wrapper of ot_kv8_read for T = cu[B] tokens; returns (k, v)."""
+    H = cache[2].shape[1]
+    k, v = (torch.empty((T, H, D), dtype=torch.float16, device=cache[0].device) for _ in range(2))
+    ot_kv8_read(*cache, cu, start, table, k, v)
+    return k, v
+
+
+def attn_kv8_workspace_for(T: int, B: int, Hq: int, Hkv: int, D: int, max_q: int, device=None):
+    """A scratch buffer for ot_attn_kv8 at these sizes, or None when it uses none."""
+    n = ot_attn_kv8_workspace_size(T, B, Hq, Hkv, D, max_q)
+    return torch.empty(n, dtype=torch.uint8, device=device or "cuda") if n else None
+
+
+def attn_kv8(q, cu, kv_len, table, cache, scale=None, causal=True, window=0, max_q=None,
+             want_lse=False, workspace=True):
+    """Allocating wrapper of ot_attn_kv8.  scale: D ** -0.5 unless given; max_q: the
+    batch's rows unless given (1 for decode: the kernel for few rows is faster);
+    workspace: True allocates one, None or False use none."""
+    T, Hq, D = q.shape
+    max_q = max(T, 1) if max_q is None else max_q
+    Y = torch.empty((T, Hq, D), dtype=torch.float16, device=q.device)
+    lse = torch.empty((T, Hq), dtype=torch.float32, device=q.device) if want_lse else None
+    if workspace is True:
+        workspace = attn_kv8_workspace_for(T, table.shape[0], Hq, cache[2].shape[1], D, max_q,
+                                           q.device)
+    ot_attn_kv8(q, cu, kv_len, table, *cache, D ** -0.5 if scale is None else scale, causal,
+                window, max_q, Y, lse, None if workspace is False else workspace)
+    return (Y, lse) if want_lse else Y

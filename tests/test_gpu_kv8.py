@@ -1,0 +1,393 @@
+"""The 8-bit cache on the GPU against the oracle: codes and scales bit for bit, values
+read back bit for bit, attention within the tolerance that oracle/kv8_oracle.py derives
+from the number formats."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import kv8_oracle as O
+from paper_2406_18832_amd import ot
+from tests import _kv8 as K
+
+pytestmark = pytest.mark.gpu
+
+
+def case(msg):
+    print(f"[case] {msg}", flush=True)
+
+
+def f16(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def append(dev, k, v, cu, kv_len, table):
+    ot.ot_kv8_append(f16(k), f16(v), K.ints(cu), K.ints(kv_len), K.ints(table), *dev)
+    torch.cuda.synchronize()
+
+
+# ---------------------------------------------------------------------------
+# Writing
+# ---------------------------------------------------------------------------
+WRITES = [  # heads, channels, tokens before, new tokens
+    (1, 64, [0], [1]), (3, 64, [100], [1]), (2, 16, [63, 64, 65], [1, 1, 1]),
+    (2, 128, [0, 0, 63, 1], [64, 65, 2, 63]), (5, 80, [10, 0, 130], [200, 3, 0]),
+    (2, 96, [0], [130]), (3, 256, [5, 64], [70, 64]), (2, 192, [60], [10]),
+    (7, 112, list(range(0, 70)), [i % 3 for i in range(70)]),
+    (1, 128, [0] * 130, [1 + i % 66 for i in range(130)]),
+]
+
+
+@pytest.mark.parametrize("H,D,before,new", WRITES)
+def test_append_codes_and_scales(H, D, before, new):
+    case(f"append H={H} D={D} B={len(before)}")
+    r = np.random.default_rng(H * 1000 + D)
+    after = [a + n for a, n in zip(before, new)]
+    table, pages = K.tables(r, after)
+    want = O.empty_cache(pages, H, D, 0xA5, np.nan)
+    cu0 = K.rows_of(before)
+    O.append(want, K.heads_of(r, cu0[-1], H, D), K.heads_of(r, cu0[-1], H, D), cu0,
+             np.array(before), table)
+    dev = K.device(want)
+    untouched = {n: a.copy() for n, a in want.items()}
+    cu = K.rows_of(new)
+    # sizes from far below to far above what the pages hold
+    size = 2.0 ** r.uniform(-6, 6, (cu[-1], 1, 1))
+    k = (K.heads_of(r, cu[-1], H, D) * size).astype(np.float16)
+    v = (K.heads_of(r, cu[-1], H, D) * size[::-1]).astype(np.float16)
+    O.append(want, k, v, cu, np.array(after), table)
+    append(dev, k, v, cu, after, table)
+    got = K.host(dev)
+    K.assert_same_cache(got, want, table, after, D)
+    used = {int(p) for b in range(len(after)) for p in table[b, :-(-after[b] // 64)]}
+    rest = [p for p in range(pages) if p not in used]
+    for n in K.ORDER:  # pages of no sequence are as they were
+        assert np.array_equal(got[n][rest], untouched[n][rest], equal_nan=got[n].dtype == np.float32)
+    append(dev, k, v, cu, after, table)  # the same tokens again change nothing
+    K.assert_same_cache(K.host(dev), want, table, after, D)
+
+
+def test_append_token_by_token_through_pages():
+    case("append token by token")
+    r = np.random.default_rng(2)
+    H, D, n = 3, 80, 140
+    table, pages = K.tables(r, [n, n])
+    want = O.empty_cache(pages, H, D, 0x11, np.nan)
+    dev = K.device(want)
+    cu = np.array([0, 1, 2])
+    for i in range(n):
+        k = (K.heads_of(r, 2, H, D) * 2.0 ** r.uniform(-3, 3)).astype(np.float16)
+        v = (K.heads_of(r, 2, H, D) * 2.0 ** r.uniform(-3, 3)).astype(np.float16)
+        O.append(want, k, v, cu, [i + 1, i + 1], table)
+        ot.ot_kv8_append(f16(k), f16(v), K.ints(cu), K.ints([i + 1, i + 1]), K.ints(table), *dev)
+    torch.cuda.synchronize()
+    K.assert_same_cache(K.host(dev), want, table, [n, n], D)
+
+
+def test_append_zeros_extremes_and_nonfinite():
+    case("append zeros, extremes, NaN")
+    H, D = 6, 64
+    table = np.array([[2, 0], [1, 3]], np.int32)
+    want = O.empty_cache(4, H, D, 0xFF, np.nan)
+    dev = K.device(want)
+    steps = []
+    a = np.zeros((6, H, D), np.float16)
+    steps.append((a, [0, 3, 6], [3, 3]))                      # zeros: scale 0
+    b = np.zeros((2, H, D), np.float16)
+    b[:, 0, 0], b[:, 1, 5], b[:, 2, 7] = 65504, 2.0 ** -24, -1  # from scale 0 on
+    b[0, 3, 1], b[1, 4, 2] = np.nan, -np.inf
+    steps.append((b, [0, 1, 2], [4, 4]))
+    c = np.full((2, H, D), 2.0 ** -24, np.float16)
+    steps.append((c, [0, 1, 2], [5, 5]))                       # far below; NaN stays
+    d = np.full((2, H, D), -65504, np.float16)
+    steps.append((d, [0, 1, 2], [6, 6]))                       # far above: k up to 40
+    e = np.ones((120, H, D), np.float16)
+    steps.append((e, [0, 60, 120], [66, 66]))                  # into a new page: finite there
+    for x, cu, lens in steps:
+        O.append(want, x, x, np.array(cu), lens, table)
+        append(dev, x, x, cu, lens, table)
+        K.assert_same_cache(K.host(dev), want, table, lens, D)
+    assert np.isnan(want["Ks"][2, 3]) and np.isfinite(want["Ks"][0]).all()
+
+
+def test_append_rounds_ties_to_even_and_clips():
+    case("append ties")
+    D = 64
+    x = np.zeros((2, 1, D), np.float16)
+    x[0, 0, 0] = 127.0                        # scale 1
+    x[0, 0, 1:9] = [0.5, 1.5, 2.5, -0.5, -1.5, -2.5, 126.5, -126.5]
+    x[1, 0, :4] = [127.5, -127.5, 63.5, 2.5]  # fits: clipped, the scale stays
+    table = np.array([[0]], np.int32)
+    want = O.empty_cache(1, 1, D)
+    dev = K.device(want)
+    for i in range(2):
+        O.append(want, x[i:i + 1], x[i:i + 1], np.array([0, 1]), [i + 1], table)
+        append(dev, x[i:i + 1], x[i:i + 1], [0, 1], [i + 1], table)
+    K.assert_same_cache(K.host(dev), want, table, [2], D)
+    assert want["Ks"][0, 0] == 1 and list(want["Kc"][0, 0, 1, :4]) == [255, 1, 192, 130]
+    # growth by 2^k rounds what is there to even too
+    y = np.zeros((1, 1, D), np.float16)
+    y[0, 0, 0] = 500.0
+    O.append(want, y, y, np.array([0, 1]), [3], table)
+    append(dev, y, y, [0, 1], [3], table)
+    K.assert_same_cache(K.host(dev), want, table, [3], D)
+    assert want["Ks"][0, 0] == 4
+
+
+def test_append_from_slices_of_a_fused_output_and_padded_rows():
+    case("append strided, padded rows and sequences")
+    r = np.random.default_rng(4)
+    H, D, new = 4, 96, [3, 0, 70, 1, 0]
+    before = [60, 0, 5, 128, 0]
+    after = [a + b for a, b in zip(before, new)]
+    table, pages = K.tables(r, after)
+    want = O.empty_cache(pages, H, D)
+    O.append(want, K.heads_of(r, sum(before), H, D), K.heads_of(r, sum(before), H, D),
+             K.rows_of(before), before, table)
+    dev = K.device(want)
+    cu, pad = K.rows_of(new), 9
+    x = r.normal(size=(cu[-1] + pad, 5 * H * D)).astype(np.float16)
+    x[cu[-1]:] = np.nan
+    dx = f16(x)
+    part = lambda a, i: a[:, (3 + i) * H * D:(4 + i) * H * D].reshape(len(a), H, D)
+    kd, vd = (dx[:, (3 + i) * H * D:(4 + i) * H * D].view(-1, H, D) for i in range(2))
+    assert not kd.is_contiguous()
+    O.append(want, part(x, 0), part(x, 1), cu, after, table)
+    ot.ot_kv8_append(kd, vd, K.ints(cu), K.ints(after), K.ints(table), *dev)
+    torch.cuda.synchronize()
+    K.assert_same_cache(K.host(dev), want, table, after, D)
+
+
+def test_append_leaves_out_tokens_without_a_page():
+    case("append bad pages")
+    r = np.random.default_rng(5)
+    H, D = 2, 64
+    # sequence 0's second page is none of the pool's, 1's third lies past the table, 2 has
+    # fewer tokens than rows, 3's pages are all bad
+    table = np.array([[0, 9], [1, 2], [3, -1], [-7, 1 << 30]], np.int32)
+    cu, lens = np.array([0, 100, 250, 260, 300]), [100, 150, 4, 40]
+    k, v = K.heads_of(r, 300, H, D), K.heads_of(r, 300, H, D)
+    want = O.empty_cache(5, H, D, 0x33, 2.0)
+    dev = K.device(want)
+    O.append(want, k[:64], v[:64], np.array([0, 64]), [64], table[:1])
+    O.append(want, k[100:228], v[100:228], np.array([0, 128]), [128], table[1:2])
+    O.append(want, k[256:260], v[256:260], np.array([0, 4]), [4], table[2:3])
+    append(dev, k, v, cu, lens, table)
+    got = K.host(dev)
+    K.assert_same_cache(got, want, np.array([[0, 0], [1, 2], [3, 0]]), [64, 128, 4], D)
+    for n in K.ORDER:
+        assert np.array_equal(got[n][4], want[n][4])
+
+
+# ---------------------------------------------------------------------------
+# Reading
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("H,D,lengths,start,count", [
+    (1, 64, [1], [0], [1]), (3, 64, [100], [37], [63]), (2, 80, [200, 64, 1], [0, 63, 0], [200, 1, 1]),
+    (2, 96, [130, 70], [64, 1], [66, 0]), (5, 128, [300, 10, 65], [63, 2, 64], [130, 7, 1]),
+    (3, 256, [90], [1], [88]), (2, 192, [70], [60], [10]), (2, 16, [64, 128], [0, 0], [64, 128])])
+def test_read(H, D, lengths, start, count):
+    case(f"read H={H} D={D} {lengths}")
+    r = np.random.default_rng(D)
+    cache, table = K.filled(r, lengths, H, D)
+    cu, pad = K.rows_of(count), 5
+    T = cu[-1] + pad
+    want = O.read(cache, cu, start, table, T, D)
+    got = [torch.full((T, H, D), 7.0, dtype=torch.float16, device="cuda") for _ in range(2)]
+    ot.ot_kv8_read(*K.device(cache), K.ints(cu), K.ints(start), K.ints(table), *got)
+    for g, w in zip(got, want):
+        g = g.cpu().numpy()
+        assert np.array_equal(g[:cu[-1]].view(np.uint16), w[:cu[-1]].view(np.uint16))
+        assert (g[cu[-1]:] == 7.0).all()  # rows of no sequence are as they were
+
+
+def test_read_bad_pages_and_nan_scales():
+    case("read bad pages")
+    r = np.random.default_rng(8)
+    H, D = 2, 64
+    cache, _ = K.filled(r, [64, 64, 64], H, D)
+    pages = cache["Ks"].shape[0]
+    cache["Vs"][2, 1] = np.nan
+    table = np.array([[0, pages], [1, -1], [2, 0]], np.int32)
+    cu, start = np.array([0, 200, 300, 400]), [0, -30, 10]
+    want = O.read(cache, cu, start, table, 400, D)
+    k, v = ot.kv8_read(K.device(cache), K.ints(cu), K.ints(start), K.ints(table), 400, D)
+    for g, w in zip((k, v), want):
+        assert np.array_equal(g.cpu().numpy(), w, equal_nan=True)
+    assert np.isnan(want[0][64:200]).all() and np.isfinite(want[0][:64]).all()
+
+
+# ---------------------------------------------------------------------------
+# Attention
+# ---------------------------------------------------------------------------
+def run_attend(cache, q, cu, kv_len, table, scale, causal, window, max_q, workspace, fill=7.0):
+    T, Hq, D = q.shape
+    Y = torch.full((T, Hq, D), fill, dtype=torch.float16, device="cuda")
+    lse = torch.full((T, Hq), fill, device="cuda")
+    B, H = len(kv_len), cache["Ks"].shape[1]
+    ws = None
+    if workspace:
+        n = ot.ot_attn_kv8_workspace_size(T, B, Hq, H, D, max_q)
+        ws = torch.full((n + 256,), 0xFF, dtype=torch.uint8, device="cuda")  # NaN, and a guard
+    ot.ot_attn_kv8(f16(q), K.ints(cu), K.ints(kv_len), K.ints(table), *K.device(cache), scale,
+                   causal, window, max_q, Y, lse, None if ws is None else ws[:n])
+    torch.cuda.synchronize()
+    if ws is not None:
+        assert bool((ws[n:] == 0xFF).all())
+    return Y.cpu().numpy(), lse.cpu().numpy()
+
+
+def check_attend(cache, q, cu, kv_len, table, scale=None, causal=True, window=0, max_q=None,
+                 splits=(False, True), lens=None):
+    T, Hq, D = q.shape
+    scale = D ** -0.5 if scale is None else scale
+    max_q = max(1, int(np.diff(cu).max())) if max_q is None else max_q
+    want, wlse, tol, ltol = O.attend(cache, q, cu, kv_len, table, scale, causal, window)
+    for split in splits:
+        plan = ot.ot_attn_kv8_plan(T, len(kv_len), Hq, cache["Ks"].shape[1], D, max_q, split)
+        case(f"attend T={T} Hq={Hq} D={D} causal={causal} window={window} plan={plan}")
+        Y, lse = run_attend(cache, q, cu, kv_len, table, scale, causal, window, max_q, split)
+        n = int(cu[-1])
+        assert (Y[n:] == 7.0).all() and (lse[n:] == 7.0).all()
+        g, w = Y[:n].astype(np.float64), want[:n]
+        assert np.array_equal(np.isnan(g), np.isnan(w))
+        bad = np.abs(g - w) > tol[:n]
+        assert not bad[~np.isnan(w)].any(), (float(np.nanmax(np.abs(g - w) - tol[:n])), split)
+        g, w = lse[:n].astype(np.float64), wlse[:n]
+        assert np.array_equal(np.isnan(g), np.isnan(w)) and np.array_equal(np.isinf(g), np.isinf(w))
+        fin = np.isfinite(w)
+        over = np.abs(g[fin] - w[fin]) - ltol[:n][fin]
+        assert (over <= 0).all(), float(over.max())
+
+
+def batch(seed, Hq, H, D, lengths, counts, pad=0, size=1.0):
+    r = np.random.default_rng(seed)
+    cache, table = K.filled(r, lengths, H, D)
+    cu = K.rows_of(counts)
+    q = (r.normal(size=(cu[-1] + pad, Hq, D)) * size).astype(np.float16)
+    q[cu[-1]:] = np.nan
+    return cache, q, cu, np.array(lengths), table
+
+
+DECODES = [  # query heads, key heads, channels, lengths
+    (1, 1, 64, [1]), (3, 3, 64, [64]), (12, 12, 64, [200]), (2, 2, 128, [65, 1, 700]),
+    (8, 2, 80, [130, 63, 64, 65]), (5, 1, 96, [1000]), (16, 1, 128, [300, 5]),
+    (24, 1, 128, [300, 5]), (4, 4, 256, [100, 333]), (2, 1, 192, [129]), (2, 1, 16, [77]),
+    (4, 2, 112, [0, 50, 0, 1]), (2, 2, 64, list(range(1, 140, 2))), (40, 1, 64, [90]),
+]
+
+
+@pytest.mark.parametrize("Hq,H,D,lengths", DECODES)
+def test_decode(Hq, H, D, lengths):
+    check_attend(*batch(len(lengths) + D, Hq, H, D, lengths, [1] * len(lengths), pad=3))
+
+
+@pytest.mark.parametrize("Hq,H,D,lengths,counts", [
+    (4, 1, 128, [100, 65, 7], [5, 1, 7]), (2, 2, 64, [64, 0, 200, 3], [16, 0, 2, 3]),
+    (3, 1, 80, [90, 66], [9, 4]), (8, 1, 96, [500], [4]), (1, 1, 256, [40, 129], [32, 31]),
+    (16, 2, 128, [260] * 5, [3, 1, 0, 2, 4])])
+@pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 1), (True, 70)])
+def test_few_rows(Hq, H, D, lengths, counts, causal, window):
+    check_attend(*batch(D + Hq, Hq, H, D, lengths, counts, pad=2), causal=causal, window=window)
+
+
+PROMPTS = [
+    (1, 1, 64, [40], [40]), (2, 2, 128, [129, 1, 300], [129, 1, 300]),
+    (4, 2, 80, [200, 90], [200, 60]), (8, 1, 128, [150, 64], [33, 64]), (2, 1, 256, [140], [140]),
+    (3, 1, 96, [64, 128, 65], [64, 100, 65]), (1, 1, 192, [260], [130]), (5, 5, 16, [257], [257]),
+    (4, 4, 64, [1000, 30], [128, 30]), (24, 1, 112, [90, 0], [50, 0]),
+]
+
+
+@pytest.mark.parametrize("Hq,H,D,lengths,counts", PROMPTS)
+@pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 33), (True, 200)])
+def test_prompts(Hq, H, D, lengths, counts, causal, window):
+    check_attend(*batch(D + Hq, Hq, H, D, lengths, counts, pad=4), causal=causal, window=window)
+
+
+@pytest.mark.parametrize("counts,max_q", [([5, 70], 70), ([5, 3], 5)])
+def test_rows_without_a_key(counts, max_q):
+    """More rows than tokens: the first ones stand before the first key."""
+    c = batch(3, 2, 1, 64, [3, 2], counts)
+    check_attend(*c, max_q=max_q)
+    check_attend(*c, causal=False, max_q=max_q)
+    c = batch(3, 2, 1, 64, [0, 0], counts)  # no key at all
+    check_attend(*c, max_q=max_q)
+    check_attend(*c, causal=False, max_q=max_q)
+
+
+@pytest.mark.parametrize("counts", [[4, 4], [40, 50]])
+def test_nan_behind_the_mask_is_not_seen(counts):
+    """NaN scales of pages that some rows see and others do not, of keys and of values."""
+    for name in ("Ks", "Vs"):
+        cache, q, cu, lens, table = batch(9, 2, 2, 64, [66, 258], counts)
+        cache[name][table[0, 1], 0] = np.nan    # only the last two rows see tokens 64, 65
+        cache[name][table[1, 0], 1] = np.nan    # behind a window
+        check_attend(cache, q, cu, lens, table)
+        check_attend(cache, q, cu, lens, table, window=130)
+        want = O.attend(cache, q, cu, lens, table, 0.125)[0]
+        assert np.isnan(want[:counts[0], 0]).any(1).sum() == 2
+
+
+@pytest.mark.parametrize("counts", [[1, 1, 1, 1], [40, 50, 33, 20]])
+def test_bad_pages_make_their_rows_nan(counts):
+    cache, q, cu, lens, table = batch(10, 2, 2, 64, [130, 100, 200, 300], counts)
+    pages = cache["Ks"].shape[0]
+    table[0, 1], table[1, 1], table[2, 3] = pages, -1, 1 << 30
+    table = table[:, :4]  # the last sequence has more keys than the table has pages for
+    scale = 0.125
+    want = O.attend(cache, q, cu, lens, table, scale)[0]
+    for split in (False, True):
+        Y, lse = run_attend(cache, q, cu, lens, table, scale, True, 0, max(counts), split)
+        nan = np.isnan(want).any(2)
+        nan[cu[3]:cu[4]] = True
+        assert np.array_equal(np.isnan(Y).all(2), nan) and np.array_equal(np.isnan(lse), nan)
+
+
+@pytest.mark.parametrize("counts", [[1, 1], [64, 64]])
+def test_sizes_of_scores_and_values(counts):
+    """Scores so large that one key takes all, values from fp16's smallest to its largest
+    in different pages, and pages of zeros."""
+    r = np.random.default_rng(12)
+    H, D, lens = 2, 64, [200, 130]
+    table, pages = K.tables(r, lens)
+    cache = O.empty_cache(pages, H, D, 0x5A, np.nan)
+    cu0 = K.rows_of(lens)
+    k, v = K.heads_of(r, cu0[-1], H, D, 4.0), K.heads_of(r, cu0[-1], H, D)
+    v[:64] *= np.float16(2.0 ** -14)
+    v[64:128] = np.float16(60000) * np.sign(v[64:128])
+    v[128:192] = 0
+    k[200:264] = 0
+    O.append(cache, k, v, cu0, lens, table)
+    cu = K.rows_of(counts)
+    for size in (0.01, 1.0, 30.0):
+        q = (r.normal(size=(cu[-1], 2 * H, D)) * size).astype(np.float16)
+        check_attend(cache, q, cu, lens, table)
+    check_attend(cache, q, cu, lens, table, scale=-0.05)
+    check_attend(cache, q, cu, lens, table, scale=0.0)
+
+
+def test_nonfinite_queries_stay_in_their_rows():
+    for counts in ([3, 2], [40, 33]):
+        cache, q, cu, lens, table = batch(14, 2, 1, 64, [100, 90], counts)
+        q[1, 0, 5], q[cu[1], 1, 0] = np.nan, np.inf
+        for split in (False, True):
+            Y, _ = run_attend(cache, q, cu, lens, table, 0.1, True, 0, max(counts), split)
+            nan = np.zeros((len(q), 2), bool)
+            nan[1, 0] = nan[cu[1], 1] = True
+            assert np.array_equal(np.isnan(Y).any(2), nan)
+
+
+def test_strided_queries_and_repeats():
+    case("attend strided, the same bits again")
+    r = np.random.default_rng(15)
+    H, G, D, lens, counts = 2, 2, 128, [300, 70], [1, 1]
+    cache, table = K.filled(r, lens, H, D)
+    for counts in ([1, 1], [70, 60]):
+        T = sum(counts)
+        x = torch.from_numpy(r.normal(size=(T, (G + 2) * H * D)).astype(np.float16)).cuda()
+        q = x[:, :G * H * D].view(T, G * H, D)
+        args = (K.ints(K.rows_of(counts)), K.ints(lens), K.ints(table), K.device(cache))
+        a = ot.attn_kv8(q, *args, max_q=max(counts), want_lse=True)
+        for _ in range(3):
+            b = ot.attn_kv8(q.contiguous(), *args, max_q=max(counts), want_lse=True)
+            assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])

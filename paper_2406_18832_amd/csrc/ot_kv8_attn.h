@@ -7,9 +7,10 @@
 // product of codes and queries.  O / L is the row's result; m and L are fp32.
 //
 // The weights 2^(x_j + l_j - m) are an operand of the matrix cores in fp16 (half a
-// step is 2^-11 of a weight); m lies kHeadroom binades under the largest weight, so
-// that fp16's normal numbers reach 2^-29 of it and what is lost below is under
-// 2^-29 of the largest term.  L sums the fp32 weights.
+// step is 2^-11 of a weight).  m is set kSet binades under the largest exponent and stays
+// while that grows by no more than kMost - kSet: O and L are scaled anew a few times in a
+// row's life, weights stay below 2^15, and fp16's normal numbers reach 2^-22 of the
+// largest, what is lost below is at most 2^-33 of it for a key.  L sums the fp32 weights.
 //
 // Which weight belongs to which token.  S^T = K Q^T has tokens as the MFMA's rows
 // and queries as its columns, and leaves a lane with weights of one query alone,
@@ -22,7 +23,7 @@
 namespace ot {
 namespace detail {
 
-constexpr float kHeadroom = 15.f;
+constexpr float kSet = 8.f, kMost = 15.f;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kNegInf = -__builtin_inff();
@@ -40,6 +41,22 @@ __device__ __forceinline__ void value_scale(float s, float &lg, float &inv) {
 
 __device__ __forceinline__ v2h pack_half(float a, float b) {
   return v2h{(_Float16)a, (_Float16)b};  // each to nearest even
+}
+
+// The maximum over the lanes of one query: xor 16 and xor 32, or xor 32 alone.  A swap
+// of a register's rows with those of its copy leaves each lane the other's value.
+__device__ __forceinline__ float max_xor16(float v) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, v);
+  const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+}
+__device__ __forceinline__ float max_xor32(float v) {
+  const uint32_t u = __builtin_bit_cast(uint32_t, v);
+  const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+}
+__device__ __forceinline__ float lane_float(float v, int lane) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
 }
 
 // How the pages of a batch are shared out between workgroups.  An item is a run of
@@ -72,44 +89,44 @@ __device__ __forceinline__ int kv8_shared_pages(const Kv8Seq &s) {
   return s.rows.n == 0 ? 0 : max(s.span.p1 - s.span.p0, 1);
 }
 
-__device__ __forceinline__ int wave_sum(int v) {
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off);
-  return v;
+// Inclusive sums along the lanes (DPP: no LDS); lane 63 has the wave's.
+template <int kCtrl, int kRows>
+__device__ __forceinline__ int dpp_add(int v) {
+  return v + __builtin_amdgcn_update_dpp(0, v, kCtrl, kRows, 0xf, false);
+}
+__device__ __forceinline__ int wave_upto(int v) {
+  v = dpp_add<0x111, 0xf>(v);  // row_shr:1, 2, 4, 8
+  v = dpp_add<0x112, 0xf>(v);
+  v = dpp_add<0x114, 0xf>(v);
+  v = dpp_add<0x118, 0xf>(v);
+  v = dpp_add<0x142, 0xa>(v);  // row_bcast:15 to rows 1 and 3
+  return dpp_add<0x143, 0xc>(v);  // row_bcast:31 to rows 2 and 3
 }
 
-// chunk: the smallest that makes at most `wanted` items and one more per sequence,
-// but `least`; wanted 0: every sequence is one item.
-__device__ __forceinline__ int kv8_chunk(const Kv8Attn &a, int lane, int wanted, int least) {
-  if (wanted == 0) return 1 << 30;
-  int64_t total = 0;
-  for (int b0 = 0; b0 < a.B; b0 += 64) {
-    const int b = b0 + lane;
-    total += wave_sum(b < a.B ? kv8_shared_pages(kv8_seq(a, b)) : 0);
-  }
-  return (int)kv8_max(least, (total + wanted - 1) / wanted);
-}
-
+// Item x.  The pages per item: the fewest that make at most `wanted` items and one more
+// per sequence, but `least`; wanted 0: every sequence is one item.
 __device__ __forceinline__ Kv8Item kv8_item(const Kv8Attn &a, int lane, int x, int wanted,
                                             int least) {
-  const int chunk = kv8_chunk(a, lane, wanted, least);
+  if (wanted == 0) return {x < a.B ? x : -1, 0, 1 << 30, x, 1};
+  int pages = lane < a.B ? kv8_shared_pages(kv8_seq(a, lane)) : 0;
+  int64_t total = __builtin_amdgcn_readlane(wave_upto(pages), 63);
+  for (int b = 64; b < a.B; b += 64)
+    total += __builtin_amdgcn_readlane(
+        wave_upto(b + lane < a.B ? kv8_shared_pages(kv8_seq(a, b + lane)) : 0), 63);
+  const int chunk = (int)kv8_max(least, (total + wanted - 1) / wanted);
   int before = 0;
   for (int b0 = 0; b0 < a.B; b0 += 64) {
-    const int b = b0 + lane;
-    const int own = b < a.B ? (kv8_shared_pages(kv8_seq(a, b)) + chunk - 1) / chunk : 0;
-    int upto = own;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-      const int o = __shfl_up(upto, off);
-      if (lane >= off) upto += o;
-    }
+    if (b0 > 0) pages = b0 + lane < a.B ? kv8_shared_pages(kv8_seq(a, b0 + lane)) : 0;
+    const int own = (int)((unsigned)(pages + chunk - 1) / (unsigned)chunk);
+    const int upto = wave_upto(own);
     const uint64_t past = __ballot(before + upto > x);
     if (past != 0) {
       const int at = __builtin_ctzll(past);
-      const int count = __shfl(own, at), first = before + __shfl(upto, at) - count;
+      const int count = __builtin_amdgcn_readlane(own, at);
+      const int first = before + __builtin_amdgcn_readlane(upto, at) - count;
       return {b0 + at, x - first, chunk, first, count};
     }
-    before += __shfl(upto, 63);
+    before += __builtin_amdgcn_readlane(upto, 63);
   }
   return {-1, 0, chunk, 0, 0};
 }
@@ -125,7 +142,7 @@ __device__ __forceinline__ int64_t kv8_partial(int64_t item, int64_t h, int64_t 
 // Partial results of a split launch: `items` runs of pages, `rows` rows to each key
 // head.  spans [B] says which items a sequence has.
 struct Kv8Split {
-  int wanted, least;  // as kv8_chunk; wanted 0: no split
+  int wanted, least;  // as kv8_item; wanted 0: no split
   int64_t items, rows;
   float *m, *l, *o;
   int2 *spans;

@@ -13,6 +13,8 @@
 // V^T's rows are channels, its 16 bytes of a lane are tokens 16 g .. of one channel.
 #include <math.h>
 
+#include <type_traits>
+
 #include "ot_kv8_attn.h"
 
 namespace ot {
@@ -20,8 +22,14 @@ namespace detail {
 
 constexpr int kDecodeWaves = 4;
 
+// Waves to a SIMD that the registers are for.
+constexpr int decode_waves(int dp, int rt) {
+  if (rt == 2) return 2;
+  return dp <= 64 ? 4 : dp <= 128 ? 3 : dp <= 192 ? 2 : 1;
+}
+
 template <int DP, int RT>
-__global__ __launch_bounds__(64 * kDecodeWaves) void kv8_decode_kernel(Kv8Attn a, Kv8Split s) {
+__global__ __launch_bounds__(64 * kDecodeWaves, decode_waves(DP, RT)) void kv8_decode_kernel(Kv8Attn a, Kv8Split s) {
   constexpr int kChunks = DP / 64, kTail = DP % 64 / 32;  // of a key's row
   constexpr int kSteps = DP / 32, kOut = DP / 16;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -76,45 +84,57 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void kv8_decode_kernel(Kv8Attn a
     for (int t = 0; t < kOut; ++t) o[r][t] = v4f{0.f, 0.f, 0.f, 0.f};
   }
   const float fac = a.scale * kLog2e;
+  const int key_at = (16 * (col >> 2) + (col & 3)) * DP + 16 * g, value_at = col * kKv8Page + 16 * g;
 
-  // 64 of this wave's pages at a time: lane i has the i-th one's number and scales
+  // 64 of this wave's pages at a time: lane i has the i-th one's number and scales.  A
+  // page's keys are fetched while the one before goes through softmax and values, its
+  // values from there until its own scores are there: both take the registers that the
+  // page before has just left.
   for (int64_t batch = p0 + wave; batch < p1; batch += 64 * kDecodeWaves) {
     const int64_t mine = batch + kDecodeWaves * lane;
+    const int todo = (int)kv8_min(64, (p1 - batch + kDecodeWaves - 1) / kDecodeWaves);
     int64_t page = -1;
-    float ks = __builtin_nanf(""), vs = 0.f;
-    if (mine < p1) {
+    if (mine < p1)
       page = kv8_page(a.cache.table, item.b, mine, a.cache.max_pages, a.cache.num_pages);
-      if (page >= 0) {
-        ks = a.cache.Ks[page * a.Hkv + h];
-        vs = a.cache.Vs[page * a.Hkv + h];
+    const bool none = page < 0;
+    const int at = none ? 0 : (int)page;  // its scale is NaN: what sees it is
+    v4u kc[4][kChunks > 0 ? kChunks : 1];
+    v2u kt[4];
+    v4u vc[kOut];
+    auto load_keys = [&](int n) {
+      const int64_t ph = (int64_t)__builtin_amdgcn_readlane(at, n) * a.Hkv + h;
+      const __amdgpu_buffer_rsrc_t keys = make_rsrc(a.cache.Kc + ph * (DP * kKv8Page), DP * kKv8Page);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c)
+          kc[t][c] = __builtin_amdgcn_raw_buffer_load_b128(keys, key_at, 4 * t * DP + 64 * c, 0);
+        if constexpr (kTail != 0)
+          kt[t] = __builtin_amdgcn_raw_buffer_load_b64(keys, key_at - 8 * g, 4 * t * DP + 64 * kChunks, 0);
       }
+    };
+    auto load_values = [&](int n) {
+      const int64_t ph = (int64_t)__builtin_amdgcn_readlane(at, n) * a.Hkv + h;
+      const __amdgpu_buffer_rsrc_t values = make_rsrc(a.cache.Vc + ph * (DP * kKv8Page), DP * kKv8Page);
+#pragma unroll
+      for (int t = 0; t < kOut; ++t)
+        vc[t] = __builtin_amdgcn_raw_buffer_load_b128(values, value_at, 1024 * t, 0);
+    };
+    float ks = __builtin_nanf(""), vs = 0.f;
+    if (!none) {
+      ks = a.cache.Ks[page * a.Hkv + h];
+      vs = a.cache.Vs[page * a.Hkv + h];
     }
-    if (page < 0) page = 0;  // its scale is NaN: what sees it is
+    load_keys(0);
+    load_values(0);
     float lg, inv;
     value_scale(vs, lg, inv);
     ks = seq.bad ? __builtin_nanf("") : ks * fac;
-    const int todo = (int)kv8_min(64, (p1 - batch + kDecodeWaves - 1) / kDecodeWaves);
-    for (int n = 0; n < todo; ++n) {
-      const int64_t ph = (int64_t)__builtin_amdgcn_readlane((int)page, n) * a.Hkv + h;
-      const float f = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, ks), n));
-      const float lgv = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, lg), n));
-      const float iv = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, inv), n));
-      const uint8_t *kp = a.cache.Kc + ph * (DP * kKv8Page);
-      const uint8_t *vp = a.cache.Vc + ph * (DP * kKv8Page);
-      v4u kc[4][kChunks > 0 ? kChunks : 1];
-      v2u kt[4];
-      v4u vc[kOut];
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        const uint8_t *p = kp + (16 * (col >> 2) + 4 * t + (col & 3)) * DP;
-#pragma unroll
-        for (int c = 0; c < kChunks; ++c) kc[t][c] = *reinterpret_cast<const v4u *>(p + 64 * c + 16 * g);
-        if constexpr (kTail) kt[t] = *reinterpret_cast<const v2u *>(p + 64 * kChunks + 8 * g);
-      }
-#pragma unroll
-      for (int t = 0; t < kOut; ++t)
-        vc[t] = *reinterpret_cast<const v4u *>(vp + (16 * t + col) * kKv8Page + 16 * g);
 
+    // keeps the scheduler from fetching into fresh registers, which there are none of
+    auto phase = [] { __builtin_amdgcn_sched_barrier(0); };
+    auto one_page = [&](int n, auto more) {
+      const float f = lane_float(ks, n), lgv = lane_float(lg, n), iv = lane_float(inv, n);
       v4f x[RT][4];
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
@@ -133,7 +153,11 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void kv8_decode_kernel(Kv8Attn a
           for (int r = 0; r < RT; ++r)
             x[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, q[r][st], x[r][t], 0, 0, 0);
         }
+        if (DP * RT >= 128) phase();
       }
+      phase();
+      if constexpr (more) load_keys(n + 1);
+      phase();
       const int token = (int)((batch + kDecodeWaves * n) * kKv8Page);
       const bool cut = token < all_lo || token + kKv8Page - 1 > all_hi;
       v8h p[RT][2];
@@ -143,20 +167,31 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void kv8_decode_kernel(Kv8Attn a
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float v = __builtin_fmaf(x[r][t][i], f, lgv);
-            const int key = token + 16 * g + 4 * t + i;
-            if (cut && (key < key_lo[r] || key > key_hi[r])) v = kNegInf;
-            x[r][t][i] = v;
-            most = fmaxf(most, v);
-          }
+          for (int i = 0; i < 4; ++i) x[r][t][i] = __builtin_fmaf(x[r][t][i], f, lgv);
         }
-        most = fmaxf(most, __shfl_xor(most, 16));
-        most = fmaxf(most, __shfl_xor(most, 32));
-        const float now = fmaxf(m[r], most - kHeadroom);
-        const float ref = now == kNegInf ? 0.f : now;  // no key yet
-        const float keep = exp2_fast(m[r] - ref);
-        m[r] = now;
+        if (cut) {
+#pragma unroll
+          for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int key = token + 16 * g + 4 * t + i;
+              if (key < key_lo[r] || key > key_hi[r]) x[r][t][i] = kNegInf;
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) most = fmaxf(most, x[r][t][i]);
+        most = max_xor32(max_xor16(most));
+        if (__any(most > m[r] + kMost)) {
+          const float now = most > m[r] + kMost ? most - kSet : m[r];
+          const float keep = m[r] == now ? 1.f : exp2_fast(m[r] - now);
+          m[r] = now;
+          l[r] *= keep;
+#pragma unroll
+          for (int t = 0; t < kOut; ++t) o[r][t] *= keep;
+        }
+        const float ref = m[r] == kNegInf ? 0.f : m[r];  // no key yet
         float sum = 0.f;
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
@@ -172,10 +207,9 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void kv8_decode_kernel(Kv8Attn a
           p[r][t >> 1][4 * (t & 1) + 2] = hi[0];
           p[r][t >> 1][4 * (t & 1) + 3] = hi[1];
         }
-        l[r] = __builtin_fmaf(l[r], keep, sum * iv);
-#pragma unroll
-        for (int t = 0; t < kOut; ++t) o[r][t] *= keep;
+        l[r] = __builtin_fmaf(sum, iv, l[r]);
       }
+      phase();
 #pragma unroll
       for (int t = 0; t < kOut; ++t) {
         const v8h v0 = kv8_halves(vc[t][0], vc[t][1]), v1 = kv8_halves(vc[t][2], vc[t][3]);
@@ -184,8 +218,14 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void kv8_decode_kernel(Kv8Attn a
           o[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, p[r][0], o[r][t], 0, 0, 0);
           o[r][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, p[r][1], o[r][t], 0, 0, 0);
         }
+        if (DP * RT >= 128 && t % 2 == 1) phase();
       }
-    }
+      phase();
+      if constexpr (more) load_values(n + 1);
+      phase();
+    };
+    for (int n = 0; n + 1 < todo; ++n) one_page(n, std::true_type{});
+    one_page(todo - 1, std::false_type{});
   }
 
   // The waves' results meet, some channels at a time; only rows that exist are written.
@@ -260,46 +300,81 @@ __global__ __launch_bounds__(64 * kDecodeWaves) void kv8_decode_kernel(Kv8Attn a
   }
 }
 
-// The items of a sequence joined: a wave to a query row.
+// The items of a sequence joined: a workgroup to a query row of a key head, its waves
+// to the items in turn, eight items' loads at a time.
 template <int DP>
 __global__ __launch_bounds__(256) void kv8_combine_kernel(Kv8Attn a, Kv8Split s) {
-  const int lane = threadIdx.x & 63, b = blockIdx.y;
+  constexpr int kPer = (DP + 63) / 64, kAhead = 8;
+  __shared__ float meet[4][2 + 64 * kPer];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int row = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
   const int G = a.Hq / a.Hkv;
   const Kv8Rows rows = kv8_rows(a.cu[b], a.cu[b + 1], a.T);
-  const int which = blockIdx.x * 4 + (threadIdx.x >> 6);  // (key head, row)
-  const int h = which / (int)s.rows, row = which % (int)s.rows;
-  if (h >= a.Hkv || row >= min(rows.n, a.max_q) * G) return;
+  if (row >= min(rows.n, a.max_q) * G) return;
   const int2 span = s.spans[b];
   if (span.y <= 1) return;
-  float ref = kNegInf;
-  for (int c = lane; c < span.y; c += 64)
-    ref = fmaxf(ref, s.m[kv8_partial(span.x + c, h, row, a.Hkv, s.rows)]);
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) ref = fmaxf(ref, __shfl_xor(ref, off));
-  const float top = ref;
-  if (ref == kNegInf) ref = 0.f;
-  constexpr int kPer = (DP + 63) / 64;
-  float sum = 0.f, out[kPer];
+  const int64_t base = kv8_partial(span.x, h, row, a.Hkv, s.rows), step = a.Hkv * s.rows;
+  float top = kNegInf, sum = 0.f, out[kPer];
 #pragma unroll
   for (int i = 0; i < kPer; ++i) out[i] = 0.f;
-  for (int c = 0; c < span.y; ++c) {
-    const int64_t at = kv8_partial(span.x + c, h, row, a.Hkv, s.rows);
-    const float part = exp2_fast(s.m[at] - ref);
-    sum = __builtin_fmaf(part, s.l[at], sum);
+  for (int c0 = wave * kAhead; c0 < span.y; c0 += 4 * kAhead) {
+    float m[kAhead], l[kAhead], v[kAhead][kPer];
 #pragma unroll
-    for (int i = 0; i < kPer; ++i)
-      if (64 * i + lane < a.D) out[i] = __builtin_fmaf(part, s.o[at * DP + 64 * i + lane], out[i]);
+    for (int j = 0; j < kAhead; ++j) {
+      const bool in = c0 + j < span.y;
+      const int64_t at = base + (in ? c0 + j : c0) * step;
+      m[j] = in ? s.m[at] : kNegInf;
+      l[j] = in ? s.l[at] : 0.f;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const int d = 64 * i + lane;
+        v[j][i] = in && (DP % 64 == 0 || d < DP) ? s.o[at * DP + d] : 0.f;
+      }
+    }
+    float now = top;
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) now = fmaxf(now, m[j]);
+    const float ref = now == kNegInf ? 0.f : now, keep = exp2_fast(top - ref);
+    top = now;
+    sum *= keep;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) out[i] *= keep;
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const float part = exp2_fast(m[j] - ref);
+      sum = __builtin_fmaf(part, l[j], sum);
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) out[i] = __builtin_fmaf(part, v[j][i], out[i]);
+    }
   }
+  if (lane == 0) {
+    meet[wave][0] = top;
+    meet[wave][1] = sum;
+  }
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) meet[wave][2 + 64 * i + lane] = out[i];
+  __syncthreads();
   const int i = row / G, head = h * G + row % G;
   const int64_t len = kv8_len(a.kv_len[b], a.cache.max_pages);
   const bool empty = len == 0 || (a.causal && len - rows.n + i < 0);
   const int64_t at = (int64_t)(rows.row0 + i) * a.Hq + head;
-  const float scale = 1.f / sum;
+  top = fmaxf(fmaxf(meet[0][0], meet[1][0]), fmaxf(meet[2][0], meet[3][0]));
+  const float ref = top == kNegInf ? 0.f : top;
+  float part[4];
+  sum = 0.f;
 #pragma unroll
-  for (int j = 0; j < kPer; ++j)
-    if (64 * j + lane < a.D)
-      a.Y[at * a.D + 64 * j + lane] = empty ? 0 : float_to_half_bits(out[j] * scale);
-  if (lane == 0 && a.lse != nullptr) a.lse[at] = empty ? kNegInf : (top + log2f(sum)) * kLn2;
+  for (int w = 0; w < 4; ++w) {
+    part[w] = exp2_fast(meet[w][0] - ref);
+    sum = __builtin_fmaf(part[w], meet[w][1], sum);
+  }
+  const int d = threadIdx.x;
+  if (d < a.D) {
+    float y = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) y = __builtin_fmaf(part[w], meet[w][2 + d], y);
+    a.Y[at * a.D + d] = empty ? 0 : float_to_half_bits(y * (1.f / sum));
+  }
+  if (d == 0 && a.lse != nullptr) a.lse[at] = empty ? kNegInf : (top + log2f(sum)) * kLn2;
 }
 
 template <int DP, int RT>
@@ -311,8 +386,10 @@ hipError_t decode_launch(const Kv8Attn &a, int64_t max_rows, const Kv8Split &s, 
 
 template <int DP>
 hipError_t decode_width(const Kv8Attn &a, int64_t max_rows, const Kv8Split &s, hipStream_t st) {
-  return max_rows <= 16 ? decode_launch<DP, 1>(a, max_rows, s, st)
-                        : decode_launch<DP, 2>(a, max_rows, s, st);
+  // two products' rows to a workgroup, where their registers leave two waves to a SIMD
+  if constexpr (DP <= 128)
+    if (max_rows > 16) return decode_launch<DP, 2>(a, max_rows, s, st);
+  return decode_launch<DP, 1>(a, max_rows, s, st);
 }
 
 }  // namespace detail
@@ -329,7 +406,7 @@ hipError_t launch_kv8_decode(const Kv8Attn &a, const Kv8Split &s, hipStream_t st
 }
 
 hipError_t launch_kv8_combine(const Kv8Attn &a, const Kv8Split &s, hipStream_t st) {
-  const dim3 grid((unsigned)((a.Hkv * s.rows + 3) / 4), (unsigned)a.B);
+  const dim3 grid((unsigned)s.rows, (unsigned)a.Hkv, (unsigned)a.B);
   switch (kv8_width(a.D)) {
     case 64: detail::kv8_combine_kernel<64><<<grid, 256, 0, st>>>(a, s); break;
     case 96: detail::kv8_combine_kernel<96><<<grid, 256, 0, st>>>(a, s); break;

@@ -138,11 +138,16 @@ __global__ __launch_bounds__(64 * kTileWaves) void kv8_tile_kernel(Kv8Attn a) {
         x[t][i] = v;
         most = fmaxf(most, v);
       }
-    most = fmaxf(most, __shfl_xor(most, 32));
-    const float now = fmaxf(m, most - kHeadroom);
-    const float ref = now == kNegInf ? 0.f : now;
-    const float keep = exp2_fast(m - ref);
-    m = now;
+    most = max_xor32(most);
+    if (__any(most > m + kMost)) {
+      const float now = most > m + kMost ? most - kSet : m;
+      const float keep = m == now ? 1.f : exp2_fast(m - now);
+      m = now;
+      l *= keep;
+#pragma unroll
+      for (int t = 0; t < kOut; ++t) o[t] *= keep;
+    }
+    const float ref = m == kNegInf ? 0.f : m;  // no key yet
     float sum = 0.f;
     v8h w[4];
 #pragma unroll
@@ -153,9 +158,7 @@ __global__ __launch_bounds__(64 * kTileWaves) void kv8_tile_kernel(Kv8Attn a) {
         sum += e;
         w[2 * t + (i >> 3)][i & 7] = (_Float16)e;
       }
-    l = __builtin_fmaf(l, keep, sum * piv);
-#pragma unroll
-    for (int t = 0; t < kOut; ++t) o[t] *= keep;
+    l = __builtin_fmaf(sum, piv, l);
 #pragma unroll
     for (int t = 0; t < kOut; ++t)
 #pragma unroll

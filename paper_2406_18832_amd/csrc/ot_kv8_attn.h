@@ -103,8 +103,10 @@ __device__ __forceinline__ int wave_upto(int v) {
   return dpp_add<0x143, 0xc>(v);  // row_bcast:31 to rows 2 and 3
 }
 
-// Item x.  The pages per item: the fewest that make at most `wanted` items and one more
-// per sequence, but `least`; wanted 0: every sequence is one item.
+// Item x.  Pages per item: the fewest, but `least`, that make at most `wanted` items (as
+// many as run at a time) where that many leave each sequence one; else those of which
+// `wanted` make all pages.  Items are then at most `wanted` and one per sequence.  wanted
+// 0: every sequence is one item.
 __device__ __forceinline__ Kv8Item kv8_item(const Kv8Attn &a, int lane, int x, int wanted,
                                             int least) {
   if (wanted == 0) return {x < a.B ? x : -1, 0, 1 << 30, x, 1};
@@ -113,7 +115,21 @@ __device__ __forceinline__ Kv8Item kv8_item(const Kv8Attn &a, int lane, int x, i
   for (int b = 64; b < a.B; b += 64)
     total += __builtin_amdgcn_readlane(
         wave_upto(b + lane < a.B ? kv8_shared_pages(kv8_seq(a, b + lane)) : 0), 63);
-  const int chunk = (int)kv8_max(least, (total + wanted - 1) / wanted);
+  int chunk = (int)kv8_max(least, (total + wanted - 1) / wanted);
+  if (a.B <= 64 && a.B <= wanted) {
+    // between these two: with the larger, rounding up cannot make too many
+    int most = (int)kv8_max(chunk, wanted > a.B ? (total + wanted - a.B - 1) / (wanted - a.B) : 1 << 30);
+    const auto items = [&](int c) {
+      return __builtin_amdgcn_readlane(wave_upto((int)((unsigned)(pages + c - 1) / (unsigned)c)), 63);
+    };
+    while (chunk < most) {
+      const int half = chunk + (most - chunk) / 2;
+      if (items(half) <= wanted)
+        most = half;
+      else
+        chunk = half + 1;
+    }
+  }
   int before = 0;
   for (int b0 = 0; b0 < a.B; b0 += 64) {
     if (b0 > 0) pages = b0 + lane < a.B ? kv8_shared_pages(kv8_seq(a, b0 + lane)) : 0;
@@ -138,6 +154,13 @@ __device__ __forceinline__ int64_t kv8_partial(int64_t item, int64_t h, int64_t 
 }
 
 }  // namespace detail
+
+// The kernel for few rows: 16-row tiles that a workgroup takes (two, where their
+// registers leave two waves to a SIMD), and the workgroups that a CU holds.
+constexpr int kv8_decode_tiles(int dp, int64_t rows) { return rows > 16 && dp <= 128 ? 2 : 1; }
+constexpr int kv8_decode_waves(int dp, int tiles) {
+  return tiles == 2 || dp == 192 ? 2 : dp <= 64 ? 4 : dp <= 128 ? 3 : 1;
+}
 
 // Partial results of a split launch: `items` runs of pages, `rows` rows to each key
 // head.  spans [B] says which items a sequence has.

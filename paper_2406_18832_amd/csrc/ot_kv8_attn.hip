@@ -8,8 +8,9 @@ namespace {
 
 // Up to so many query rows to a key head and sequence the kernel for few rows runs.
 constexpr int64_t kFewRows = 32;
-// Workgroups that it should have to fill the card, and pages to an item, at least.
-constexpr int kGroupsPerCu = 4, kLeastPages = 4;
+// Pages to an item, at least, and pages of a sequence up to which it is not split: a
+// second launch takes as long as a workgroup's waves take for so many.
+constexpr int kLeastPages = 4, kWholePages = 16;
 
 bool few_rows(int64_t G, int64_t max_q) { return max_q * G <= kFewRows; }
 
@@ -21,13 +22,15 @@ size_t plan_split(int64_t B, int64_t Hq, int64_t Hkv, int64_t D, int64_t max_q, 
   s.rows = max_q * G;
   s.least = kLeastPages;
   if (!few_rows(G, max_q)) return 0;
-  const int64_t wanted = (int64_t)device_cus() * kGroupsPerCu / Hkv;
-  if (wanted <= B / 4) return 0;  // the sequences fill the card
+  // as many workgroups as run at a time
+  const int dp = kv8_width(D), tiles = kv8_decode_tiles(dp, s.rows);
+  const int64_t per_item = Hkv * ((s.rows + 16 * tiles - 1) / (16 * tiles));
+  const int64_t wanted = (int64_t)device_cus() * kv8_decode_waves(dp, tiles) / per_item;
   s.wanted = (int)(wanted > 0 ? wanted : 1);
   s.items = s.wanted + B;
   const int64_t rows = s.items * Hkv * s.rows;
   return (size_t)(B + (B & 1)) * sizeof(int2) + (size_t)(rows + (rows & 1)) * 2 * sizeof(float) +
-         (size_t)rows * kv8_width(D) * sizeof(float);
+         (size_t)rows * dp * sizeof(float);
 }
 
 }  // namespace
@@ -50,7 +53,7 @@ hipError_t launch_attn_kv8(const Kv8Attn &a, void *workspace, hipStream_t st) {
   if (!few_rows(a.Hq / a.Hkv, a.max_q)) return launch_kv8_tiles(a, st);
   Kv8Split s;
   const size_t bytes = plan_split(a.B, a.Hq, a.Hkv, a.D, a.max_q, s);
-  if (workspace == nullptr || bytes == 0) {
+  if (workspace == nullptr || bytes == 0 || a.cache.max_pages <= kWholePages) {
     s.wanted = 0;
     s.items = a.B;
     return launch_kv8_decode(a, s, st);

@@ -21,15 +21,10 @@ namespace ot {
 namespace detail {
 
 constexpr int kDecodeWaves = 4;
-
-// Waves to a SIMD that the registers are for.
-constexpr int decode_waves(int dp, int rt) {
-  if (rt == 2) return 2;
-  return dp <= 64 ? 4 : dp <= 128 ? 3 : dp <= 192 ? 2 : 1;
-}
+constexpr int kNonTemporal = 2;  // buffer load hint: codes are read once
 
 template <int DP, int RT>
-__global__ __launch_bounds__(64 * kDecodeWaves, decode_waves(DP, RT)) void kv8_decode_kernel(Kv8Attn a, Kv8Split s) {
+__global__ __launch_bounds__(64 * kDecodeWaves, kv8_decode_waves(DP, RT)) void kv8_decode_kernel(Kv8Attn a, Kv8Split s) {
   constexpr int kChunks = DP / 64, kTail = DP % 64 / 32;  // of a key's row
   constexpr int kSteps = DP / 32, kOut = DP / 16;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -108,9 +103,9 @@ __global__ __launch_bounds__(64 * kDecodeWaves, decode_waves(DP, RT)) void kv8_d
       for (int t = 0; t < 4; ++t) {
 #pragma unroll
         for (int c = 0; c < kChunks; ++c)
-          kc[t][c] = __builtin_amdgcn_raw_buffer_load_b128(keys, key_at, 4 * t * DP + 64 * c, 0);
+          kc[t][c] = __builtin_amdgcn_raw_buffer_load_b128(keys, key_at, 4 * t * DP + 64 * c, kNonTemporal);
         if constexpr (kTail != 0)
-          kt[t] = __builtin_amdgcn_raw_buffer_load_b64(keys, key_at - 8 * g, 4 * t * DP + 64 * kChunks, 0);
+          kt[t] = __builtin_amdgcn_raw_buffer_load_b64(keys, key_at - 8 * g, 4 * t * DP + 64 * kChunks, kNonTemporal);
       }
     };
     auto load_values = [&](int n) {
@@ -118,7 +113,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, decode_waves(DP, RT)) void kv8_d
       const __amdgpu_buffer_rsrc_t values = make_rsrc(a.cache.Vc + ph * (DP * kKv8Page), DP * kKv8Page);
 #pragma unroll
       for (int t = 0; t < kOut; ++t)
-        vc[t] = __builtin_amdgcn_raw_buffer_load_b128(values, value_at, 1024 * t, 0);
+        vc[t] = __builtin_amdgcn_raw_buffer_load_b128(values, value_at, 1024 * t, kNonTemporal);
     };
     float ks = __builtin_nanf(""), vs = 0.f;
     if (!none) {
@@ -300,81 +295,95 @@ __global__ __launch_bounds__(64 * kDecodeWaves, decode_waves(DP, RT)) void kv8_d
   }
 }
 
-// The items of a sequence joined: a workgroup to a query row of a key head, its waves
-// to the items in turn, eight items' loads at a time.
+// The items of a sequence joined: a wave to a query row of a key head at a time, or four
+// (`team`) where there are many items, which they take in turn, eight items' loads at a
+// time.
 template <int DP>
 __global__ __launch_bounds__(256) void kv8_combine_kernel(Kv8Attn a, Kv8Split s) {
   constexpr int kPer = (DP + 63) / 64, kAhead = 8;
   __shared__ float meet[4][2 + 64 * kPer];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int row = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
-  const int G = a.Hq / a.Hkv;
+  const int b = blockIdx.y, G = a.Hq / a.Hkv;
   const Kv8Rows rows = kv8_rows(a.cu[b], a.cu[b + 1], a.T);
-  if (row >= min(rows.n, a.max_q) * G) return;
+  if (rows.n == 0) return;
   const int2 span = s.spans[b];
   if (span.y <= 1) return;
-  const int64_t base = kv8_partial(span.x, h, row, a.Hkv, s.rows), step = a.Hkv * s.rows;
-  float top = kNegInf, sum = 0.f, out[kPer];
+  const int64_t len = kv8_len(a.kv_len[b], a.cache.max_pages);
+  const int mine = min(rows.n, a.max_q) * G, all = a.Hkv * mine;
+  const int team = span.y > 2 * kAhead ? 4 : 1, first = team == 4 ? wave : 0;
+  for (int base = blockIdx.x * (4 / team); base < all; base += gridDim.x * (4 / team)) {
+    const int which = team == 4 ? base : min(base + wave, all - 1);
+    const int h = which / mine, row = which % mine;
+    const int64_t from = kv8_partial(span.x, h, row, a.Hkv, s.rows), step = a.Hkv * s.rows;
+    float top = kNegInf, sum = 0.f, out[kPer];
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) out[i] = 0.f;
-  for (int c0 = wave * kAhead; c0 < span.y; c0 += 4 * kAhead) {
-    float m[kAhead], l[kAhead], v[kAhead][kPer];
+    for (int i = 0; i < kPer; ++i) out[i] = 0.f;
+    for (int c0 = first * kAhead; c0 < span.y; c0 += team * kAhead) {
+      float m[kAhead], l[kAhead], v[kAhead][kPer];
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) {
-      const bool in = c0 + j < span.y;
-      const int64_t at = base + (in ? c0 + j : c0) * step;
-      m[j] = in ? s.m[at] : kNegInf;
-      l[j] = in ? s.l[at] : 0.f;
+      for (int j = 0; j < kAhead; ++j) {
+        const bool in = c0 + j < span.y;
+        const int64_t at = from + (in ? c0 + j : c0) * step;
+        m[j] = in ? s.m[at] : kNegInf;
+        l[j] = in ? s.l[at] : 0.f;
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        const int d = 64 * i + lane;
-        v[j][i] = in && (DP % 64 == 0 || d < DP) ? s.o[at * DP + d] : 0.f;
+        for (int i = 0; i < kPer; ++i) {
+          const int d = 64 * i + lane;
+          v[j][i] = in && (DP % 64 == 0 || d < DP) ? s.o[at * DP + d] : 0.f;
+        }
+      }
+      float now = top;
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) now = fmaxf(now, m[j]);
+      const float ref = now == kNegInf ? 0.f : now, keep = exp2_fast(top - ref);
+      top = now;
+      sum *= keep;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) out[i] *= keep;
+#pragma unroll
+      for (int j = 0; j < kAhead; ++j) {
+        const float part = exp2_fast(m[j] - ref);
+        sum = __builtin_fmaf(part, l[j], sum);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) out[i] = __builtin_fmaf(part, v[j][i], out[i]);
       }
     }
-    float now = top;
+    if (team == 4) {
+      __syncthreads();  // the row before is done with
+      if (lane == 0) {
+        meet[wave][0] = top;
+        meet[wave][1] = sum;
+      }
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) now = fmaxf(now, m[j]);
-    const float ref = now == kNegInf ? 0.f : now, keep = exp2_fast(top - ref);
-    top = now;
-    sum *= keep;
+      for (int i = 0; i < kPer; ++i) meet[wave][2 + 64 * i + lane] = out[i];
+      __syncthreads();
+      if (wave != 0) continue;
+      top = fmaxf(fmaxf(meet[0][0], meet[1][0]), fmaxf(meet[2][0], meet[3][0]));
+      const float ref = top == kNegInf ? 0.f : top;
+      sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) out[i] *= keep;
+      for (int i = 0; i < kPer; ++i) out[i] = 0.f;
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) {
-      const float part = exp2_fast(m[j] - ref);
-      sum = __builtin_fmaf(part, l[j], sum);
+      for (int w = 0; w < 4; ++w) {
+        const float part = exp2_fast(meet[w][0] - ref);
+        sum = __builtin_fmaf(part, meet[w][1], sum);
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) out[i] = __builtin_fmaf(part, v[j][i], out[i]);
+        for (int i = 0; i < kPer; ++i)
+          out[i] = __builtin_fmaf(part, meet[w][2 + 64 * i + lane], out[i]);
+      }
+    } else if (base + wave >= all) {
+      continue;
     }
-  }
-  if (lane == 0) {
-    meet[wave][0] = top;
-    meet[wave][1] = sum;
-  }
+    const int i = row / G, head = h * G + row % G;
+    const bool empty = len == 0 || (a.causal && len - rows.n + i < 0);
+    const int64_t at = (int64_t)(rows.row0 + i) * a.Hq + head;
+    const float scale = 1.f / sum;
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) meet[wave][2 + 64 * i + lane] = out[i];
-  __syncthreads();
-  const int i = row / G, head = h * G + row % G;
-  const int64_t len = kv8_len(a.kv_len[b], a.cache.max_pages);
-  const bool empty = len == 0 || (a.causal && len - rows.n + i < 0);
-  const int64_t at = (int64_t)(rows.row0 + i) * a.Hq + head;
-  top = fmaxf(fmaxf(meet[0][0], meet[1][0]), fmaxf(meet[2][0], meet[3][0]));
-  const float ref = top == kNegInf ? 0.f : top;
-  float part[4];
-  sum = 0.f;
-#pragma unroll
-  for (int w = 0; w < 4; ++w) {
-    part[w] = exp2_fast(meet[w][0] - ref);
-    sum = __builtin_fmaf(part[w], meet[w][1], sum);
+    for (int j = 0; j < kPer; ++j)
+      if (64 * j + lane < a.D)
+        a.Y[at * a.D + 64 * j + lane] = empty ? 0 : float_to_half_bits(out[j] * scale);
+    if (lane == 0 && a.lse != nullptr) a.lse[at] = empty ? kNegInf : (top + log2f(sum)) * kLn2;
   }
-  const int d = threadIdx.x;
-  if (d < a.D) {
-    float y = 0.f;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) y = __builtin_fmaf(part[w], meet[w][2 + d], y);
-    a.Y[at * a.D + d] = empty ? 0 : float_to_half_bits(y * (1.f / sum));
-  }
-  if (d == 0 && a.lse != nullptr) a.lse[at] = empty ? kNegInf : (top + log2f(sum)) * kLn2;
 }
 
 template <int DP, int RT>
@@ -386,8 +395,7 @@ hipError_t decode_launch(const Kv8Attn &a, int64_t max_rows, const Kv8Split &s, 
 
 template <int DP>
 hipError_t decode_width(const Kv8Attn &a, int64_t max_rows, const Kv8Split &s, hipStream_t st) {
-  // two products' rows to a workgroup, where their registers leave two waves to a SIMD
-  if constexpr (DP <= 128)
+  if constexpr (kv8_decode_tiles(DP, 32) == 2)
     if (max_rows > 16) return decode_launch<DP, 2>(a, max_rows, s, st);
   return decode_launch<DP, 1>(a, max_rows, s, st);
 }
@@ -406,7 +414,10 @@ hipError_t launch_kv8_decode(const Kv8Attn &a, const Kv8Split &s, hipStream_t st
 }
 
 hipError_t launch_kv8_combine(const Kv8Attn &a, const Kv8Split &s, hipStream_t st) {
-  const dim3 grid((unsigned)s.rows, (unsigned)a.Hkv, (unsigned)a.B);
+  // a row to a wave; more workgroups where there are few sequences, which may have many
+  // items each
+  const int64_t rows = s.rows * a.Hkv, share = kv8_max((rows + 3) / 4, 512 / a.B);
+  const dim3 grid((unsigned)kv8_min(rows, share), (unsigned)a.B);
   switch (kv8_width(a.D)) {
     case 64: detail::kv8_combine_kernel<64><<<grid, 256, 0, st>>>(a, s); break;
     case 96: detail::kv8_combine_kernel<96><<<grid, 256, 0, st>>>(a, s); break;

@@ -261,7 +261,7 @@ def check_attend(cache, q, cu, kv_len, table, scale=None, causal=True, window=0,
 
 def batch(seed, Hq, H, D, lengths, counts, pad=0, size=1.0):
     r = np.random.default_rng(seed)
-    cache, table = K.filled(r, lengths, H, D)
+    cache, table = K.filled(r, lengths, H, D, slack=20)  # wide tables are split
     cu = K.rows_of(counts)
     q = (r.normal(size=(cu[-1] + pad, Hq, D)) * size).astype(np.float16)
     q[cu[-1]:] = np.nan
@@ -279,6 +279,16 @@ DECODES = [  # query heads, key heads, channels, lengths
 @pytest.mark.parametrize("Hq,H,D,lengths", DECODES)
 def test_decode(Hq, H, D, lengths):
     check_attend(*batch(len(lengths) + D, Hq, H, D, lengths, [1] * len(lengths), pad=3))
+
+
+@pytest.mark.parametrize("Hq,H,D,lengths", [
+    (8, 8, 128, [3000, 5, 64 * 90]), (4, 1, 64, [64 * 130 + 1]), (2, 2, 80, [1500] + [1, 70] * 40),
+    (3, 3, 256, [2500, 2500, 64]), (6, 2, 96, [5000, 4999, 100, 0])])
+@pytest.mark.parametrize("window", [0, 1000])
+def test_decode_long(Hq, H, D, lengths, window):
+    """Sequences of several items, joined; among short ones, of which there are more than
+    a wave's lanes."""
+    check_attend(*batch(D, Hq, H, D, lengths, [1] * len(lengths)), window=window)
 
 
 @pytest.mark.parametrize("Hq,H,D,lengths,counts", [
@@ -333,8 +343,8 @@ def test_bad_pages_make_their_rows_nan(counts):
     cache, q, cu, lens, table = batch(10, 2, 2, 64, [130, 100, 200, 300], counts)
     pages = cache["Ks"].shape[0]
     table[0, 1], table[1, 1], table[2, 3] = pages, -1, 1 << 30
-    table = table[:, :4]  # the last sequence has more keys than the table has pages for
     scale = 0.125
+    lens[3] = 64 * table.shape[1] + 1  # more keys than the table has pages for
     want = O.attend(cache, q, cu, lens, table, scale)[0]
     for split in (False, True):
         Y, lse = run_attend(cache, q, cu, lens, table, scale, True, 0, max(counts), split)
@@ -349,7 +359,7 @@ def test_sizes_of_scores_and_values(counts):
     in different pages, and pages of zeros."""
     r = np.random.default_rng(12)
     H, D, lens = 2, 64, [200, 130]
-    table, pages = K.tables(r, lens)
+    table, pages = K.tables(r, lens, slack=20)
     cache = O.empty_cache(pages, H, D, 0x5A, np.nan)
     cu0 = K.rows_of(lens)
     k, v = K.heads_of(r, cu0[-1], H, D, 4.0), K.heads_of(r, cu0[-1], H, D)
@@ -381,7 +391,7 @@ def test_strided_queries_and_repeats():
     case("attend strided, the same bits again")
     r = np.random.default_rng(15)
     H, G, D, lens, counts = 2, 2, 128, [300, 70], [1, 1]
-    cache, table = K.filled(r, lens, H, D)
+    cache, table = K.filled(r, lens, H, D, slack=20)
     for counts in ([1, 1], [70, 60]):
         T = sum(counts)
         x = torch.from_numpy(r.normal(size=(T, (G + 2) * H * D)).astype(np.float16)).cuda()

@@ -72,7 +72,7 @@ void describe_attn_kv8(int64_t T, int64_t B, int64_t Hq, int64_t Hkv, int64_t D,
   Kv8Split s;
   const size_t bytes = plan_split(B, Hq, Hkv, D, max_q, s);
   if (!few_rows(Hq / Hkv, max_q))
-    snprintf(buf, len, "tiles 128");
+    snprintf(buf, len, "tiles 256");
   else if (workspace && bytes != 0)
     snprintf(buf, len, "few %d rows, %lld items", max_q * (Hq / Hkv) <= 16 ? 16 : 32, (long long)s.items);
   else

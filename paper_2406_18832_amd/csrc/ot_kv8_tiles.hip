@@ -17,18 +17,16 @@
 namespace ot {
 namespace detail {
 
-constexpr int kTileWaves = 4, kTileRows = 32 * kTileWaves;
-
-template <int DP>
-__global__ __launch_bounds__(64 * kTileWaves) void kv8_tile_kernel(Kv8Attn a) {
-  constexpr int kThreads = 64 * kTileWaves;
+template <int DP, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, DP > 192 ? 1 : 2) void kv8_tile_kernel(Kv8Attn a) {
+  constexpr int kThreads = 64 * WAVES, kRows = 32 * WAVES;
   constexpr int kKStride = DP + 8, kVStride = kKv8Page + 8;  // halves; off the banks
   constexpr int kSteps = DP / 16, kOut = DP / 32;
   constexpr int kUnits = DP * kKv8Page / 16;     // 16 bytes each, of K as of V
-  constexpr int kLoads = 2 * kUnits / kThreads;  // K's units, then V's
-  static_assert(kLoads * kThreads == 2 * kUnits && kUnits % 64 == 0, "a page in whole loads");
-  __shared__ _Float16 ks[kKv8Page * kKStride];
-  __shared__ _Float16 vs[DP * kVStride];
+  constexpr int kLoads = (2 * kUnits + kThreads - 1) / kThreads;  // K's units, then V's
+  static_assert(kUnits % 64 == 0, "whole waves");
+  __shared__ __attribute__((aligned(16))) _Float16 ks[2][kKv8Page * kKStride];
+  __shared__ __attribute__((aligned(16))) _Float16 vs[2][DP * kVStride];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int col = lane & 31, half = lane >> 5;
@@ -36,20 +34,20 @@ __global__ __launch_bounds__(64 * kTileWaves) void kv8_tile_kernel(Kv8Attn a) {
   const int64_t slot = blockIdx.x / a.Hkv;
   const int G = a.Hq / a.Hkv;
   const int b = kv8_find(a.B, lane, slot,
-                         [&](int i) { return kv8_tile_slot((int64_t)a.cu[i] * G, i, kTileRows); });
+                         [&](int i) { return kv8_tile_slot((int64_t)a.cu[i] * G, i, kRows); });
   if (b < 0) return;
   const Kv8Rows rows = kv8_rows(a.cu[b], a.cu[b + 1], a.T);
   // counted from the end: under a causal mask the last tile has the most pages
-  const int64_t tiles = ((int64_t)rows.n * G + kTileRows - 1) / kTileRows;
-  const int64_t tile = tiles - 1 - (slot - kv8_tile_slot((int64_t)a.cu[b] * G, b, kTileRows));
+  const int64_t tiles = ((int64_t)rows.n * G + kRows - 1) / kRows;
+  const int64_t tile = tiles - 1 - (slot - kv8_tile_slot((int64_t)a.cu[b] * G, b, kRows));
   if (tile < 0 || tile >= tiles) return;
   const int64_t len0 = a.kv_len[b];
   const int len = (int)kv8_len(len0, a.cache.max_pages);
   const bool bad = len0 > len;
-  const int row0 = (int)tile * kTileRows + 32 * wave;
+  const int row0 = (int)tile * kRows + 32 * wave;
   const int all = rows.n * G;
-  const int first = (int)tile * kTileRows / G;
-  const int last = min((int)(tile + 1) * kTileRows - 1, all - 1) / G;
+  const int first = (int)tile * kRows / G;
+  const int last = min((int)(tile + 1) * kRows - 1, all - 1) / G;
   const Kv8Span span = kv8_span(len, rows.n, first, last - first + 1, a.causal, a.window);
 
   // this lane's query row
@@ -63,6 +61,7 @@ __global__ __launch_bounds__(64 * kTileWaves) void kv8_tile_kernel(Kv8Attn a) {
     const int d = 16 * st + 8 * half;
     v4u w = {0u, 0u, 0u, 0u};
     if (d < a.D) w = *reinterpret_cast<const v4u *>(qp + d);
+    if (a.scale < 0.f) w ^= 0x80008000u;  // the factor of a score is not negative then
     q[st] = __builtin_bit_cast(v8h, w);
   }
   const int pos = len - rows.n + qi;
@@ -79,39 +78,54 @@ __global__ __launch_bounds__(64 * kTileWaves) void kv8_tile_kernel(Kv8Attn a) {
   for (int t = 0; t < kOut; ++t)
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
-  const float fac = a.scale * kLog2e;
+  const float fac = fabsf(a.scale) * kLog2e;
 
   v4u code[kLoads];
   float f = 0.f, lg = 0.f, iv = 1.f;
+  // page p's codes on their way into registers, and its scales
   auto fetch = [&](int p) {
     int64_t page = kv8_page(a.cache.table, b, p, a.cache.max_pages, a.cache.num_pages);
     const bool none = page < 0 || bad;
     if (page < 0) page = 0;
     const int64_t ph = page * a.Hkv + h;
-    const uint8_t *kp = a.cache.Kc + ph * (DP * kKv8Page), *vp = a.cache.Vc + ph * (DP * kKv8Page);
+    const __amdgpu_buffer_rsrc_t keys = make_rsrc(a.cache.Kc + ph * (DP * kKv8Page), DP * kKv8Page);
+    const __amdgpu_buffer_rsrc_t values = make_rsrc(a.cache.Vc + ph * (DP * kKv8Page), DP * kKv8Page);
 #pragma unroll
     for (int u = 0; u < kLoads; ++u) {
-      const int at = u * kThreads + tid;
-      code[u] = *reinterpret_cast<const v4u *>(at < kUnits ? kp + at * 16 : vp + (at - kUnits) * 16);
+      const int at = u * kThreads + wave * 64;  // a wave's are all of one kind
+      if (at < kUnits)
+        code[u] = __builtin_amdgcn_raw_buffer_load_b128(keys, (u * kThreads + tid) * 16, 0, 0);
+      else if (at < 2 * kUnits)
+        code[u] = __builtin_amdgcn_raw_buffer_load_b128(values, (u * kThreads + tid - kUnits) * 16, 0, 0);
     }
     f = none ? __builtin_nanf("") : a.cache.Ks[ph] * fac;
     value_scale(none ? 0.f : a.cache.Vs[ph], lg, iv);
   };
-  if (span.p0 < span.p1) fetch(span.p0);
-
-  for (int p = span.p0; p < span.p1; ++p) {
-    __syncthreads();  // the page before is done with
+  // and as fp16 into LDS
+  auto stage = [&](int to) {
 #pragma unroll
     for (int u = 0; u < kLoads; ++u) {
+      if (u * kThreads + wave * 64 >= 2 * kUnits) break;
       const int at = (u * kThreads + tid) * 16, vat = at - 16 * kUnits;
-      _Float16 *to = at < 16 * kUnits ? ks + at / DP * kKStride + at % DP
-                                      : vs + vat / kKv8Page * kVStride + vat % kKv8Page;
-      *reinterpret_cast<v8h *>(to) = kv8_halves(code[u][0], code[u][1]);
-      *reinterpret_cast<v8h *>(to + 8) = kv8_halves(code[u][2], code[u][3]);
+      _Float16 *p = u * kThreads + wave * 64 < kUnits
+                        ? ks[to] + at / DP * kKStride + at % DP
+                        : vs[to] + vat / kKv8Page * kVStride + vat % kKv8Page;
+      *reinterpret_cast<v8h *>(p) = kv8_halves(code[u][0], code[u][1]);
+      *reinterpret_cast<v8h *>(p + 8) = kv8_halves(code[u][2], code[u][3]);
     }
+  };
+  const int key_row = 16 * (col >> 4) + 8 * ((col >> 2) & 1) + 4 * ((col >> 3) & 1) + (col & 3);
+  if (span.p0 < span.p1) {
+    fetch(span.p0);
+    stage(0);
+  }
+  for (int p = span.p0, buf = 0; p < span.p1; ++p, buf ^= 1) {
     const float pf = f, plg = lg, piv = iv;
-    __syncthreads();
-    if (p + 1 < span.p1) fetch(p + 1);
+    __syncthreads();  // this page is there, and the one before is done with
+    const bool more = p + 1 < span.p1;
+    if (more) fetch(p + 1);
+    const _Float16 *kp = ks[buf] + key_row * kKStride + 8 * half;
+    const _Float16 *vp = vs[buf] + col * kVStride + 8 * half;
 
     const int token = p * kKv8Page;
     v16f x[2];
@@ -119,26 +133,30 @@ __global__ __launch_bounds__(64 * kTileWaves) void kv8_tile_kernel(Kv8Attn a) {
     for (int t = 0; t < 2; ++t) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) x[t][i] = 0.f;
-      const int at = 32 * t + 16 * (col >> 4) + 8 * ((col >> 2) & 1) + 4 * ((col >> 3) & 1) + (col & 3);
 #pragma unroll
       for (int st = 0; st < kSteps; ++st) {
-        const v8h k = *reinterpret_cast<const v8h *>(ks + at * kKStride + 16 * st + 8 * half);
+        const v8h k = *reinterpret_cast<const v8h *>(kp + 32 * t * kKStride + 16 * st);
         x[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q[st], x[t], 0, 0, 0);
       }
     }
     const bool cut = token < all_lo || token + kKv8Page - 1 > all_hi;
+    auto hidden = [&](int t, int i) {
+      const int key = token + 32 * t + 16 * (i >> 3) + 8 * half + (i & 7);
+      return key < key_lo || key > key_hi;
+    };
+    if (cut) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (hidden(t, i)) x[t][i] = kNegInf;
+    }
     float most = kNegInf;
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        float v = __builtin_fmaf(x[t][i], pf, plg);
-        const int key = token + 32 * t + 16 * (i >> 3) + 8 * half + (i & 7);
-        if (cut && (key < key_lo || key > key_hi)) v = kNegInf;
-        x[t][i] = v;
-        most = fmaxf(most, v);
-      }
-    most = max_xor32(most);
+      for (int i = 0; i < 16; ++i) most = fmaxf(most, x[t][i]);
+    most = __builtin_fmaf(max_xor32(most), pf, plg);  // pf >= 0: a row's largest exponent
     if (__any(most > m + kMost)) {
       const float now = most > m + kMost ? most - kSet : m;
       const float keep = m == now ? 1.f : exp2_fast(m - now);
@@ -147,14 +165,25 @@ __global__ __launch_bounds__(64 * kTileWaves) void kv8_tile_kernel(Kv8Attn a) {
 #pragma unroll
       for (int t = 0; t < kOut; ++t) o[t] *= keep;
     }
-    const float ref = m == kNegInf ? 0.f : m;  // no key yet
+    const float off = plg - (m == kNegInf ? 0.f : m);  // no key yet
     float sum = 0.f;
     v8h w[4];
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
+      for (int i = 0; i < 16; ++i) x[t][i] = __builtin_fmaf(x[t][i], pf, off);
+    if (cut) {  // a scale of 0 has made NaN of them
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (hidden(t, i)) x[t][i] = kNegInf;
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const float e = exp2_fast(x[t][i] - ref);
+        const float e = exp2_fast(x[t][i]);
         sum += e;
         w[2 * t + (i >> 3)][i & 7] = (_Float16)e;
       }
@@ -163,9 +192,10 @@ __global__ __launch_bounds__(64 * kTileWaves) void kv8_tile_kernel(Kv8Attn a) {
     for (int t = 0; t < kOut; ++t)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const v8h v = *reinterpret_cast<const v8h *>(vs + (32 * t + col) * kVStride + 16 * j + 8 * half);
+        const v8h v = *reinterpret_cast<const v8h *>(vp + 32 * t * kVStride + 16 * j);
         o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, w[j], o[t], 0, 0, 0);
       }
+    if (more) stage(buf ^ 1);
   }
 
   l += __shfl_xor(l, 32);
@@ -191,17 +221,21 @@ __global__ __launch_bounds__(64 * kTileWaves) void kv8_tile_kernel(Kv8Attn a) {
 
 }  // namespace detail
 
-hipError_t launch_kv8_tiles(const Kv8Attn &a, hipStream_t st) {
-  const int64_t slots = kv8_tile_slots((int64_t)a.T * (a.Hq / a.Hkv), a.B, detail::kTileRows);
-  const unsigned grid = (unsigned)(slots * a.Hkv);
-  switch (kv8_width(a.D)) {
-    case 64: detail::kv8_tile_kernel<64><<<grid, 256, 0, st>>>(a); break;
-    case 96: detail::kv8_tile_kernel<96><<<grid, 256, 0, st>>>(a); break;
-    case 128: detail::kv8_tile_kernel<128><<<grid, 256, 0, st>>>(a); break;
-    case 192: detail::kv8_tile_kernel<192><<<grid, 256, 0, st>>>(a); break;
-    default: detail::kv8_tile_kernel<256><<<grid, 256, 0, st>>>(a); break;
-  }
+template <int DP, int WAVES>
+static hipError_t tile_launch(const Kv8Attn &a, hipStream_t st) {
+  const int64_t slots = kv8_tile_slots((int64_t)a.T * (a.Hq / a.Hkv), a.B, 32 * WAVES);
+  detail::kv8_tile_kernel<DP, WAVES><<<(unsigned)(slots * a.Hkv), 64 * WAVES, 0, st>>>(a);
   return hipGetLastError();
+}
+
+hipError_t launch_kv8_tiles(const Kv8Attn &a, hipStream_t st) {
+  switch (kv8_width(a.D)) {
+    case 64: return tile_launch<64, 8>(a, st);
+    case 96: return tile_launch<96, 8>(a, st);
+    case 128: return tile_launch<128, 8>(a, st);
+    case 192: return tile_launch<192, 8>(a, st);
+    default: return tile_launch<256, 4>(a, st);
+  }
 }
 
 }  // namespace ot

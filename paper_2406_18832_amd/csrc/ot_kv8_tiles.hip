@@ -1,10 +1,10 @@
 // Attention over the 8-bit cache for many query rows (prompts, pieces of prompts):
 // bound by the matrix cores.
 //
-// A workgroup takes 128 query rows (tokens times the query heads of one key head)
-// of a sequence, 32 to each of its four waves, and goes over the pages that they
-// see.  A page's codes are turned to fp16 once, on their way into LDS, where all
-// waves read them as the A operands of v_mfma_f32_32x32x16_f16.
+// A workgroup takes a tile of query rows (tokens times the query heads of one key head)
+// of a sequence, 32 to each of its waves, and goes over the pages that they see.  A
+// page's codes are turned to fp16 once, on their way into LDS, where all waves read them
+// as the A operands of v_mfma_f32_32x32x16_f16.
 //
 // S^T = K Q^T: lane l has query row l mod 32; K's row 8 a + 4 h + i of a tile of 32
 // tokens is token 16 (a / 2) + 8 h + 4 (a mod 2) + i, so that the 16 results of a lane
@@ -12,151 +12,147 @@
 // of the B operand of one product O^T += V^T P^T.
 #include <math.h>
 
+#include <type_traits>
+
 #include "ot_kv8_attn.h"
 
 namespace ot {
 namespace detail {
 
-template <int DP, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, DP > 192 ? 1 : 2) void kv8_tile_kernel(Kv8Attn a) {
-  constexpr int kThreads = 64 * WAVES, kRows = 32 * WAVES;
-  constexpr int kKStride = DP + 8, kVStride = kKv8Page + 8;  // halves; off the banks
-  constexpr int kSteps = DP / 16, kOut = DP / 32;
-  constexpr int kUnits = DP * kKv8Page / 16;     // 16 bytes each, of K as of V
-  constexpr int kLoads = (2 * kUnits + kThreads - 1) / kThreads;  // K's units, then V's
-  static_assert(kUnits % 64 == 0, "whole waves");
-  __shared__ __attribute__((aligned(16))) _Float16 ks[2][kKv8Page * kKStride];
-  __shared__ __attribute__((aligned(16))) _Float16 vs[2][DP * kVStride];
+// A page in LDS, and one wave's 32 rows.
+template <int DP>
+struct Kv8Tile {
+  static constexpr int kKStride = DP + 8, kVStride = kKv8Page + 8;  // halves; off the banks
+  static constexpr int kKPage = kKv8Page * kKStride, kVPage = DP * kVStride;
+  static constexpr int kSteps = DP / 16, kOut = DP / 32;
+  static constexpr int kUnits = DP * kKv8Page / 16;  // 16 bytes each, of a page's K as of its V
 
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int col = lane & 31, half = lane >> 5;
-  const int h = blockIdx.x % a.Hkv;
-  const int64_t slot = blockIdx.x / a.Hkv;
-  const int G = a.Hq / a.Hkv;
-  const int b = kv8_find(a.B, lane, slot,
-                         [&](int i) { return kv8_tile_slot((int64_t)a.cu[i] * G, i, kRows); });
-  if (b < 0) return;
-  const Kv8Rows rows = kv8_rows(a.cu[b], a.cu[b + 1], a.T);
-  // counted from the end: under a causal mask the last tile has the most pages
-  const int64_t tiles = ((int64_t)rows.n * G + kRows - 1) / kRows;
-  const int64_t tile = tiles - 1 - (slot - kv8_tile_slot((int64_t)a.cu[b] * G, b, kRows));
-  if (tile < 0 || tile >= tiles) return;
-  const int64_t len0 = a.kv_len[b];
-  const int len = (int)kv8_len(len0, a.cache.max_pages);
-  const bool bad = len0 > len;
-  const int row0 = (int)tile * kRows + 32 * wave;
-  const int all = rows.n * G;
-  const int first = (int)tile * kRows / G;
-  const int last = min((int)(tile + 1) * kRows - 1, all - 1) / G;
-  const Kv8Span span = kv8_span(len, rows.n, first, last - first + 1, a.causal, a.window);
+  int b, h, len, first_page, pages;
+  bool bad;  // more keys than the table has pages for
 
-  // this lane's query row
-  const int row = row0 + col;
-  const bool in = row < all;
-  const int qi = (in ? row : all - 1) / G, head = h * G + (in ? row : all - 1) % G;
-  const uint16_t *qp = a.q + (int64_t)(rows.row0 + qi) * a.ldq + head * a.D;
+  bool in, empty;              // this lane's row is one; it sees no key
+  int64_t out;                 // its number among all rows of all heads
+  int key_lo, key_hi;          // the keys that it sees
+  int all_lo, all_hi;          // that all of the wave's see
+  int key_at, value_at;        // its first halves of a page's K and V in LDS
   v8h q[kSteps];
-#pragma unroll
-  for (int st = 0; st < kSteps; ++st) {
-    const int d = 16 * st + 8 * half;
-    v4u w = {0u, 0u, 0u, 0u};
-    if (d < a.D) w = *reinterpret_cast<const v4u *>(qp + d);
-    if (a.scale < 0.f) w ^= 0x80008000u;  // the factor of a score is not negative then
-    q[st] = __builtin_bit_cast(v8h, w);
-  }
-  const int pos = len - rows.n + qi;
-  const int key_hi = a.causal ? pos : len - 1;
-  const int key_lo = a.window > 0 ? max(0, (int)kv8_max(pos - a.window + 1, 0)) : 0;
-  // keys that every row of the wave sees
-  const int wave_first = min(row0, all - 1) / G, wave_last = min(row0 + 31, all - 1) / G;
-  const int all_hi = a.causal ? len - rows.n + wave_first : len - 1;
-  const int all_lo = a.window > 0 ? (int)kv8_max(0, len - rows.n + wave_last - a.window + 1) : 0;
-
-  float m = kNegInf, l = 0.f;
   v16f o[kOut];
-#pragma unroll
-  for (int t = 0; t < kOut; ++t)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
-  const float fac = fabsf(a.scale) * kLog2e;
+  float m, l;
 
-  v4u code[kLoads];
-  float f = 0.f, lg = 0.f, iv = 1.f;
-  // page p's codes on their way into registers, and its scales
-  auto fetch = [&](int p) {
-    int64_t page = kv8_page(a.cache.table, b, p, a.cache.max_pages, a.cache.num_pages);
-    const bool none = page < 0 || bad;
-    if (page < 0) page = 0;
-    const int64_t ph = page * a.Hkv + h;
-    const __amdgpu_buffer_rsrc_t keys = make_rsrc(a.cache.Kc + ph * (DP * kKv8Page), DP * kKv8Page);
-    const __amdgpu_buffer_rsrc_t values = make_rsrc(a.cache.Vc + ph * (DP * kKv8Page), DP * kKv8Page);
+  // The tile of slot `slot`; false where there is none.
+  template <int kRows>
+  __device__ __forceinline__ bool aim(const Kv8Attn &a, int64_t slot, int head_k, int wave, int lane) {
+    const int col = lane & 31, half = lane >> 5;
+    const int G = a.Hq / a.Hkv;
+    h = head_k;
+    b = kv8_find(a.B, lane, slot,
+                 [&](int i) { return kv8_tile_slot((int64_t)a.cu[i] * G, i, kRows); });
+    if (b < 0) return false;
+    const Kv8Rows rows = kv8_rows(a.cu[b], a.cu[b + 1], a.T);
+    // counted from the end: under a causal mask the last tile has the most pages
+    const int64_t tiles = ((int64_t)rows.n * G + kRows - 1) / kRows;
+    const int64_t tile = tiles - 1 - (slot - kv8_tile_slot((int64_t)a.cu[b] * G, b, kRows));
+    if (tile < 0 || tile >= tiles) return false;
+    const int64_t whole = a.kv_len[b];
+    len = (int)kv8_len(whole, a.cache.max_pages);
+    bad = whole > len;
+    const int all = rows.n * G, row0 = (int)tile * kRows + 32 * wave;
+    const int q0 = (int)tile * kRows / G, q1 = min((int)(tile + 1) * kRows - 1, all - 1) / G;
+    const Kv8Span span = kv8_span(len, rows.n, q0, q1 - q0 + 1, a.causal, a.window);
+    first_page = span.p0;
+    pages = span.p1 - span.p0;
+
+    const int row = row0 + col;
+    in = row < all;
+    const int some = in ? row : all - 1, qi = some / G, head = h * G + some % G;
+    out = (int64_t)(rows.row0 + qi) * a.Hq + head;
+    const uint16_t *qp = a.q + (int64_t)(rows.row0 + qi) * a.ldq + head * a.D;
 #pragma unroll
-    for (int u = 0; u < kLoads; ++u) {
-      const int at = u * kThreads + wave * 64;  // a wave's are all of one kind
-      if (at < kUnits)
-        code[u] = __builtin_amdgcn_raw_buffer_load_b128(keys, (u * kThreads + tid) * 16, 0, 0);
-      else if (at < 2 * kUnits)
-        code[u] = __builtin_amdgcn_raw_buffer_load_b128(values, (u * kThreads + tid - kUnits) * 16, 0, 0);
+    for (int st = 0; st < kSteps; ++st) {
+      const int d = 16 * st + 8 * half;
+      v4u w = {0u, 0u, 0u, 0u};
+      if (d < a.D) w = *reinterpret_cast<const v4u *>(qp + d);
+      if (a.scale < 0.f) w ^= 0x80008000u;  // the factor of a score is not negative then
+      q[st] = __builtin_bit_cast(v8h, w);
     }
-    f = none ? __builtin_nanf("") : a.cache.Ks[ph] * fac;
-    value_scale(none ? 0.f : a.cache.Vs[ph], lg, iv);
-  };
-  // and as fp16 into LDS
-  auto stage = [&](int to) {
+    const int pos = len - rows.n + qi;
+    empty = len == 0 || (a.causal && pos < 0);
+    key_hi = a.causal ? pos : len - 1;
+    key_lo = a.window > 0 ? (int)kv8_max(pos - a.window + 1, 0) : 0;
+    const int w0 = min(row0, all - 1) / G, w1 = min(row0 + 31, all - 1) / G;
+    all_hi = a.causal ? len - rows.n + w0 : len - 1;
+    all_lo = a.window > 0 ? (int)kv8_max(0, len - rows.n + w1 - a.window + 1) : 0;
+    key_at = (16 * (col >> 4) + 8 * ((col >> 2) & 1) + 4 * ((col >> 3) & 1) + (col & 3)) * kKStride +
+             8 * half;
+    value_at = col * kVStride + 8 * half;
+    m = kNegInf;
+    l = 0.f;
 #pragma unroll
-    for (int u = 0; u < kLoads; ++u) {
-      if (u * kThreads + wave * 64 >= 2 * kUnits) break;
-      const int at = (u * kThreads + tid) * 16, vat = at - 16 * kUnits;
-      _Float16 *p = u * kThreads + wave * 64 < kUnits
-                        ? ks[to] + at / DP * kKStride + at % DP
-                        : vs[to] + vat / kKv8Page * kVStride + vat % kKv8Page;
-      *reinterpret_cast<v8h *>(p) = kv8_halves(code[u][0], code[u][1]);
-      *reinterpret_cast<v8h *>(p + 8) = kv8_halves(code[u][2], code[u][3]);
-    }
-  };
-  const int key_row = 16 * (col >> 4) + 8 * ((col >> 2) & 1) + 4 * ((col >> 3) & 1) + (col & 3);
-  if (span.p0 < span.p1) {
-    fetch(span.p0);
-    stage(0);
+    for (int t = 0; t < kOut; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
+    return true;
   }
-  for (int p = span.p0, buf = 0; p < span.p1; ++p, buf ^= 1) {
-    const float pf = f, plg = lg, piv = iv;
-    __syncthreads();  // this page is there, and the one before is done with
-    const bool more = p + 1 < span.p1;
-    if (more) fetch(p + 1);
-    const _Float16 *kp = ks[buf] + key_row * kKStride + 8 * half;
-    const _Float16 *vp = vs[buf] + col * kVStride + 8 * half;
 
-    const int token = p * kKv8Page;
-    v16f x[2];
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) x[t][i] = 0.f;
-#pragma unroll
-      for (int st = 0; st < kSteps; ++st) {
-        const v8h k = *reinterpret_cast<const v8h *>(kp + 32 * t * kKStride + 16 * st);
-        x[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k, q[st], x[t], 0, 0, 0);
-      }
-    }
-    const bool cut = token < all_lo || token + kKv8Page - 1 > all_hi;
-    auto hidden = [&](int t, int i) {
-      const int key = token + 32 * t + 16 * (i >> 3) + 8 * half + (i & 7);
-      return key < key_lo || key > key_hi;
-    };
-    if (cut) {
+  // Pages' numbers and scales are looked up 64 at a time, one to a lane: looked up when
+  // they are needed, they would be two memory latencies in every page.
+  int id;           // of the pages from 64 (j / 64) on: where codes are fetched
+  float f, lg, iv;  // of the same pages, where scores become weights: factor of a score,
+                    // value exponent and what undoes that
+  __device__ __forceinline__ int lookup(const Kv8Attn &a, int j) const {
+    if (j >= pages) return -1;
+    return (int)kv8_page(a.cache.table, b, first_page + j, a.cache.max_pages, a.cache.num_pages);
+  }
+  // The first of page j's pages and heads in the pool (some page for one that it does not
+  // have).
+  __device__ __forceinline__ int64_t place(const Kv8Attn &a, int j, int lane) {
+    if ((j & 63) == 0) id = max(lookup(a, j + lane), 0);
+    return (int64_t)__builtin_amdgcn_readlane(id, j & 63) * a.Hkv + h;
+  }
+  __device__ __forceinline__ void scales(const Kv8Attn &a, int j, int lane, float fac) {
+    if ((j & 63) != 0) return;
+    const int page = lookup(a, j + lane);
+    const int64_t ph = (int64_t)max(page, 0) * a.Hkv + h;
+    f = factor(page < 0 || bad ? __builtin_nanf("") : a.cache.Ks[ph], fac);
+    value_scale(page < 0 ? 0.f : a.cache.Vs[ph], lg, iv);
+  }
+
+  // A page's factor of a score: not 0, where what is masked would be NaN (all scores are 0
+  // then, or as good as).
+  static __device__ __forceinline__ float factor(float scale, float fac) {
+    const float f = scale * fac;
+    return f < 1e-30f ? 1e-30f : f;
+  }
+
+  // Scores of page j to weights.
+  __device__ __forceinline__ void weights(const Kv8Attn &a, int j, int lane, float fac, v16f (&x)[2],
+                                          v8h (&w)[4]) {
+    scales(a, j, lane, fac);
+    const int half = lane >> 5;
+    float pf = lane_float(f, j & 63), plg = lane_float(lg, j & 63);
+    const float piv = lane_float(iv, j & 63);
+    const int token = (first_page + j) * kKv8Page;
+    if (token < all_lo || token + kKv8Page - 1 > all_hi) {
+      asm volatile("");  // a branch, not selects on every page
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (hidden(t, i)) x[t][i] = kNegInf;
+        for (int i = 0; i < 16; ++i) {
+          const int key = token + 32 * t + 16 * (i >> 3) + 8 * half + (i & 7);
+          if (key < key_lo || key > key_hi) x[t][i] = kNegInf;
+        }
+      // a row that sees none of the page keeps out of its scales, which can be NaN
+      if (key_hi < token || key_lo > token + kKv8Page - 1) {
+        pf = 1.f;
+        plg = 0.f;
+      }
     }
     float most = kNegInf;
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int i = 0; i < 16; ++i) most = fmaxf(most, x[t][i]);
-    most = __builtin_fmaf(max_xor32(most), pf, plg);  // pf >= 0: a row's largest exponent
+    most = __builtin_fmaf(max_xor32(most), pf, plg);  // a row's largest exponent
     if (__any(most > m + kMost)) {
       const float now = most > m + kMost ? most - kSet : m;
       const float keep = m == now ? 1.f : exp2_fast(m - now);
@@ -167,56 +163,220 @@ __global__ __launch_bounds__(64 * WAVES, DP > 192 ? 1 : 2) void kv8_tile_kernel(
     }
     const float off = plg - (m == kNegInf ? 0.f : m);  // no key yet
     float sum = 0.f;
-    v8h w[4];
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) x[t][i] = __builtin_fmaf(x[t][i], pf, off);
-    if (cut) {  // a scale of 0 has made NaN of them
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (hidden(t, i)) x[t][i] = kNegInf;
-    }
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const float e = exp2_fast(x[t][i]);
+        const float e = exp2_fast(__builtin_fmaf(x[t][i], pf, off));
         sum += e;
         w[2 * t + (i >> 3)][i & 7] = (_Float16)e;
       }
     l = __builtin_fmaf(sum, piv, l);
 #pragma unroll
-    for (int t = 0; t < kOut; ++t)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const v8h v = *reinterpret_cast<const v8h *>(vp + 32 * t * kVStride + 16 * j);
-        o[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, w[j], o[t], 0, 0, 0);
-      }
-    if (more) stage(buf ^ 1);
+    for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(w[i]));  // they are done here, not among the products
   }
 
-  l += __shfl_xor(l, 32);
-  if (!in) return;
-  // a row that sees no key: as its position says, not as its sum does
-  const bool empty = len == 0 || (a.causal && pos < 0);
-  const float scale = 1.f / l;
-  const int64_t at = (int64_t)(rows.row0 + qi) * a.Hq + head;
+  // Products in a row: O += V W where VALUES (w of a page, its V at vs), X = K Q where
+  // SCORES (another page's K at ks).  Fragments come out of LDS kAhead products early.
+  template <bool VALUES, bool SCORES>
+  __device__ __forceinline__ void products(const _Float16 *vs, const v8h (&w)[4], const _Float16 *ks,
+                                           v16f (&x)[2]) {
+    constexpr int kV = VALUES ? 4 * kOut : 0, kS = SCORES ? 2 * kSteps : 0, kAhead = 6;
+    const _Float16 *vp = vs + value_at, *kp = ks + key_at;
+    auto fragment = [&](int i) {
+      return i < kV ? *reinterpret_cast<const v8h *>(vp + 32 * (i % kOut) * kVStride + 16 * (i / kOut))
+                    : *reinterpret_cast<const v8h *>(kp + 32 * ((i - kV) & 1) * kKStride + 16 * ((i - kV) >> 1));
+    };
+    if constexpr (SCORES) {
 #pragma unroll
-  for (int t = 0; t < kOut; ++t)
+      for (int t = 0; t < 2; ++t)
 #pragma unroll
-    for (int i = 0; i < 16; i += 4) {
-      const int d = 32 * t + 2 * i + 4 * half;
-      if (d >= a.D) continue;
-      v2u y;
-      y[0] = __builtin_bit_cast(uint32_t, pack_half(o[t][i] * scale, o[t][i + 1] * scale));
-      y[1] = __builtin_bit_cast(uint32_t, pack_half(o[t][i + 2] * scale, o[t][i + 3] * scale));
-      if (empty) y = v2u{0u, 0u};
-      *reinterpret_cast<v2u *>(a.Y + at * a.D + d) = y;
+        for (int i = 0; i < 16; ++i) x[t][i] = 0.f;
     }
-  if (half == 0 && a.lse != nullptr) a.lse[at] = empty ? kNegInf : (m + log2f(l)) * kLn2;
+    v8h ring[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) ring[i] = fragment(i);
+    __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
+#pragma unroll
+    for (int i = 0; i < kV + kS; ++i) {
+      const v8h now = ring[i % kAhead];
+      if (i < kV)
+        o[i % kOut] = __builtin_amdgcn_mfma_f32_32x32x16_f16(now, w[i / kOut], o[i % kOut], 0, 0, 0);
+      else
+        x[(i - kV) & 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(now, q[(i - kV) >> 1], x[(i - kV) & 1], 0, 0, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      if (i + kAhead < kV + kS) {
+        ring[i % kAhead] = fragment(i + kAhead);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+    }
+  }
+
+  __device__ __forceinline__ void finish(const Kv8Attn &a, int half) {
+    l += __shfl_xor(l, 32);
+    if (!in) return;
+    const float scale = 1.f / l;
+#pragma unroll
+    for (int t = 0; t < kOut; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4) {
+        const int d = 32 * t + 2 * i + 4 * half;
+        if (d >= a.D) continue;
+        v2u y;
+        y[0] = __builtin_bit_cast(uint32_t, pack_half(o[t][i] * scale, o[t][i + 1] * scale));
+        y[1] = __builtin_bit_cast(uint32_t, pack_half(o[t][i + 2] * scale, o[t][i + 3] * scale));
+        if (empty) y = v2u{0u, 0u};
+        *reinterpret_cast<v2u *>(a.Y + out * a.D + d) = y;
+      }
+    if (half == 0 && a.lse != nullptr) a.lse[out] = empty ? kNegInf : (m + log2f(l)) * kLn2;
+  }
+
+  // Where 16 codes (unit u of a page's K or V) go in LDS, as fp16.
+  static __device__ __forceinline__ int key_place(int u) {
+    return u / (DP / 16) * kKStride + u % (DP / 16) * 16;
+  }
+  static __device__ __forceinline__ int value_place(int u) {
+    return u / (kKv8Page / 16) * kVStride + u % (kKv8Page / 16) * 16;
+  }
+};
+
+__device__ __forceinline__ void stage16(_Float16 *to, v4u w) {
+  *reinterpret_cast<v8h *>(to) = kv8_halves(w[0], w[1]);
+  *reinterpret_cast<v8h *>(to + 8) = kv8_halves(w[2], w[3]);
+}
+
+// One phase after another: every wave does scores, softmax and values of a page, and its
+// part of the next page's codes, between two barriers.
+template <int DP, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, DP > 192 ? 1 : 2) void kv8_tile_kernel(Kv8Attn a) {
+  using Tile = Kv8Tile<DP>;
+  constexpr int kThreads = 64 * WAVES, kUnits = Tile::kUnits;
+  constexpr int kLoads = (2 * kUnits + kThreads - 1) / kThreads;  // K's units, then V's
+  static_assert(kUnits % 64 == 0, "whole waves");
+  __shared__ __attribute__((aligned(16))) _Float16 ks[2][Tile::kKPage];
+  __shared__ __attribute__((aligned(16))) _Float16 vs[2][Tile::kVPage];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  Tile t;
+  if (!t.template aim<32 * WAVES>(a, blockIdx.x / a.Hkv, blockIdx.x % a.Hkv, wave, lane)) return;
+  const float fac = fabsf(a.scale) * kLog2e;
+
+  v4u code[kLoads];
+  auto fetch = [&](int j) {
+    const int64_t ph = t.place(a, j, lane);
+    const __amdgpu_buffer_rsrc_t keys = make_rsrc(a.cache.Kc + ph * (DP * kKv8Page), DP * kKv8Page);
+    const __amdgpu_buffer_rsrc_t values = make_rsrc(a.cache.Vc + ph * (DP * kKv8Page), DP * kKv8Page);
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) {
+      const int at = u * kThreads + wave * 64;  // a wave's are all of one kind
+      if (at < kUnits)
+        code[u] = __builtin_amdgcn_raw_buffer_load_b128(keys, (u * kThreads + tid) * 16, 0, 0);
+      else if (at < 2 * kUnits)
+        code[u] = __builtin_amdgcn_raw_buffer_load_b128(values, (u * kThreads + tid - kUnits) * 16, 0, 0);
+    }
+  };
+  auto stage = [&](int to) {
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) {
+      const int at = u * kThreads + wave * 64;
+      if (at < kUnits)
+        stage16(ks[to] + Tile::key_place(u * kThreads + tid), code[u]);
+      else if (at < 2 * kUnits)
+        stage16(vs[to] + Tile::value_place(u * kThreads + tid - kUnits), code[u]);
+    }
+  };
+  if (t.pages > 0) {
+    fetch(0);
+    stage(0);
+  }
+  for (int j = 0; j < t.pages; ++j) {
+    __syncthreads();  // this page is there, and the one before is done with
+    const bool more = j + 1 < t.pages;
+    if (more) fetch(j + 1);
+    v16f x[2];
+    v8h w[4];
+    t.template products<false, true>(nullptr, w, ks[j & 1], x);
+    t.weights(a, j, lane, fac, x, w);
+    t.template products<true, false>(vs[j & 1], w, nullptr, x);
+    if (more) stage((j + 1) & 1);
+  }
+  t.finish(a, lane >> 5);
+}
+
+// LDS is as this wave has left it, and the other waves too.  (Global loads stay in flight.)
+__device__ __forceinline__ void meet() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// Two teams of four waves, one of each to a SIMD, half a page apart: while one has the
+// matrix cores (values of a page, scores of the next), the other has the vector units
+// (softmax, codes to fp16), and at every barrier they change over.  With i counting the
+// intervals between barriers, the first team has its products in even i and the second in
+// odd i: scores of page j in 2 j and 2 j + 1, values in 2 j + 2 and 2 j + 3.  The first
+// team brings K: page j + 1 in interval 2 j + 1, over page j - 1, last read in 2 j - 1.
+// The second brings V: page j + 1 in interval 2 j + 2, over page j - 1, last read in
+// 2 j + 1.  Each therefore has two stages.
+template <int DP>
+__global__ __launch_bounds__(512, 2) void kv8_pair_kernel(Kv8Attn a) {
+  using Tile = Kv8Tile<DP>;
+  constexpr int kUnits = Tile::kUnits, kLoads = (kUnits + 255) / 256;
+  __shared__ __attribute__((aligned(16))) _Float16 ks[2][Tile::kKPage];
+  __shared__ __attribute__((aligned(16))) _Float16 vs[2][Tile::kVPage];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int half = lane >> 5, mine = tid & 255;
+  const bool second = wave >= 4;
+  Tile t;
+  if (!t.template aim<256>(a, blockIdx.x / a.Hkv, blockIdx.x % a.Hkv, wave, lane)) return;
+  const float fac = fabsf(a.scale) * kLog2e;
+
+  v4u code[kLoads];
+  const uint8_t *pool = second ? a.cache.Vc : a.cache.Kc;
+  auto fetch = [&](int j) {
+    const int64_t ph = t.place(a, j, lane);
+    const __amdgpu_buffer_rsrc_t page = make_rsrc(pool + ph * (DP * kKv8Page), DP * kKv8Page);
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u)
+      if (u * 256 + (wave & 3) * 64 < kUnits)
+        code[u] = __builtin_amdgcn_raw_buffer_load_b128(page, (u * 256 + mine) * 16, 0, 0);
+  };
+  auto stage = [&](int j) {
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u)
+      if (u * 256 + (wave & 3) * 64 < kUnits)
+        stage16(second ? vs[j & 1] + Tile::value_place(u * 256 + mine)
+                       : ks[j & 1] + Tile::key_place(u * 256 + mine), code[u]);
+  };
+  const int n = t.pages;
+  if (n > 0) {
+    v16f x[2];
+    v8h w[4];
+    fetch(0);
+    stage(0);
+    if (n > 1) fetch(1);
+    meet();
+    if (second) meet();
+    auto soft = [&](int j, bool more) {
+      t.weights(a, j, lane, fac, x, w);
+      if (more) {
+        stage(j + 1);
+        if (j + 2 < n) fetch(j + 2);
+      }
+    };
+    t.template products<false, true>(nullptr, w, ks[0], x);
+    meet();
+    for (int j = 0; j + 1 < n; ++j) {
+      soft(j, true);
+      meet();
+      t.template products<true, true>(vs[j & 1], w, ks[(j + 1) & 1], x);
+      meet();
+    }
+    soft(n - 1, false);
+    meet();
+    t.template products<true, false>(vs[(n - 1) & 1], w, nullptr, x);
+    if (!second) meet();
+  }
+  t.finish(a, half);
 }
 
 }  // namespace detail
@@ -227,13 +387,28 @@ static hipError_t tile_launch(const Kv8Attn &a, hipStream_t st) {
   detail::kv8_tile_kernel<DP, WAVES><<<(unsigned)(slots * a.Hkv), 64 * WAVES, 0, st>>>(a);
   return hipGetLastError();
 }
+template <int DP>
+static hipError_t pair_launch(const Kv8Attn &a, hipStream_t st) {
+  const int64_t slots = kv8_tile_slots((int64_t)a.T * (a.Hq / a.Hkv), a.B, 256);
+  detail::kv8_pair_kernel<DP><<<(unsigned)(slots * a.Hkv), 512, 0, st>>>(a);
+  return hipGetLastError();
+}
 
 hipError_t launch_kv8_tiles(const Kv8Attn &a, hipStream_t st) {
+#ifdef TW
   switch (kv8_width(a.D)) {
-    case 64: return tile_launch<64, 8>(a, st);
-    case 96: return tile_launch<96, 8>(a, st);
-    case 128: return tile_launch<128, 8>(a, st);
-    case 192: return tile_launch<192, 8>(a, st);
+    case 64: return tile_launch<64, TW>(a, st);
+    case 96: return tile_launch<96, TW>(a, st);
+    case 128: return tile_launch<128, TW>(a, st);
+    case 192: return tile_launch<192, TW>(a, st);
+    default: return tile_launch<256, 4>(a, st);
+  }
+#endif
+  switch (kv8_width(a.D)) {
+    case 64: return pair_launch<64>(a, st);
+    case 96: return pair_launch<96>(a, st);
+    case 128: return pair_launch<128>(a, st);
+    case 192: return pair_launch<192>(a, st);
     default: return tile_launch<256, 4>(a, st);
   }
 }

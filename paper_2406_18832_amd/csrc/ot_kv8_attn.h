@@ -173,6 +173,17 @@ struct Kv8Split {
 
 hipError_t launch_kv8_decode(const Kv8Attn &a, const Kv8Split &s, hipStream_t st);
 hipError_t launch_kv8_combine(const Kv8Attn &a, const Kv8Split &s, hipStream_t st);
-hipError_t launch_kv8_tiles(const Kv8Attn &a, hipStream_t st);
+
+// A launch of tiles in which each one's pages are shared between up to `parts` workgroups,
+// `least` pages and more to each.  rows: all query rows, T Hq; for each of them how many
+// parts it has, and part by part m, L and O [Dp].
+struct Kv8Parts {
+  int parts, least;
+  int64_t rows;
+  int *counts;  // nullptr: one part
+  float *m, *l, *o;
+};
+hipError_t launch_kv8_tiles(const Kv8Attn &a, int rows, const Kv8Parts &p, hipStream_t st);
+hipError_t launch_kv8_join(const Kv8Attn &a, const Kv8Parts &p, hipStream_t st);
 
 }  // namespace ot

@@ -11,6 +11,8 @@ constexpr int64_t kFewRows = 32;
 // Pages to an item, at least, and pages of a sequence up to which it is not split: a
 // second launch takes as long as a workgroup's waves take for so many.
 constexpr int kLeastPages = 4, kWholePages = 16;
+// Parts of a tile's pages, at most.
+constexpr int64_t kMostParts = 64;
 
 bool few_rows(int64_t G, int64_t max_q) { return max_q * G <= kFewRows; }
 
@@ -33,24 +35,68 @@ size_t plan_split(int64_t B, int64_t Hq, int64_t Hkv, int64_t D, int64_t max_q, 
          (size_t)rows * dp * sizeof(float);
 }
 
+// Tiles of many rows: their size and how many parts their pages are shared in.  128 rows
+// take two workgroups to a CU, of which one works while the other starts or ends.  256 rows,
+// one to a CU, take less time for a page, which pays where a tile has many: for 128
+// channels, some 3000 rows and more to a sequence, and a tile for most CUs.  MI355X, 256
+// against 128 rows: an 8192-token prompt of 72 heads 1202 us against 1290, 4096 tokens of 8 x 4
+// heads 151 against 181, 2 x 1024 tokens of 8 x 4 heads in a window of 4096 147 against 160;
+// 2048 tokens of 40 heads 76 against 70, 32 prompts of 512 tokens 279 against 238; with 64
+// channels 8192 tokens of 12 heads 190 against 166.
+// Bytes of the workspace (0: none).
+size_t plan_tiles(int64_t T, int64_t B, int64_t Hq, int64_t Hkv, int64_t D, int &rows, Kv8Parts &p) {
+  const int64_t G = Hq / Hkv, cus = device_cus();
+  const int dp = kv8_width(D);
+  rows = dp == 128 && T * G >= 3000 * B && T * G * Hkv / 256 >= cus * 3 / 4 ? 256 : 128;
+  p = Kv8Parts{};
+  p.parts = 1;
+  p.least = 4;
+  p.rows = T * Hq;
+  const int64_t groups = (T * G / rows + (B + 1) / 2) * Hkv;  // half a tile of each sequence is empty
+  const int64_t room = rows == 128 && dp <= 128 ? 2 * cus : cus;
+  const int64_t parts = kv8_min(room / groups, kMostParts);
+  if (parts <= 1) return 0;
+  p.parts = (int)parts;
+  const int64_t all = p.rows + (p.rows & 1);
+  return sizeof(float) * (size_t)(2 * all + 2 * parts * all + parts * p.rows * dp);
+}
+
 }  // namespace
 
-// Fewer than 2^32 work-items: tiles of 128 rows, and up to wanted + B items, all heads,
-// 256 threads each; rows of a key head below 2^30.
+// Fewer than 2^32 work-items: tiles of 128 rows (several parts only where there are few),
+// up to wanted + B items, all heads, 256 threads each; rows of a key head below 2^30.
 bool attn_kv8_fits(int64_t T, int64_t B, int64_t Hq, int64_t Hkv) {
   const int64_t G = Hq / Hkv, limit = (int64_t(1) << 32) / 256;
-  return T * G < (int64_t(1) << 30) && kv8_tile_slots(T * G, B, 128) * Hkv < limit &&
-         (B + 4096) * Hkv < limit && (Hkv * kFewRows / 4 + 1) * B < limit;
+  return T * G < (int64_t(1) << 30) && (T * G / 128 + B) * Hkv < limit &&
+         (B + 4096) * Hkv < limit && (Hkv * kFewRows / 4 + 1) * B < limit && T * Hq / 4 < limit;
 }
 
 size_t attn_kv8_workspace_bytes(int64_t T, int64_t B, int64_t Hq, int64_t Hkv, int64_t D,
                                 int64_t max_q) {
   Kv8Split s;
-  return plan_split(B, Hq, Hkv, D, max_q, s);
+  Kv8Parts p;
+  int rows;
+  return few_rows(Hq / Hkv, max_q) ? plan_split(B, Hq, Hkv, D, max_q, s)
+                                   : plan_tiles(T, B, Hq, Hkv, D, rows, p);
 }
 
 hipError_t launch_attn_kv8(const Kv8Attn &a, void *workspace, hipStream_t st) {
-  if (!few_rows(a.Hq / a.Hkv, a.max_q)) return launch_kv8_tiles(a, st);
+  if (!few_rows(a.Hq / a.Hkv, a.max_q)) {
+    Kv8Parts p;
+    int rows;
+    const size_t bytes = plan_tiles(a.T, a.B, a.Hq, a.Hkv, a.D, rows, p);
+    if (workspace == nullptr || bytes == 0 || a.cache.max_pages <= kWholePages) {
+      p.parts = 1;
+      return launch_kv8_tiles(a, rows, p, st);
+    }
+    const int64_t all = p.rows + (p.rows & 1);
+    p.counts = static_cast<int *>(workspace);
+    p.m = reinterpret_cast<float *>(p.counts + 2 * all);
+    p.l = p.m + p.parts * all;
+    p.o = p.l + p.parts * all;
+    const hipError_t e = launch_kv8_tiles(a, rows, p, st);
+    return e != hipSuccess ? e : launch_kv8_join(a, p, st);
+  }
   Kv8Split s;
   const size_t bytes = plan_split(a.B, a.Hq, a.Hkv, a.D, a.max_q, s);
   if (workspace == nullptr || bytes == 0 || a.cache.max_pages <= kWholePages) {
@@ -69,14 +115,23 @@ hipError_t launch_attn_kv8(const Kv8Attn &a, void *workspace, hipStream_t st) {
 
 void describe_attn_kv8(int64_t T, int64_t B, int64_t Hq, int64_t Hkv, int64_t D, int64_t max_q,
                        bool workspace, char *buf, size_t len) {
+  if (!few_rows(Hq / Hkv, max_q)) {
+    Kv8Parts p;
+    int rows;
+    plan_tiles(T, B, Hq, Hkv, D, rows, p);
+    if (workspace && p.parts > 1)
+      snprintf(buf, len, "tiles %d, %d parts", rows, p.parts);
+    else
+      snprintf(buf, len, "tiles %d", rows);
+    return;
+  }
   Kv8Split s;
   const size_t bytes = plan_split(B, Hq, Hkv, D, max_q, s);
-  if (!few_rows(Hq / Hkv, max_q))
-    snprintf(buf, len, "tiles 256");
-  else if (workspace && bytes != 0)
-    snprintf(buf, len, "few %d rows, %lld items", max_q * (Hq / Hkv) <= 16 ? 16 : 32, (long long)s.items);
+  const int at_once = 16 * kv8_decode_tiles(kv8_width(D), s.rows);
+  if (workspace && bytes != 0)
+    snprintf(buf, len, "few %d rows, %lld items", at_once, (long long)s.items);
   else
-    snprintf(buf, len, "few %d rows", max_q * (Hq / Hkv) <= 16 ? 16 : 32);
+    snprintf(buf, len, "few %d rows", at_once);
 }
 
 }  // namespace ot

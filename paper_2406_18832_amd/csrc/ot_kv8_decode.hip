@@ -386,6 +386,59 @@ __global__ __launch_bounds__(256) void kv8_combine_kernel(Kv8Attn a, Kv8Split s)
   }
 }
 
+// The parts of tiles' rows joined: a wave to a row of a head, four parts' loads at a time.
+template <int DP>
+__global__ __launch_bounds__(256) void kv8_join_kernel(Kv8Attn a, Kv8Parts p) {
+  constexpr int kPer = (DP + 63) / 64, kAhead = 4;
+  const int lane = threadIdx.x & 63;
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  // rows of no sequence have no count
+  if (row >= p.rows || row < (int64_t)a.cu[0] * a.Hq || row >= (int64_t)a.cu[a.B] * a.Hq) return;
+  const int marked = p.counts[row];  // below 0: the row sees no key
+  const int count = min(abs(marked), p.parts);
+  if (count <= 1) return;
+  float top = kNegInf, sum = 0.f, out[kPer];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) out[i] = 0.f;
+  for (int c0 = 0; c0 < count; c0 += kAhead) {
+    float m[kAhead], l[kAhead], v[kAhead][kPer];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const bool in = c0 + j < count;
+      const int64_t at = (in ? c0 + j : c0) * p.rows + row;
+      m[j] = in ? p.m[at] : kNegInf;
+      l[j] = in ? p.l[at] : 0.f;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const int d = 64 * i + lane;
+        v[j][i] = in && (DP % 64 == 0 || d < DP) ? p.o[at * DP + d] : 0.f;
+      }
+    }
+    float now = top;
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) now = fmaxf(now, m[j]);
+    const float ref = now == kNegInf ? 0.f : now, keep = exp2_fast(top - ref);
+    top = now;
+    sum *= keep;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) out[i] *= keep;
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const float part = exp2_fast(m[j] - ref);
+      sum = __builtin_fmaf(part, l[j], sum);
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) out[i] = __builtin_fmaf(part, v[j][i], out[i]);
+    }
+  }
+  const float scale = 1.f / sum;
+#pragma unroll
+  for (int j = 0; j < kPer; ++j)
+    if (64 * j + lane < a.D)
+      a.Y[row * a.D + 64 * j + lane] = marked < 0 ? 0 : float_to_half_bits(out[j] * scale);
+  if (lane == 0 && a.lse != nullptr)
+    a.lse[row] = marked < 0 ? kNegInf : (top + log2f(sum)) * kLn2;
+}
+
 template <int DP, int RT>
 hipError_t decode_launch(const Kv8Attn &a, int64_t max_rows, const Kv8Split &s, hipStream_t st) {
   const dim3 grid((unsigned)s.items, (unsigned)a.Hkv, (unsigned)((max_rows + 16 * RT - 1) / (16 * RT)));
@@ -424,6 +477,18 @@ hipError_t launch_kv8_combine(const Kv8Attn &a, const Kv8Split &s, hipStream_t s
     case 128: detail::kv8_combine_kernel<128><<<grid, 256, 0, st>>>(a, s); break;
     case 192: detail::kv8_combine_kernel<192><<<grid, 256, 0, st>>>(a, s); break;
     default: detail::kv8_combine_kernel<256><<<grid, 256, 0, st>>>(a, s); break;
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_kv8_join(const Kv8Attn &a, const Kv8Parts &p, hipStream_t st) {
+  const unsigned grid = (unsigned)((p.rows + 3) / 4);
+  switch (kv8_width(a.D)) {
+    case 64: detail::kv8_join_kernel<64><<<grid, 256, 0, st>>>(a, p); break;
+    case 96: detail::kv8_join_kernel<96><<<grid, 256, 0, st>>>(a, p); break;
+    case 128: detail::kv8_join_kernel<128><<<grid, 256, 0, st>>>(a, p); break;
+    case 192: detail::kv8_join_kernel<192><<<grid, 256, 0, st>>>(a, p); break;
+    default: detail::kv8_join_kernel<256><<<grid, 256, 0, st>>>(a, p); break;
   }
   return hipGetLastError();
 }

@@ -19,6 +19,65 @@
 namespace ot {
 namespace detail {
 
+// Which tile a slot is.  A few sequences' tiles come in the order of their pages, the
+// most first (under a causal mask a tile's pages go with its number, and its sequence's
+// earlier tokens count as tiles in front of it), so that the last ones to run are short:
+// with S(x) the number of tiles with x and more tiles before them, slot s is among those
+// with the largest x that S(x) > s has.  Of more than a wave's lanes of sequences, each
+// one's tiles come together, the last first.
+struct Kv8Slot {
+  int b;  // sequence, or -1
+  int64_t tile;
+  Kv8Rows rows;  // the sequence's, and its keys
+  int kv_len;
+};
+template <int kRows>
+__device__ __forceinline__ Kv8Slot kv8_slot(const Kv8Attn &a, int64_t slot, int lane) {
+  const int G = a.Hq / a.Hkv;
+  if (a.B > 64) {
+    const int b = kv8_find(a.B, lane, slot,
+                           [&](int i) { return kv8_tile_slot((int64_t)a.cu[i] * G, i, kRows); });
+    if (b < 0) return {-1, 0, {0, 0}, 0};
+    const Kv8Rows rows = kv8_rows(a.cu[b], a.cu[b + 1], a.T);
+    const int64_t tiles = ((int64_t)rows.n * G + kRows - 1) / kRows;
+    const int64_t tile = tiles - 1 - (slot - kv8_tile_slot((int64_t)a.cu[b] * G, b, kRows));
+    return {tile < 0 || tile >= tiles ? -1 : b, tile, rows, a.kv_len[b]};
+  }
+  int tiles = 0, before = 0, kv_len = 0;
+  Kv8Rows rows{0, 0};
+  if (lane < a.B) {
+    rows = kv8_rows(a.cu[lane], a.cu[lane + 1], a.T);
+    kv_len = a.kv_len[lane];
+    tiles = (int)(((int64_t)rows.n * G + kRows - 1) / kRows);
+    if (a.causal && a.window == 0)
+      before = (int)kv8_min(kv8_max(kv8_len(kv_len, a.cache.max_pages) - rows.n, 0) * G / kRows,
+                            1 << 24);
+  }
+  const auto more = [&](int x) {
+    return __builtin_amdgcn_readlane(wave_upto(max(min(tiles + before - x, tiles), 0)), 63);
+  };
+  if (slot >= more(0)) return {-1, 0, {0, 0}, 0};
+  int x = 0, past = tiles + before;
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) past = max(past, __shfl_xor(past, off));
+  past = __builtin_amdgcn_readfirstlane(past);
+  while (past - x > 1) {
+    const int half = x + (past - x) / 2;
+    if (more(half) > slot)
+      x = half;
+    else
+      past = half;
+  }
+  const int rank = (int)slot - more(x + 1);
+  const bool has = x >= before && x < before + tiles;
+  const uint64_t all = __ballot(has);
+  const bool mine = has && __popcll(all & ((uint64_t(1) << lane) - 1)) == rank;
+  const int b = __builtin_ctzll(__ballot(mine));
+  return {b, x - __builtin_amdgcn_readlane(before, b),
+          {__builtin_amdgcn_readlane(rows.row0, b), __builtin_amdgcn_readlane(rows.n, b)},
+          __builtin_amdgcn_readlane(kv_len, b)};
+}
+
 // A page in LDS, and one wave's 32 rows.
 template <int DP>
 struct Kv8Tile {
@@ -34,33 +93,42 @@ struct Kv8Tile {
   int64_t out;                 // its number among all rows of all heads
   int key_lo, key_hi;          // the keys that it sees
   int all_lo, all_hi;          // that all of the wave's see
+  int any_lo, any_hi;          // that some of them sees
   int key_at, value_at;        // its first halves of a page's K and V in LDS
   v8h q[kSteps];
   v16f o[kOut];
   float m, l;
 
-  // The tile of slot `slot`; false where there is none.
+  int part, parts;             // which of a tile's runs of pages this is
+
+  // The tile of slot `slot` and its `which`-th part of at most p.parts; false where there
+  // is none.
   template <int kRows>
-  __device__ __forceinline__ bool aim(const Kv8Attn &a, int64_t slot, int head_k, int wave, int lane) {
+  __device__ __forceinline__ bool aim(const Kv8Attn &a, const Kv8Parts &p, int64_t slot, int which,
+                                      int head_k, int wave, int lane) {
     const int col = lane & 31, half = lane >> 5;
     const int G = a.Hq / a.Hkv;
     h = head_k;
-    b = kv8_find(a.B, lane, slot,
-                 [&](int i) { return kv8_tile_slot((int64_t)a.cu[i] * G, i, kRows); });
+    const Kv8Slot at = kv8_slot<kRows>(a, slot, lane);
+    b = at.b;
     if (b < 0) return false;
-    const Kv8Rows rows = kv8_rows(a.cu[b], a.cu[b + 1], a.T);
-    // counted from the end: under a causal mask the last tile has the most pages
-    const int64_t tiles = ((int64_t)rows.n * G + kRows - 1) / kRows;
-    const int64_t tile = tiles - 1 - (slot - kv8_tile_slot((int64_t)a.cu[b] * G, b, kRows));
-    if (tile < 0 || tile >= tiles) return false;
-    const int64_t whole = a.kv_len[b];
+    const int64_t tile = at.tile;
+    const Kv8Rows rows = at.rows;
+    const int64_t whole = at.kv_len;
     len = (int)kv8_len(whole, a.cache.max_pages);
     bad = whole > len;
     const int all = rows.n * G, row0 = (int)tile * kRows + 32 * wave;
     const int q0 = (int)tile * kRows / G, q1 = min((int)(tile + 1) * kRows - 1, all - 1) / G;
     const Kv8Span span = kv8_span(len, rows.n, q0, q1 - q0 + 1, a.causal, a.window);
-    first_page = span.p0;
-    pages = span.p1 - span.p0;
+    // even runs of pages, of p.least and more
+    const int count = span.p1 - span.p0, some_parts = max(min(p.parts, (count + p.least - 1) / p.least), 1);
+    const int run = (count + some_parts - 1) / some_parts;
+    part = which;
+    parts = run == 0 ? 1 : (count + run - 1) / run;
+    if (part >= parts) return false;
+    first_page = span.p0 + part * run;
+    pages = min(run, span.p1 - first_page);
+    id = max(lookup(a, lane), 0);  // the first that something waits for
 
     const int row = row0 + col;
     in = row < all;
@@ -81,6 +149,8 @@ struct Kv8Tile {
     key_lo = a.window > 0 ? (int)kv8_max(pos - a.window + 1, 0) : 0;
     const int w0 = min(row0, all - 1) / G, w1 = min(row0 + 31, all - 1) / G;
     all_hi = a.causal ? len - rows.n + w0 : len - 1;
+    any_hi = a.causal ? len - rows.n + w1 : len - 1;
+    any_lo = a.window > 0 ? (int)kv8_max(0, len - rows.n + w0 - a.window + 1) : 0;
     all_lo = a.window > 0 ? (int)kv8_max(0, len - rows.n + w1 - a.window + 1) : 0;
     key_at = (16 * (col >> 4) + 8 * ((col >> 2) & 1) + 4 * ((col >> 3) & 1) + (col & 3)) * kKStride +
              8 * half;
@@ -106,7 +176,7 @@ struct Kv8Tile {
   // The first of page j's pages and heads in the pool (some page for one that it does not
   // have).
   __device__ __forceinline__ int64_t place(const Kv8Attn &a, int j, int lane) {
-    if ((j & 63) == 0) id = max(lookup(a, j + lane), 0);
+    if ((j & 63) == 0 && j > 0) id = max(lookup(a, j + lane), 0);
     return (int64_t)__builtin_amdgcn_readlane(id, j & 63) * a.Hkv + h;
   }
   __device__ __forceinline__ void scales(const Kv8Attn &a, int j, int lane, float fac) {
@@ -125,9 +195,7 @@ struct Kv8Tile {
   }
 
   // Scores of page j to weights.
-  __device__ __forceinline__ void weights(const Kv8Attn &a, int j, int lane, float fac, v16f (&x)[2],
-                                          v8h (&w)[4]) {
-    scales(a, j, lane, fac);
+  __device__ __forceinline__ void weights(int j, int lane, v16f (&x)[2], v8h (&w)[4]) {
     const int half = lane >> 5;
     float pf = lane_float(f, j & 63), plg = lane_float(lg, j & 63);
     const float piv = lane_float(iv, j & 63);
@@ -212,9 +280,24 @@ struct Kv8Tile {
     }
   }
 
-  __device__ __forceinline__ void finish(const Kv8Attn &a, int half) {
+  __device__ __forceinline__ void finish(const Kv8Attn &a, const Kv8Parts &p, int half) {
     l += __shfl_xor(l, 32);
     if (!in) return;
+    if (p.counts != nullptr && part == 0 && half == 0) p.counts[out] = empty ? -parts : parts;
+    if (parts > 1) {
+      const int64_t at = part * p.rows + out;
+      if (half == 0) {
+        p.m[at] = m;
+        p.l[at] = l;
+      }
+#pragma unroll
+      for (int t = 0; t < kOut; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4)
+          *reinterpret_cast<v4f *>(p.o + at * DP + 32 * t + 2 * i + 4 * half) =
+              v4f{o[t][i], o[t][i + 1], o[t][i + 2], o[t][i + 3]};
+      return;
+    }
     const float scale = 1.f / l;
 #pragma unroll
     for (int t = 0; t < kOut; ++t)
@@ -248,7 +331,7 @@ __device__ __forceinline__ void stage16(_Float16 *to, v4u w) {
 // One phase after another: every wave does scores, softmax and values of a page, and its
 // part of the next page's codes, between two barriers.
 template <int DP, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, DP > 192 ? 1 : 2) void kv8_tile_kernel(Kv8Attn a) {
+__global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void kv8_tile_kernel(Kv8Attn a, Kv8Parts parts) {
   using Tile = Kv8Tile<DP>;
   constexpr int kThreads = 64 * WAVES, kUnits = Tile::kUnits;
   constexpr int kLoads = (2 * kUnits + kThreads - 1) / kThreads;  // K's units, then V's
@@ -257,7 +340,10 @@ __global__ __launch_bounds__(64 * WAVES, DP > 192 ? 1 : 2) void kv8_tile_kernel(
   __shared__ __attribute__((aligned(16))) _Float16 vs[2][Tile::kVPage];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   Tile t;
-  if (!t.template aim<32 * WAVES>(a, blockIdx.x / a.Hkv, blockIdx.x % a.Hkv, wave, lane)) return;
+  const int item = blockIdx.x / a.Hkv;
+  if (!t.template aim<32 * WAVES>(a, parts, item / parts.parts, item % parts.parts, blockIdx.x % a.Hkv,
+                                  wave, lane))
+    return;
   const float fac = fabsf(a.scale) * kLog2e;
 
   v4u code[kLoads];
@@ -292,14 +378,18 @@ __global__ __launch_bounds__(64 * WAVES, DP > 192 ? 1 : 2) void kv8_tile_kernel(
     __syncthreads();  // this page is there, and the one before is done with
     const bool more = j + 1 < t.pages;
     if (more) fetch(j + 1);
-    v16f x[2];
-    v8h w[4];
-    t.template products<false, true>(nullptr, w, ks[j & 1], x);
-    t.weights(a, j, lane, fac, x, w);
-    t.template products<true, false>(vs[j & 1], w, nullptr, x);
+    t.scales(a, j, lane, fac);
+    const int token = (t.first_page + j) * kKv8Page;
+    if (token <= t.any_hi && token + kKv8Page > t.any_lo) {  // else no row of the wave sees it
+      v16f x[2];
+      v8h w[4];
+      t.template products<false, true>(nullptr, w, ks[j & 1], x);
+      t.weights(j, lane, x, w);
+      t.template products<true, false>(vs[j & 1], w, nullptr, x);
+    }
     if (more) stage((j + 1) & 1);
   }
-  t.finish(a, lane >> 5);
+  t.finish(a, parts, lane >> 5);
 }
 
 // LDS is as this wave has left it, and the other waves too.  (Global loads stay in flight.)
@@ -318,7 +408,7 @@ __device__ __forceinline__ void meet() {
 // The second brings V: page j + 1 in interval 2 j + 2, over page j - 1, last read in
 // 2 j + 1.  Each therefore has two stages.
 template <int DP>
-__global__ __launch_bounds__(512, 2) void kv8_pair_kernel(Kv8Attn a) {
+__global__ __launch_bounds__(512, 2) void kv8_pair_kernel(Kv8Attn a, Kv8Parts parts) {
   using Tile = Kv8Tile<DP>;
   constexpr int kUnits = Tile::kUnits, kLoads = (kUnits + 255) / 256;
   __shared__ __attribute__((aligned(16))) _Float16 ks[2][Tile::kKPage];
@@ -327,7 +417,9 @@ __global__ __launch_bounds__(512, 2) void kv8_pair_kernel(Kv8Attn a) {
   const int half = lane >> 5, mine = tid & 255;
   const bool second = wave >= 4;
   Tile t;
-  if (!t.template aim<256>(a, blockIdx.x / a.Hkv, blockIdx.x % a.Hkv, wave, lane)) return;
+  const int item = blockIdx.x / a.Hkv;
+  if (!t.template aim<256>(a, parts, item / parts.parts, item % parts.parts, blockIdx.x % a.Hkv, wave, lane))
+    return;
   const float fac = fabsf(a.scale) * kLog2e;
 
   v4u code[kLoads];
@@ -357,7 +449,8 @@ __global__ __launch_bounds__(512, 2) void kv8_pair_kernel(Kv8Attn a) {
     meet();
     if (second) meet();
     auto soft = [&](int j, bool more) {
-      t.weights(a, j, lane, fac, x, w);
+      t.scales(a, j, lane, fac);
+      t.weights(j, lane, x, w);
       if (more) {
         stage(j + 1);
         if (j + 2 < n) fetch(j + 2);
@@ -376,40 +469,31 @@ __global__ __launch_bounds__(512, 2) void kv8_pair_kernel(Kv8Attn a) {
     t.template products<true, false>(vs[(n - 1) & 1], w, nullptr, x);
     if (!second) meet();
   }
-  t.finish(a, half);
+  t.finish(a, parts, half);
 }
 
 }  // namespace detail
 
 template <int DP, int WAVES>
-static hipError_t tile_launch(const Kv8Attn &a, hipStream_t st) {
+static hipError_t tile_launch(const Kv8Attn &a, const Kv8Parts &p, hipStream_t st) {
   const int64_t slots = kv8_tile_slots((int64_t)a.T * (a.Hq / a.Hkv), a.B, 32 * WAVES);
-  detail::kv8_tile_kernel<DP, WAVES><<<(unsigned)(slots * a.Hkv), 64 * WAVES, 0, st>>>(a);
+  detail::kv8_tile_kernel<DP, WAVES><<<(unsigned)(slots * p.parts * a.Hkv), 64 * WAVES, 0, st>>>(a, p);
   return hipGetLastError();
 }
 template <int DP>
-static hipError_t pair_launch(const Kv8Attn &a, hipStream_t st) {
+static hipError_t pair_launch(const Kv8Attn &a, const Kv8Parts &p, hipStream_t st) {
   const int64_t slots = kv8_tile_slots((int64_t)a.T * (a.Hq / a.Hkv), a.B, 256);
-  detail::kv8_pair_kernel<DP><<<(unsigned)(slots * a.Hkv), 512, 0, st>>>(a);
+  detail::kv8_pair_kernel<DP><<<(unsigned)(slots * p.parts * a.Hkv), 512, 0, st>>>(a, p);
   return hipGetLastError();
 }
 
-hipError_t launch_kv8_tiles(const Kv8Attn &a, hipStream_t st) {
-#ifdef TW
+hipError_t launch_kv8_tiles(const Kv8Attn &a, int rows, const Kv8Parts &p, hipStream_t st) {
   switch (kv8_width(a.D)) {
-    case 64: return tile_launch<64, TW>(a, st);
-    case 96: return tile_launch<96, TW>(a, st);
-    case 128: return tile_launch<128, TW>(a, st);
-    case 192: return tile_launch<192, TW>(a, st);
-    default: return tile_launch<256, 4>(a, st);
-  }
-#endif
-  switch (kv8_width(a.D)) {
-    case 64: return pair_launch<64>(a, st);
-    case 96: return pair_launch<96>(a, st);
-    case 128: return pair_launch<128>(a, st);
-    case 192: return pair_launch<192>(a, st);
-    default: return tile_launch<256, 4>(a, st);
+    case 64: return tile_launch<64, 4>(a, p, st);
+    case 96: return tile_launch<96, 4>(a, p, st);
+    case 128: return rows == 256 ? pair_launch<128>(a, p, st) : tile_launch<128, 4>(a, p, st);
+    case 192: return tile_launch<192, 4>(a, p, st);
+    default: return tile_launch<256, 4>(a, p, st);
   }
 }
 

@@ -314,6 +314,26 @@ def test_prompts(Hq, H, D, lengths, counts, causal, window):
     check_attend(*batch(D + Hq, Hq, H, D, lengths, counts, pad=4), causal=causal, window=window)
 
 
+@pytest.mark.parametrize("Hq,H,D,lengths,counts", [
+    (4, 1, 128, [64 * 70 + 5, 300], [40, 300]),       # more pages than a wave's lanes
+    (2, 2, 64, [64 * 140, 64 * 3], [130, 7]), (1, 1, 96, [5000], [33]),
+    (8, 1, 80, [3000, 2000], [20, 1]), (2, 1, 256, [2500], [70]), (1, 1, 192, [4200, 70], [140, 70]),
+    (1, 1, 64, [i % 90 for i in range(75)], [i % 90 for i in range(75)]),  # more sequences
+    (2, 1, 64, [5 + i % 9 for i in range(64)], [i % 5 for i in range(64)])])
+@pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 700)])
+def test_prompts_long_and_many(Hq, H, D, lengths, counts, causal, window):
+    check_attend(*batch(D + Hq, Hq, H, D, lengths, counts, pad=4), causal=causal, window=window,
+                 max_q=min(sum(counts) + 4, max(33, *counts)))
+
+
+def test_prompts_in_large_tiles():
+    """Rows enough for tiles of 256, with a partial one, a prefix and an empty sequence."""
+    for lengths, counts, Hq, H in [([4200], [4150], 16, 16), ([1300, 0, 300], [1250, 0, 300], 64, 8)]:
+        c = batch(21, Hq, H, 112, lengths, counts, pad=3)
+        assert ot.ot_attn_kv8_plan(len(c[1]), len(lengths), Hq, H, 112, max(counts)) == "tiles 256"
+        check_attend(*c, window=0 if len(lengths) > 1 else 150)
+
+
 @pytest.mark.parametrize("counts,max_q", [([5, 70], 70), ([5, 3], 5)])
 def test_rows_without_a_key(counts, max_q):
     """More rows than tokens: the first ones stand before the first key."""

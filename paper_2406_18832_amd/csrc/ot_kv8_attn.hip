@@ -10,8 +10,8 @@ namespace {
 constexpr int64_t kFewRows = 32;
 // Pages to an item, at least, and pages of a sequence up to which it is not split: a
 // second launch takes as long as a workgroup's waves take for so many.
-constexpr int kLeastPages = 4, kWholePages = 16;
-// Parts of a tile's pages, at most.
+constexpr int kLeastPages = 4, kWholePages = 16, kManyPages = 128;
+// Parts of a tile's pages, at most; of four passes of tiles and more none is split.
 constexpr int64_t kMostParts = 64;
 
 bool few_rows(int64_t G, int64_t max_q) { return max_q * G <= kFewRows; }
@@ -39,22 +39,24 @@ size_t plan_split(int64_t B, int64_t Hq, int64_t Hkv, int64_t D, int64_t max_q, 
 // take two workgroups to a CU, of which one works while the other starts or ends.  256 rows,
 // one to a CU, take less time for a page, which pays where a tile has many: for 128
 // channels, some 3000 rows and more to a sequence, and a tile for most CUs.  MI355X, 256
-// against 128 rows: an 8192-token prompt of 72 heads 1202 us against 1290, 4096 tokens of 8 x 4
-// heads 151 against 181, 2 x 1024 tokens of 8 x 4 heads in a window of 4096 147 against 160;
-// 2048 tokens of 40 heads 76 against 70, 32 prompts of 512 tokens 279 against 238; with 64
-// channels 8192 tokens of 12 heads 190 against 166.
+// against 128 rows: an 8192-token prompt of 72 heads 1205 us against 1290, 4096 tokens of
+// 8 x 4 heads 154 against 181, 2 x 1024 tokens of 8 x 4 heads in a window of 4096 147 against
+// 160; 2048 tokens of 40 heads 76 against 70, 32 prompts of 512 tokens 279 against 238; with
+// 64 channels 8192 tokens of 12 heads 190 against 166.  With 192 channels the stages of a
+// page leave LDS for one workgroup of either: 12 prompts of 1300 tokens of 3 x 5 heads 155
+// against 240.  With 256 they leave registers for one wave to a SIMD, and 128 rows.
 // Bytes of the workspace (0: none).
 size_t plan_tiles(int64_t T, int64_t B, int64_t Hq, int64_t Hkv, int64_t D, int &rows, Kv8Parts &p) {
   const int64_t G = Hq / Hkv, cus = device_cus();
   const int dp = kv8_width(D);
-  rows = dp == 128 && T * G >= 3000 * B && T * G * Hkv / 256 >= cus * 3 / 4 ? 256 : 128;
+  rows = dp == 192 || (dp == 128 && T * G >= 3000 * B && T * G * Hkv / 256 >= cus * 3 / 4) ? 256 : 128;
   p = Kv8Parts{};
   p.parts = 1;
   p.least = 4;
   p.rows = T * Hq;
   const int64_t groups = (T * G / rows + (B + 1) / 2) * Hkv;  // half a tile of each sequence is empty
-  const int64_t room = rows == 128 && dp <= 128 ? 2 * cus : cus;
-  const int64_t parts = kv8_min(room / groups, kMostParts);
+  p.groups = (int)(rows == 128 && dp <= 128 ? 2 * cus : cus);
+  const int64_t parts = kv8_min(4 * p.groups / groups, kMostParts);
   if (parts <= 1) return 0;
   p.parts = (int)parts;
   const int64_t all = p.rows + (p.rows & 1);
@@ -85,7 +87,12 @@ hipError_t launch_attn_kv8(const Kv8Attn &a, void *workspace, hipStream_t st) {
     Kv8Parts p;
     int rows;
     const size_t bytes = plan_tiles(a.T, a.B, a.Hq, a.Hkv, a.D, rows, p);
-    if (workspace == nullptr || bytes == 0 || a.cache.max_pages <= kWholePages) {
+    // A tile's pages, at most.  Tiles that fill half of the card are only split where one
+    // of them can have very many: the launch that joins the parts costs a few per cent.
+    int64_t most = a.cache.max_pages;
+    if (a.window > 0) most = kv8_min(most, (a.window + rows) / kKv8Page + 2);
+    const bool few = p.rows / rows * 2 <= p.groups;
+    if (workspace == nullptr || bytes == 0 || most <= (few ? kWholePages : kManyPages)) {
       p.parts = 1;
       return launch_kv8_tiles(a, rows, p, st);
     }

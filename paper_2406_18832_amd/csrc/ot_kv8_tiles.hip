@@ -19,44 +19,88 @@
 namespace ot {
 namespace detail {
 
-// Which tile a slot is.  A few sequences' tiles come in the order of their pages, the
-// most first (under a causal mask a tile's pages go with its number, and its sequence's
-// earlier tokens count as tiles in front of it), so that the last ones to run are short:
-// with S(x) the number of tiles with x and more tiles before them, slot s is among those
-// with the largest x that S(x) > s has.  Of more than a wave's lanes of sequences, each
-// one's tiles come together, the last first.
+// All tiles' pages, of one key head: those of a sequence taken to lie evenly between its
+// first tile's and its last one's.
+template <int kRows>
+__device__ __forceinline__ float kv8_tile_pages(const Kv8Attn &a, int lane) {
+  const int G = a.Hq / a.Hkv;
+  float sum = 0.f;
+  for (int b = lane; b < a.B; b += 64) {
+    const Kv8Rows rows = kv8_rows(a.cu[b], a.cu[b + 1], a.T);
+    if (rows.n == 0) continue;
+    const int64_t len = kv8_len(a.kv_len[b], a.cache.max_pages), q = (kRows + G - 1) / G;
+    const Kv8Span first = kv8_span(len, rows.n, 0, kv8_min(q, rows.n), a.causal, a.window);
+    const Kv8Span last = kv8_span(len, rows.n, kv8_max(rows.n - q, 0), kv8_min(q, rows.n), a.causal, a.window);
+    const float tiles = (float)(((int64_t)rows.n * G + kRows - 1) / kRows);
+    sum += tiles * 0.5f * (float)(first.p1 - first.p0 + last.p1 - last.p0);
+  }
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) sum += __shfl_xor(sum, off);
+  return sum;
+}
+
+// Which tile a key head's i-th workgroup takes, and which part of its pages.
+//
+// A few sequences' tiles come in the order of their pages, the most first (under a causal
+// mask a tile's pages go with its number, and its sequence's earlier tokens count as tiles
+// in front of it), so that the last ones to run are short: with S(x) the number of tiles
+// with x and more tiles before them, the s-th tile is among those with the largest x that
+// S(x) > s has.  Tiles that can have more pages than `run` come with all their parts.
+// Otherwise, and of more than a wave's lanes of sequences, workgroups come part by part:
+// most of the later parts are none, and hold no CU there that something waits for.
 struct Kv8Slot {
   int b;  // sequence, or -1
   int64_t tile;
-  Kv8Rows rows;  // the sequence's, and its keys
+  int part, parts;  // of at most so many, all of which are launched
+  Kv8Rows rows;     // the sequence's, and its keys
   int kv_len;
 };
 template <int kRows>
-__device__ __forceinline__ Kv8Slot kv8_slot(const Kv8Attn &a, int64_t slot, int lane) {
+__device__ __forceinline__ Kv8Slot kv8_slot(const Kv8Attn &a, const Kv8Parts &p, int run, int i, int lane) {
   const int G = a.Hq / a.Hkv;
+  const Kv8Slot none{-1, 0, 0, 0, {0, 0}, 0};
   if (a.B > 64) {
+    const int64_t slot = i % p.slots;
     const int b = kv8_find(a.B, lane, slot,
-                           [&](int i) { return kv8_tile_slot((int64_t)a.cu[i] * G, i, kRows); });
-    if (b < 0) return {-1, 0, {0, 0}, 0};
+                           [&](int x) { return kv8_tile_slot((int64_t)a.cu[x] * G, x, kRows); });
+    if (b < 0) return none;
     const Kv8Rows rows = kv8_rows(a.cu[b], a.cu[b + 1], a.T);
     const int64_t tiles = ((int64_t)rows.n * G + kRows - 1) / kRows;
     const int64_t tile = tiles - 1 - (slot - kv8_tile_slot((int64_t)a.cu[b] * G, b, kRows));
-    return {tile < 0 || tile >= tiles ? -1 : b, tile, rows, a.kv_len[b]};
+    if (tile < 0 || tile >= tiles) return none;
+    return {b, tile, i / p.slots, p.parts, rows, a.kv_len[b]};
   }
+  const bool rising = a.causal && a.window == 0;
   int tiles = 0, before = 0, kv_len = 0;
   Kv8Rows rows{0, 0};
   if (lane < a.B) {
     rows = kv8_rows(a.cu[lane], a.cu[lane + 1], a.T);
     kv_len = a.kv_len[lane];
     tiles = (int)(((int64_t)rows.n * G + kRows - 1) / kRows);
-    if (a.causal && a.window == 0)
-      before = (int)kv8_min(kv8_max(kv8_len(kv_len, a.cache.max_pages) - rows.n, 0) * G / kRows,
-                            1 << 24);
+    if (rising)
+      before = (int)kv8_min(kv8_max(kv8_len(kv_len, a.cache.max_pages) - rows.n, 0) * G / kRows, 1 << 24);
   }
   const auto more = [&](int x) {
     return __builtin_amdgcn_readlane(wave_upto(max(min(tiles + before - x, tiles), 0)), 63);
   };
-  if (slot >= more(0)) return {-1, 0, {0, 0}, 0};
+  const int all = more(0);
+  int slot = i, part = 0, parts = p.parts;
+  if (p.parts > 1) {
+    // a tile with x before it ends before x + 2 tiles' queries and one more
+    const int whole = (int)kv8_min((int64_t)run * kKv8Page * G / kRows, 1 << 24);
+    const int split = rising ? more(max(whole - 1 - (G + kRows - 1) / kRows, 0)) : 0;
+    if (i < split * p.parts) {
+      slot = i / p.parts;
+      part = i % p.parts;
+    } else if (rising) {
+      slot = i - split * (p.parts - 1);
+      parts = 1;
+    } else if (all > 0) {
+      slot = i % all;
+      part = i / all;
+    }
+  }
+  if (slot >= all || part >= p.parts) return none;
   int x = 0, past = tiles + before;
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1) past = max(past, __shfl_xor(past, off));
@@ -68,12 +112,12 @@ __device__ __forceinline__ Kv8Slot kv8_slot(const Kv8Attn &a, int64_t slot, int 
     else
       past = half;
   }
-  const int rank = (int)slot - more(x + 1);
+  const int rank = slot - more(x + 1);
   const bool has = x >= before && x < before + tiles;
-  const uint64_t all = __ballot(has);
-  const bool mine = has && __popcll(all & ((uint64_t(1) << lane) - 1)) == rank;
+  const uint64_t like = __ballot(has);
+  const bool mine = has && __popcll(like & ((uint64_t(1) << lane) - 1)) == rank;
   const int b = __builtin_ctzll(__ballot(mine));
-  return {b, x - __builtin_amdgcn_readlane(before, b),
+  return {b, x - __builtin_amdgcn_readlane(before, b), part, parts,
           {__builtin_amdgcn_readlane(rows.row0, b), __builtin_amdgcn_readlane(rows.n, b)},
           __builtin_amdgcn_readlane(kv_len, b)};
 }
@@ -101,15 +145,19 @@ struct Kv8Tile {
 
   int part, parts;             // which of a tile's runs of pages this is
 
-  // The tile of slot `slot` and its `which`-th part of at most p.parts; false where there
-  // is none.
+  // What the head's i-th workgroup takes; false where that is nothing.
   template <int kRows>
-  __device__ __forceinline__ bool aim(const Kv8Attn &a, const Kv8Parts &p, int64_t slot, int which,
-                                      int head_k, int wave, int lane) {
+  __device__ __forceinline__ bool aim(const Kv8Attn &a, const Kv8Parts &p, int i, int head_k, int wave,
+                                      int lane) {
     const int col = lane & 31, half = lane >> 5;
     const int G = a.Hq / a.Hkv;
     h = head_k;
-    const Kv8Slot at = kv8_slot<kRows>(a, slot, lane);
+    // the longest part: a quarter over a workgroup's share of all pages
+    int most = 1 << 30;
+    if (p.parts > 1)
+      most = max(p.least, (int)fminf(1.25f * kv8_tile_pages<kRows>(a, lane) * (float)a.Hkv / (float)p.groups,
+                                     1e9f) + 1);
+    const Kv8Slot at = kv8_slot<kRows>(a, p, most, i, lane);
     b = at.b;
     if (b < 0) return false;
     const int64_t tile = at.tile;
@@ -120,10 +168,11 @@ struct Kv8Tile {
     const int all = rows.n * G, row0 = (int)tile * kRows + 32 * wave;
     const int q0 = (int)tile * kRows / G, q1 = min((int)(tile + 1) * kRows - 1, all - 1) / G;
     const Kv8Span span = kv8_span(len, rows.n, q0, q1 - q0 + 1, a.causal, a.window);
-    // even runs of pages, of p.least and more
-    const int count = span.p1 - span.p0, some_parts = max(min(p.parts, (count + p.least - 1) / p.least), 1);
+    // even runs of pages, none longer than that where p.parts are enough
+    const int count = span.p1 - span.p0;
+    const int some_parts = max(min(at.parts, (int)(((int64_t)count + most - 1) / most)), 1);
     const int run = (count + some_parts - 1) / some_parts;
-    part = which;
+    part = at.part;
     parts = run == 0 ? 1 : (count + run - 1) / run;
     if (part >= parts) return false;
     first_page = span.p0 + part * run;
@@ -249,7 +298,7 @@ struct Kv8Tile {
   template <bool VALUES, bool SCORES>
   __device__ __forceinline__ void products(const _Float16 *vs, const v8h (&w)[4], const _Float16 *ks,
                                            v16f (&x)[2]) {
-    constexpr int kV = VALUES ? 4 * kOut : 0, kS = SCORES ? 2 * kSteps : 0, kAhead = 6;
+    constexpr int kV = VALUES ? 4 * kOut : 0, kS = SCORES ? 2 * kSteps : 0, kAhead = DP == 192 ? 3 : 6;
     const _Float16 *vp = vs + value_at, *kp = ks + key_at;
     auto fragment = [&](int i) {
       return i < kV ? *reinterpret_cast<const v8h *>(vp + 32 * (i % kOut) * kVStride + 16 * (i / kOut))
@@ -340,10 +389,7 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void kv8_tile_kernel(
   __shared__ __attribute__((aligned(16))) _Float16 vs[2][Tile::kVPage];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   Tile t;
-  const int item = blockIdx.x / a.Hkv;
-  if (!t.template aim<32 * WAVES>(a, parts, item / parts.parts, item % parts.parts, blockIdx.x % a.Hkv,
-                                  wave, lane))
-    return;
+  if (!t.template aim<32 * WAVES>(a, parts, blockIdx.x / a.Hkv, blockIdx.x % a.Hkv, wave, lane)) return;
   const float fac = fabsf(a.scale) * kLog2e;
 
   v4u code[kLoads];
@@ -417,9 +463,7 @@ __global__ __launch_bounds__(512, 2) void kv8_pair_kernel(Kv8Attn a, Kv8Parts pa
   const int half = lane >> 5, mine = tid & 255;
   const bool second = wave >= 4;
   Tile t;
-  const int item = blockIdx.x / a.Hkv;
-  if (!t.template aim<256>(a, parts, item / parts.parts, item % parts.parts, blockIdx.x % a.Hkv, wave, lane))
-    return;
+  if (!t.template aim<256>(a, parts, blockIdx.x / a.Hkv, blockIdx.x % a.Hkv, wave, lane)) return;
   const float fac = fabsf(a.scale) * kLog2e;
 
   v4u code[kLoads];
@@ -475,15 +519,15 @@ __global__ __launch_bounds__(512, 2) void kv8_pair_kernel(Kv8Attn a, Kv8Parts pa
 }  // namespace detail
 
 template <int DP, int WAVES>
-static hipError_t tile_launch(const Kv8Attn &a, const Kv8Parts &p, hipStream_t st) {
-  const int64_t slots = kv8_tile_slots((int64_t)a.T * (a.Hq / a.Hkv), a.B, 32 * WAVES);
-  detail::kv8_tile_kernel<DP, WAVES><<<(unsigned)(slots * p.parts * a.Hkv), 64 * WAVES, 0, st>>>(a, p);
+static hipError_t tile_launch(const Kv8Attn &a, Kv8Parts p, hipStream_t st) {
+  p.slots = (int)kv8_tile_slots((int64_t)a.T * (a.Hq / a.Hkv), a.B, 32 * WAVES);
+  detail::kv8_tile_kernel<DP, WAVES><<<(unsigned)p.slots * p.parts * a.Hkv, 64 * WAVES, 0, st>>>(a, p);
   return hipGetLastError();
 }
 template <int DP>
-static hipError_t pair_launch(const Kv8Attn &a, const Kv8Parts &p, hipStream_t st) {
-  const int64_t slots = kv8_tile_slots((int64_t)a.T * (a.Hq / a.Hkv), a.B, 256);
-  detail::kv8_pair_kernel<DP><<<(unsigned)(slots * p.parts * a.Hkv), 512, 0, st>>>(a, p);
+static hipError_t pair_launch(const Kv8Attn &a, Kv8Parts p, hipStream_t st) {
+  p.slots = (int)kv8_tile_slots((int64_t)a.T * (a.Hq / a.Hkv), a.B, 256);
+  detail::kv8_pair_kernel<DP><<<(unsigned)p.slots * p.parts * a.Hkv, 512, 0, st>>>(a, p);
   return hipGetLastError();
 }
 
@@ -492,7 +536,7 @@ hipError_t launch_kv8_tiles(const Kv8Attn &a, int rows, const Kv8Parts &p, hipSt
     case 64: return tile_launch<64, 4>(a, p, st);
     case 96: return tile_launch<96, 4>(a, p, st);
     case 128: return rows == 256 ? pair_launch<128>(a, p, st) : tile_launch<128, 4>(a, p, st);
-    case 192: return tile_launch<192, 4>(a, p, st);
+    case 192: return rows == 256 ? pair_launch<192>(a, p, st) : tile_launch<192, 4>(a, p, st);
     default: return tile_launch<256, 4>(a, p, st);
   }
 }

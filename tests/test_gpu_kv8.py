@@ -319,7 +319,9 @@ def test_prompts(Hq, H, D, lengths, counts, causal, window):
     (2, 2, 64, [64 * 140, 64 * 3], [130, 7]), (1, 1, 96, [5000], [33]),
     (8, 1, 80, [3000, 2000], [20, 1]), (2, 1, 256, [2500], [70]), (1, 1, 192, [4200, 70], [140, 70]),
     (1, 1, 64, [i % 90 for i in range(75)], [i % 90 for i in range(75)]),  # more sequences
-    (2, 1, 64, [5 + i % 9 for i in range(64)], [i % 5 for i in range(64)])])
+    (2, 1, 64, [5 + i % 9 for i in range(64)], [i % 5 for i in range(64)]),
+    (300, 1, 64, [2500, 1900, 700], [3, 4, 1]),       # a tile is part of a token's heads
+    (6, 2, 16, [64 * 60 + 1, 64 * 59, 10, 64 * 40], [64 * 30, 33, 10, 200])])
 @pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 700)])
 def test_prompts_long_and_many(Hq, H, D, lengths, counts, causal, window):
     check_attend(*batch(D + Hq, Hq, H, D, lengths, counts, pad=4), causal=causal, window=window,

@@ -636,7 +636,7 @@ ot_status ot_attn_kv8(const uint16_t *q, int64_t ldq, int64_t T, int64_t B, int6
                          num_pages};
   a.scale = scale;
   a.causal = causal != 0;
-  a.window = window;
+  a.window = window < kMaxRows ? window : kMaxRows;  // past every position
   a.Y = Y;
   a.lse = lse;
   return hip_status(ot::launch_attn_kv8(a, workspace, static_cast<hipStream_t>(stream)));

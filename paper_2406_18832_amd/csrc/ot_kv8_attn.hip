@@ -65,11 +65,12 @@ size_t plan_tiles(int64_t T, int64_t B, int64_t Hq, int64_t Hkv, int64_t D, int 
 
 }  // namespace
 
-// Fewer than 2^32 work-items: tiles of 128 rows (several parts only where there are few),
-// up to wanted + B items, all heads, 256 threads each; rows of a key head below 2^30.
+// Fewer than 2^32 work-items: T G / 128 + B tiles of 128 rows by 256 threads, or
+// T G / 256 + B of 256 rows by 512 (several parts only where there are few), up to
+// wanted + B items by 256, of all heads; rows of a key head below 2^30.
 bool attn_kv8_fits(int64_t T, int64_t B, int64_t Hq, int64_t Hkv) {
   const int64_t G = Hq / Hkv, limit = (int64_t(1) << 32) / 256;
-  return T * G < (int64_t(1) << 30) && (T * G / 128 + B) * Hkv < limit &&
+  return T * G < (int64_t(1) << 30) && (T * G / 128 + 2 * B) * Hkv < limit &&
          (B + 4096) * Hkv < limit && (Hkv * kFewRows / 4 + 1) * B < limit && T * Hq / 4 < limit;
 }
 

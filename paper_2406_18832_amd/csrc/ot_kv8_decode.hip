@@ -39,8 +39,8 @@ __global__ __launch_bounds__(64 * kDecodeWaves, kv8_decode_waves(DP, RT)) void k
   if (blockIdx.z == 0 && h == 0 && item.index == 0 && threadIdx.x == 0 && s.wanted != 0)
     s.spans[item.b] = make_int2(item.first, item.count);
   if (row_base >= rows) return;
-  const int64_t p0 = seq.span.p0 + (int64_t)item.index * item.chunk;
-  const int64_t p1 = kv8_min(p0 + item.chunk, seq.span.p1);
+  const int p0 = seq.span.p0 + item.index * item.chunk;
+  const int p1 = p0 + min(item.chunk, seq.span.p1 - p0);
 
   // this lane's query rows, and the positions of the keys that they see
   v8h q[RT][kSteps];
@@ -85,9 +85,9 @@ __global__ __launch_bounds__(64 * kDecodeWaves, kv8_decode_waves(DP, RT)) void k
   // page's keys are fetched while the one before goes through softmax and values, its
   // values from there until its own scores are there: both take the registers that the
   // page before has just left.
-  for (int64_t batch = p0 + wave; batch < p1; batch += 64 * kDecodeWaves) {
-    const int64_t mine = batch + kDecodeWaves * lane;
-    const int todo = (int)kv8_min(64, (p1 - batch + kDecodeWaves - 1) / kDecodeWaves);
+  for (int batch = p0 + wave; batch < p1; batch += 64 * kDecodeWaves) {
+    const int mine = batch + kDecodeWaves * lane;
+    const int todo = min(64, (p1 - batch + kDecodeWaves - 1) / kDecodeWaves);
     int64_t page = -1;
     if (mine < p1)
       page = kv8_page(a.cache.table, item.b, mine, a.cache.max_pages, a.cache.num_pages);
@@ -153,7 +153,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, kv8_decode_waves(DP, RT)) void k
       phase();
       if constexpr (more) load_keys(n + 1);
       phase();
-      const int token = (int)((batch + kDecodeWaves * n) * kKv8Page);
+      const int token = (batch + kDecodeWaves * n) * kKv8Page;
       const bool cut = token < all_lo || token + kKv8Page - 1 > all_hi;
       v8h p[RT][2];
 #pragma unroll

@@ -198,7 +198,7 @@ struct Kv8Tile {
     key_lo = a.window > 0 ? (int)kv8_max(pos - a.window + 1, 0) : 0;
     const int w0 = min(row0, all - 1) / G, w1 = min(row0 + 31, all - 1) / G;
     all_hi = a.causal ? len - rows.n + w0 : len - 1;
-    any_hi = a.causal ? len - rows.n + w1 : len - 1;
+    any_hi = row0 >= all ? -1 : a.causal ? len - rows.n + w1 : len - 1;
     any_lo = a.window > 0 ? (int)kv8_max(0, len - rows.n + w0 - a.window + 1) : 0;
     all_lo = a.window > 0 ? (int)kv8_max(0, len - rows.n + w1 - a.window + 1) : 0;
     key_at = (16 * (col >> 4) + 8 * ((col >> 2) & 1) + 4 * ((col >> 3) & 1) + (col & 3)) * kKStride +

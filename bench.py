@@ -69,7 +69,8 @@ def parse():
                    help="only run a plain 1 GiB device copy (calibrates the HBM byte counters)")
     p.add_argument("--quality", action="store_true",
                    help="only run the symmetrization ablation / bit-width sweep of output error "
-                        "against float64 (one JSON line)")
+                        "against float64, and that of attention over an 8-bit key/value cache "
+                        "(one JSON line)")
     p.add_argument("--helper-probe", action="store_true",
                    help="launch the quantizer and the fused LayerNorm on the OPT-13B shapes "
                         "(for counter runs)")
@@ -1025,7 +1026,8 @@ def main():
         from paper_2406_18832_amd import quality
         ot.lib()
         recs = quality.sweep(log=log)
-        print(json.dumps({"quality_sweep": recs}), flush=True)
+        attention = quality.attention_sweep(log=log)
+        print(json.dumps({"quality_sweep": recs, "attention_sweep": attention}), flush=True)
         return
     ot.lib()
     wl = synth.WORKLOADS[args.workload]

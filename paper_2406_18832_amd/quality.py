@@ -3,7 +3,8 @@ workloads: a symmetrization ablation and bit-width sweep standing in for the
 paper's Table 6 (with and without symmetrization, Sec. 4.4) and Table 10
 (W8A6, W6A6, W8A4, W4A4), plus the per-token path of Eq. (c) as the
 baseline the paper argues against (Sec. 2.2), and the same linears on 4-bit
-floating point (MX4) with and without the channels' shift and scale.
+floating point (MX4) with and without the channels' shift and scale, and the
+attention behind a qkv linear with its keys and values in an 8-bit cache.
 
 The paper measures perplexity on checkpoints and datasets that are not used
 here; this measures the error the method introduces in one linear, which is
@@ -96,4 +97,67 @@ def sweep(workloads=("opt6.7b_w8a8", "opt13b_w6a6", "opt66b_w8a8"), rows=256, ca
                 if log:
                     log(f"quality {name}/{lay.name} {label}: rel {rec['rel_fro']:.3e}")
             del X, W, b, minmax, ref
+    return out
+
+
+# Attention behind a workload's qkv linear: (label, path of the linear, None for float64,
+# whether keys and values go through the 8-bit cache)
+ATTENTION_CONFIGS = [("KV8", None, True), ("W8A8", "channel", False), ("W8A8 KV8", "channel", True)]
+
+
+def head_channels(hidden):
+    """Channels of a head: OPT's smaller sizes have 64, the others 128."""
+    return 64 if hidden < 2048 else 128
+
+
+def attention_ref(q, k, v):
+    """Causal softmax(q k^T / sqrt(D)) v of one sequence [tokens, heads, D] in float64."""
+    q, k, v = q.double(), k.double(), v.double()
+    n, heads, D = q.shape
+    hidden = torch.ones(n, n, dtype=torch.bool, device=q.device).triu(1)
+    out = torch.empty_like(q)
+    for h in range(heads):
+        x = (q[:, h] @ k[:, h].t()) * D ** -0.5
+        out[:, h] = x.masked_fill(hidden, float("-inf")).softmax(1) @ v[:, h]
+    return out
+
+
+def attention_kv8(q, k, v, singles=8):
+    """The same through the cache (fp16): a prompt and then `singles` tokens one by one, each
+    written with ot_kv8_append and read by ot_attn_kv8, as a server would."""
+    n, heads, D = q.shape
+    ints = lambda *x: torch.tensor(x, dtype=torch.int32, device=q.device)
+    pages = -(-n // ot.KV8_PAGE)
+    table = torch.randperm(pages, device=q.device).int()[None]
+    cache = ot.kv8_cache(pages, heads, D, q.device)
+    first = max(n - singles, 1)
+    out = torch.empty(n, heads, D, dtype=torch.float16, device=q.device)
+    for lo, hi in [(0, first)] + [(i, i + 1) for i in range(first, n)]:
+        cu, length = ints(0, hi - lo), ints(hi)
+        ot.kv8_append(k[lo:hi], v[lo:hi], cu, length, table, cache)
+        out[lo:hi] = ot.attn_kv8(q[lo:hi], cu, length, table, cache)
+    return out
+
+
+def attention_sweep(workloads=("opt6.7b_w8a8", "opt13b_w6a6", "opt66b_w8a8"), rows=256,
+                    calib_rows=None, calib_batches=None, configs=None, device="cuda", log=None):
+    """Errors of attention over `rows` tokens behind each workload's qkv linear, against
+    float64 attention on the float64 linear.  Returns a list of dicts (workload, config,
+    rel_fro, mean_abs, max_abs)."""
+    out = []
+    for name in workloads:
+        wl = synth.WORKLOADS[name]
+        li = [lay.name for lay in wl.layers].index("qkv")
+        X, W, b, minmax = layer_inputs(wl, li, rows, calib_rows, calib_batches, device)
+        hidden = W.shape[0] // 3
+        heads = lambda y: y.view(rows, 3, hidden // head_channels(hidden), -1).unbind(1)
+        exact = torch.matmul(X.double(), W.double().t()) + b.double()
+        ref = attention_ref(*heads(exact))
+        for label, path, cached in ATTENTION_CONFIGS if configs is None else configs:
+            y = exact.half() if path is None else run_config(X, W, b, minmax, 8, 8, path)
+            Y = attention_kv8(*heads(y)) if cached else attention_ref(*heads(y))
+            rec = dict(workload=name, config=label, **errors(Y, ref))
+            out.append(rec)
+            if log:
+                log(f"quality {name}/attention {label}: rel {rec['rel_fro']:.3e}")
     return out

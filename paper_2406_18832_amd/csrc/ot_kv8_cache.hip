@@ -315,42 +315,63 @@ __global__ __launch_bounds__(64 * kKv8Waves) void kv8_read_kernel(
     const float s = none ? __builtin_nanf("") : cache.Ks[ph];
     const uint8_t *p = cache.Kc + ph * (DP * kKv8Page);
     uint16_t *out = k + (row * H + h) * D;
-#pragma unroll 4
-    for (int u = 0; u < DP / 8; ++u) {
-      const Place<DP, true> place(lane, u);
-      const int t = place.token, c = place.channel;
-      if (t < at.lo || t >= at.hi || c >= D) continue;
-      const v2u w = *reinterpret_cast<const v2u *>(p + t * DP + c);
-      v4u y;
+    constexpr int kAtOnce = DP / 8 < 16 ? DP / 8 : DP / 16;
+#pragma unroll 1
+    for (int u0 = 0; u0 < DP / 8; u0 += kAtOnce) {
+      // loads have no condition, or each would wait for the one before: lanes without a
+      // token take another's
+      v2u w[kAtOnce];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t x = w[i >> 1] >> (16 * (i & 1));
-        y[i] = value_pair(x & 0xffu, x >> 8 & 0xffu, s);
+      for (int u = 0; u < kAtOnce; ++u) {
+        const Place<DP, true> place(lane, u0 + u);
+        w[u] = *reinterpret_cast<const v2u *>(p + min(max(place.token, at.lo), at.hi - 1) * DP + place.channel);
       }
-      __builtin_nontemporal_store(y, reinterpret_cast<v4u *>(out + (int64_t)(t - at.lo) * H * D + c));
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u) {
+        const Place<DP, true> place(lane, u0 + u);
+        const int t = place.token, c = place.channel;
+        if (t < at.lo || t >= at.hi || c >= D) continue;
+        v4u y;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t x = w[u][i >> 1] >> (16 * (i & 1));
+          y[i] = value_pair(x & 0xffu, x >> 8 & 0xffu, s);
+        }
+        __builtin_nontemporal_store(y, reinterpret_cast<v4u *>(out + (int64_t)(t - at.lo) * H * D + c));
+      }
     }
   } else {
     const float s = none ? __builtin_nanf("") : cache.Vs[ph];
     const uint8_t *p = cache.Vc + ph * (DP * kKv8Page);
     uint16_t *out = v + (row * H + h) * D;
+    constexpr int kGroups = Place<DP, false>::kUnits / 8, kAtOnce = kGroups == 3 ? 3 : kGroups < 2 ? 1 : 2;
+    static_assert(kGroups % kAtOnce == 0, "whole groups");
 #pragma unroll 1
-    for (int u = 0; u < Place<DP, false>::kUnits; u += 8) {
-      const Place<DP, false> place(lane, u);
-      const int t = place.token, c = place.channel;
-      if (t + 8 <= at.lo || t >= at.hi || c >= D) continue;
-      v2u w[8];
+    for (int g0 = 0; g0 < kGroups; g0 += kAtOnce) {
+      v2u w[kAtOnce][8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        w[i] = *reinterpret_cast<const v2u *>(p + (c + i) * kKv8Page + t);
+      for (int g = 0; g < kAtOnce; ++g) {
+        const Place<DP, false> place(lane, 8 * (g0 + g));
+        const int t = min(max(place.token, at.lo & ~7), (at.hi - 1) & ~7), c = min(place.channel, DP - 8);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        if (t + j < at.lo || t + j >= at.hi) continue;
-        v4u y;
+        for (int i = 0; i < 8; ++i)
+          w[g][i] = *reinterpret_cast<const v2u *>(p + (c + i) * kKv8Page + t);
+      }
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          y[i] = value_pair(w[2 * i][j >> 2] >> (8 * (j & 3)) & 0xffu,
-                            w[2 * i + 1][j >> 2] >> (8 * (j & 3)) & 0xffu, s);
-        __builtin_nontemporal_store(y, reinterpret_cast<v4u *>(out + (int64_t)(t + j - at.lo) * H * D + c));
+      for (int g = 0; g < kAtOnce; ++g) {
+        const Place<DP, false> place(lane, 8 * (g0 + g));
+        const int t = place.token, c = place.channel;
+        if (t + 8 <= at.lo || t >= at.hi || c >= D) continue;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if (t + j < at.lo || t + j >= at.hi) continue;
+          v4u y;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            y[i] = value_pair(w[g][2 * i][j >> 2] >> (8 * (j & 3)) & 0xffu,
+                              w[g][2 * i + 1][j >> 2] >> (8 * (j & 3)) & 0xffu, s);
+          __builtin_nontemporal_store(y, reinterpret_cast<v4u *>(out + (int64_t)(t + j - at.lo) * H * D + c));
+        }
       }
     }
   }

@@ -122,13 +122,13 @@ __device__ __forceinline__ Kv8Slot kv8_slot(const Kv8Attn &a, const Kv8Parts &p,
           __builtin_amdgcn_readlane(kv_len, b)};
 }
 
-// A page in LDS, and one wave's 32 rows.
-template <int DP>
+// A page's first DC channels (of DP) in LDS, and one wave's 32 rows.
+template <int DP, int DC>
 struct Kv8Tile {
-  static constexpr int kKStride = DP + 8, kVStride = kKv8Page + 8;  // halves; off the banks
-  static constexpr int kKPage = kKv8Page * kKStride, kVPage = DP * kVStride;
-  static constexpr int kSteps = DP / 16, kOut = DP / 32;
-  static constexpr int kUnits = DP * kKv8Page / 16;  // 16 bytes each, of a page's K as of its V
+  static constexpr int kKStride = DC + 8, kVStride = kKv8Page + 8;  // halves; off the banks
+  static constexpr int kKPage = kKv8Page * kKStride, kVPage = DC * kVStride;
+  static constexpr int kSteps = DC / 16, kOut = DC / 32;
+  static constexpr int kUnits = DC * kKv8Page / 16;  // 16 bytes each, of a page's K as of its V
 
   int b, h, len, first_page, pages;
   bool bad;  // more keys than the table has pages for
@@ -363,9 +363,13 @@ struct Kv8Tile {
     if (half == 0 && a.lse != nullptr) a.lse[out] = empty ? kNegInf : (m + log2f(l)) * kLn2;
   }
 
-  // Where 16 codes (unit u of a page's K or V) go in LDS, as fp16.
+  // Where 16 codes (unit u of a page's K; V's are in order) come from, and where they go
+  // in LDS, as fp16.
+  static __device__ __forceinline__ int key_bytes(int u) {
+    return DC == DP ? u * 16 : u / (DC / 16) * DP + u % (DC / 16) * 16;
+  }
   static __device__ __forceinline__ int key_place(int u) {
-    return u / (DP / 16) * kKStride + u % (DP / 16) * 16;
+    return u / (DC / 16) * kKStride + u % (DC / 16) * 16;
   }
   static __device__ __forceinline__ int value_place(int u) {
     return u / (kKv8Page / 16) * kVStride + u % (kKv8Page / 16) * 16;
@@ -381,7 +385,7 @@ __device__ __forceinline__ void stage16(_Float16 *to, v4u w) {
 // part of the next page's codes, between two barriers.
 template <int DP, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void kv8_tile_kernel(Kv8Attn a, Kv8Parts parts) {
-  using Tile = Kv8Tile<DP>;
+  using Tile = Kv8Tile<DP, DP>;
   constexpr int kThreads = 64 * WAVES, kUnits = Tile::kUnits;
   constexpr int kLoads = (2 * kUnits + kThreads - 1) / kThreads;  // K's units, then V's
   static_assert(kUnits % 64 == 0, "whole waves");
@@ -401,7 +405,7 @@ __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void kv8_tile_kernel(
     for (int u = 0; u < kLoads; ++u) {
       const int at = u * kThreads + wave * 64;  // a wave's are all of one kind
       if (at < kUnits)
-        code[u] = __builtin_amdgcn_raw_buffer_load_b128(keys, (u * kThreads + tid) * 16, 0, 0);
+        code[u] = __builtin_amdgcn_raw_buffer_load_b128(keys, Tile::key_bytes(u * kThreads + tid), 0, 0);
       else if (at < 2 * kUnits)
         code[u] = __builtin_amdgcn_raw_buffer_load_b128(values, (u * kThreads + tid - kUnits) * 16, 0, 0);
     }
@@ -453,9 +457,9 @@ __device__ __forceinline__ void meet() {
 // team brings K: page j + 1 in interval 2 j + 1, over page j - 1, last read in 2 j - 1.
 // The second brings V: page j + 1 in interval 2 j + 2, over page j - 1, last read in
 // 2 j + 1.  Each therefore has two stages.
-template <int DP>
+template <int DP, int DC>
 __global__ __launch_bounds__(512, 2) void kv8_pair_kernel(Kv8Attn a, Kv8Parts parts) {
-  using Tile = Kv8Tile<DP>;
+  using Tile = Kv8Tile<DP, DC>;
   constexpr int kUnits = Tile::kUnits, kLoads = (kUnits + 255) / 256;
   __shared__ __attribute__((aligned(16))) _Float16 ks[2][Tile::kKPage];
   __shared__ __attribute__((aligned(16))) _Float16 vs[2][Tile::kVPage];
@@ -474,7 +478,8 @@ __global__ __launch_bounds__(512, 2) void kv8_pair_kernel(Kv8Attn a, Kv8Parts pa
 #pragma unroll
     for (int u = 0; u < kLoads; ++u)
       if (u * 256 + (wave & 3) * 64 < kUnits)
-        code[u] = __builtin_amdgcn_raw_buffer_load_b128(page, (u * 256 + mine) * 16, 0, 0);
+        code[u] = __builtin_amdgcn_raw_buffer_load_b128(
+            page, second ? (u * 256 + mine) * 16 : Tile::key_bytes(u * 256 + mine), 0, 0);
   };
   auto stage = [&](int j) {
 #pragma unroll
@@ -524,10 +529,10 @@ static hipError_t tile_launch(const Kv8Attn &a, Kv8Parts p, hipStream_t st) {
   detail::kv8_tile_kernel<DP, WAVES><<<(unsigned)p.slots * p.parts * a.Hkv, 64 * WAVES, 0, st>>>(a, p);
   return hipGetLastError();
 }
-template <int DP>
+template <int DP, int DC = DP>
 static hipError_t pair_launch(const Kv8Attn &a, Kv8Parts p, hipStream_t st) {
   p.slots = (int)kv8_tile_slots((int64_t)a.T * (a.Hq / a.Hkv), a.B, 256);
-  detail::kv8_pair_kernel<DP><<<(unsigned)p.slots * p.parts * a.Hkv, 512, 0, st>>>(a, p);
+  detail::kv8_pair_kernel<DP, DC><<<(unsigned)p.slots * p.parts * a.Hkv, 512, 0, st>>>(a, p);
   return hipGetLastError();
 }
 
@@ -536,7 +541,7 @@ hipError_t launch_kv8_tiles(const Kv8Attn &a, int rows, const Kv8Parts &p, hipSt
     case 64: return tile_launch<64, 4>(a, p, st);
     case 96: return tile_launch<96, 4>(a, p, st);
     case 128: return rows == 256 ? pair_launch<128>(a, p, st) : tile_launch<128, 4>(a, p, st);
-    case 192: return rows == 256 ? pair_launch<192>(a, p, st) : tile_launch<192, 4>(a, p, st);
+    case 192: return a.D <= 160 ? pair_launch<192, 160>(a, p, st) : pair_launch<192>(a, p, st);
     default: return tile_launch<256, 4>(a, p, st);
   }
 }

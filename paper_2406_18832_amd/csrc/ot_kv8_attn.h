@@ -23,7 +23,7 @@
 namespace ot {
 namespace detail {
 
-constexpr float kSet = 8.f, kMost = 15.f;
+constexpr float kSet = 8.f, kMost = 15.f, kMostSum = 32768.f;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kNegInf = -__builtin_inff();

@@ -264,33 +264,41 @@ struct Kv8Tile {
         plg = 0.f;
       }
     }
-    float most = kNegInf;
+    float sum;
+    const auto all_weights = [&] {
+      const float off = plg - (m == kNegInf ? 0.f : m);  // no key yet
+      sum = 0.f;
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+      for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) most = fmaxf(most, x[t][i]);
-    most = __builtin_fmaf(max_xor32(most), pf, plg);  // a row's largest exponent
-    if (__any(most > m + kMost)) {
-      const float now = most > m + kMost ? most - kSet : m;
+        for (int i = 0; i < 16; ++i) {
+          const float e = exp2_fast(__builtin_fmaf(x[t][i], pf, off));
+          sum += e;
+          w[2 * t + (i >> 3)][i & 7] = (_Float16)e;
+        }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(w[i]));  // here, not among the products
+    };
+    all_weights();
+    // The largest exponent is looked for only where weights are too large, or have no
+    // reference yet.
+    if (__any(sum > kMostSum || m == kNegInf)) {
+      asm volatile("");
+      float most = kNegInf;
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) most = fmaxf(most, x[t][i]);
+      most = __builtin_fmaf(max_xor32(most), pf, plg);
+      const float now = fmaxf(m, most - kSet);
       const float keep = m == now ? 1.f : exp2_fast(m - now);
       m = now;
       l *= keep;
 #pragma unroll
       for (int t = 0; t < kOut; ++t) o[t] *= keep;
+      all_weights();
     }
-    const float off = plg - (m == kNegInf ? 0.f : m);  // no key yet
-    float sum = 0.f;
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const float e = exp2_fast(__builtin_fmaf(x[t][i], pf, off));
-        sum += e;
-        w[2 * t + (i >> 3)][i & 7] = (_Float16)e;
-      }
     l = __builtin_fmaf(sum, piv, l);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(w[i]));  // they are done here, not among the products
   }
 
   // Products in a row: O += V W where VALUES (w of a page, its V at vs), X = K Q where

@@ -624,7 +624,7 @@ ot_status ot_kv8_append(const uint16_t *k, int64_t ldk, const uint16_t *v,
  * ot_kv8_read -- tokens of the cache as fp16(fp32(code s)), dense: rows cu[b] ..
  * cu[b+1] - 1 of k and v receive sequence b's tokens from position start[b] ([B]
  * int32) on.  Rows of a page that the pool does not have, and of positions below 0,
- * are NaN.
+ * are NaN.  (A value near fp16's largest can come back as infinity: it is off by up to s.)
  *   k, v   [T x H x D] fp16 outputs (device).
  * Asynchronous on stream.
  */
@@ -649,16 +649,19 @@ ot_status ot_kv8_read(const uint8_t *Kc, const uint8_t *Vc, const float *Ks,
  * table makes all of its sequence's rows NaN.
  *   q      [T x Hq x D] fp16, rows ldq elements apart (>= Hq D, a multiple of 8).
  *   Hq     1 .. 16384, a multiple of Hkv.
- *   scale  finite.   window  >= 0; 0: all keys (OT_EINVAL for others, and for a window
- *          without causal).
+ *   scale  finite (scores past fp32's range are unspecified).   window  >= 0; 0: all
+ *          keys (OT_EINVAL for others, and for a window without causal).
  *   max_q  1 .. T: no sequence has more rows than this (1 for decode).  Up to 32 rows to
  *          a key head (max_q Hq / Hkv) a kernel for few rows runs, which reads the cache
- *          at memory speed; rows of a sequence past max_q may be left as they were.
+ *          at memory speed; rows of a sequence past max_q may be left as they were.  A
+ *          prompt among many single tokens is faster as a call of its own where a key
+ *          head has few query heads (a token takes a tile of 128 rows then).
  *   Y      [T x Hq x D] fp16 output, lse [T x Hq] fp32 output or NULL (device).
  *   workspace  NULL, or at least ot_attn_kv8_workspace_size(T, B, Hq, Hkv, D, max_q)
  *          bytes of 16-byte aligned scratch (device), with which a sequence's keys are
- *          shared between workgroups.  It needs no initialization; calls that overlap in
- *          time must not share one.
+ *          shared between workgroups: few rows where tables have more than 16 pages,
+ *          tiles where they would leave much of the device idle.  It needs no
+ *          initialization; calls that overlap in time must not share one.
  * The order of the sums is fixed by the sizes, the lengths and whether there is a
  * workspace: the same call gives the same bits.  Asynchronous on stream; no
  * synchronization, no allocation.
@@ -678,7 +681,7 @@ size_t ot_attn_kv8_workspace_size(int64_t T, int64_t B, int64_t Hq, int64_t Hkv,
  * ot_attn_kv8_plan -- which kernel configuration ot_attn_kv8 launches for these sizes
  * on the current device, as ot_qlinear_plan: "none" (T or B == 0), "few <rows> rows"
  * (16 or 32 at a time), with ", <items> items" at most where a sequence's keys are shared
- * between workgroups (with tables of more than 16 pages), or "tiles <rows>".
+ * between workgroups, or "tiles <rows>", with ", <parts> parts" at most where a tile's are.
  */
 ot_status ot_attn_kv8_plan(int64_t T, int64_t B, int64_t Hq, int64_t Hkv,
                            int64_t D, int64_t max_q, int with_workspace,

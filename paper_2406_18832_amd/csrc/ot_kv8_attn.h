@@ -8,9 +8,11 @@
 //
 // The weights 2^(x_j + l_j - m) are an operand of the matrix cores in fp16 (half a
 // step is 2^-11 of a weight).  m is set kSet binades under the largest exponent and stays
-// while that grows by no more than kMost - kSet: O and L are scaled anew a few times in a
-// row's life, weights stay below 2^15, and fp16's normal numbers reach 2^-22 of the
-// largest, what is lost below is at most 2^-33 of it for a key.  L sums the fp32 weights.
+// until a weight would pass 2^kMost: O and L are scaled anew a few times in a row's life,
+// and fp16's normal numbers reach 2^-22 of the largest, what is lost below is at most
+// 2^-33 of it for a key.  L sums the fp32 weights.  (Tiles, whose time goes by vector
+// instructions, look for the largest exponent only where the sum of a lane's weights of a
+// page, none of which is larger than it, passes kMostSum or a row has no m yet.)
 //
 // Which weight belongs to which token.  S^T = K Q^T has tokens as the MFMA's rows
 // and queries as its columns, and leaves a lane with weights of one query alone,

@@ -39,12 +39,13 @@ size_t plan_split(int64_t B, int64_t Hq, int64_t Hkv, int64_t D, int64_t max_q, 
 // take two workgroups to a CU, of which one works while the other starts or ends.  256 rows,
 // one to a CU, take less time for a page, which pays where a tile has many: for 128
 // channels, some 3000 rows and more to a sequence, and a tile for most CUs.  MI355X, 256
-// against 128 rows: an 8192-token prompt of 72 heads 1205 us against 1290, 4096 tokens of
-// 8 x 4 heads 154 against 181, 2 x 1024 tokens of 8 x 4 heads in a window of 4096 147 against
-// 160; 2048 tokens of 40 heads 76 against 70, 32 prompts of 512 tokens 279 against 238; with
-// 64 channels 8192 tokens of 12 heads 190 against 166.  With 192 channels the stages of a
-// page leave LDS for one workgroup of either: 12 prompts of 1300 tokens of 3 x 5 heads 155
-// against 240.  With 256 they leave registers for one wave to a SIMD, and 128 rows.
+// against 128 rows: an 8192-token prompt of 72 heads 1165 us against 1268, 4096 tokens of
+// 8 x 4 heads 149 against 177, 2 x 1024 tokens of 8 x 4 heads in a window of 4096 147 against
+// 166; 2048 tokens of 40 heads 72 against 67, 32 prompts of 512 tokens 279 against 232; with
+// 64 channels 8192 tokens of 12 heads 186 against 164, with 96 up to 3 % less.  With 192
+// channels the stages of a page leave LDS for one workgroup of either: 12 prompts of 1300
+// tokens of 3 x 5 heads of 144 channels 155 against 240 (150 in products of 160 channels).
+// With 256 they leave registers for one wave to a SIMD, and 128 rows.
 // Bytes of the workspace (0: none).
 size_t plan_tiles(int64_t T, int64_t B, int64_t Hq, int64_t Hkv, int64_t D, int &rows, Kv8Parts &p) {
   const int64_t G = Hq / Hkv, cus = device_cus();

@@ -3,6 +3,11 @@
 // Both are memory-bound (2 bytes of fp16 and 1 of codes per value) and take a
 // wave to a page of one head, keys or values, with the whole page in registers:
 // lane l holds 8 channels of Dp / 8 tokens.
+//
+// MI355X: four prompts of 1900-2048 tokens of 56 heads of 128 channels written in 66 us
+// (340 MB at 5.1 TB/s; a copy reaches 5.15) and read back in 57 (6.0).  A step's single
+// tokens of 64 sequences are a launch and a few latencies, 10.4 us for 40 heads: their
+// values are bytes of 5120 cache lines each.
 #include <math.h>
 
 #include "ot_kv8.h"

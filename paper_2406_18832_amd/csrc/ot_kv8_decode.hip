@@ -8,6 +8,14 @@
 // those of two; with a single row 15/16 of the matrix cores' work is for nothing,
 // which costs less than the loads take.
 //
+// MI355X, cache bytes per time, where a large read reaches 6.2 TB/s: 4 sequences of
+// 32000-131000 keys of 8 heads of 128 channels with 4 query heads each 109 us (6.1 TB/s),
+// 64 sequences of 100-2047 keys of 40 heads 127 us (5.6), 5 tokens of 16 sequences of
+// 900-8000 keys 37 us (4.0: four or five pages to a wave, and the joining).  One sequence
+// of 200 keys is 5 us, three memory latencies behind each other.  Codes pass the caches
+// by (with them kept 147 us in place of 130), and the card is filled once: with more and
+// smaller items their starts and their joining cost more than the evener end gives.
+//
 // Lane l has query row l mod 16 and, with g = l / 16, tokens 16 g .. 16 g + 15 of a
 // page: K's row 4 g' + i of the s-th of four products is token 16 g' + 4 s + i.
 // V^T's rows are channels, its 16 bytes of a lane are tokens 16 g .. of one channel.

@@ -115,6 +115,16 @@ def test_few_rows_take_one_launch_where_tables_are_short(launch):
     assert [len(g[1]) for g in launch(calls)] == [1, 1, 1, 2]
 
 
+def test_plans_say_how_tiles_are_shared():
+    plan, size = ot.ot_attn_kv8_plan, ot.ot_attn_kv8_workspace_size
+    assert plan(64, 1, 8, 8, 128, 64, True) == "tiles 128, 64 parts" and size(64, 1, 8, 8, 128, 64) > 0
+    assert plan(64, 1, 8, 8, 128, 64) == "tiles 128"
+    for s in ((8192, 1, 72, 72, 128, 8192), (4096, 64, 40, 40, 128, 64), (4096, 1, 64, 64, 160, 4096)):
+        # as many tiles as the device takes at a time, several times over
+        assert plan(*s, True) == plan(*s) == f"tiles {256 if s[4] == 160 or s[0] == 8192 else 128}"
+        assert size(*s) == 0
+
+
 @pytest.mark.timeout(900)
 @pytest.mark.parametrize("src", ["ot_kv8_cache.hip", "ot_kv8_decode.hip", "ot_kv8_tiles.hip"])
 def test_kernels_do_not_spill(src, tmp_path):

@@ -130,12 +130,13 @@ __device__ __forceinline__ Kv8Slot kv8_slot(const Kv8Attn &a, const Kv8Parts &p,
           __builtin_amdgcn_readlane(kv_len, b)};
 }
 
-// A page's first DC channels (of DP) in LDS, and one wave's 32 rows.
+// A page's first DC channels (of DP) in LDS, and one wave's 32 rows.  (V's rows past them,
+// up to a whole product's, are never written: nor are the channels that come of them.)
 template <int DP, int DC>
 struct Kv8Tile {
   static constexpr int kKStride = DC + 8, kVStride = kKv8Page + 8;  // halves; off the banks
-  static constexpr int kKPage = kKv8Page * kKStride, kVPage = DC * kVStride;
-  static constexpr int kSteps = DC / 16, kOut = DC / 32;
+  static constexpr int kSteps = DC / 16, kOut = (DC + 31) / 32;
+  static constexpr int kKPage = kKv8Page * kKStride, kVPage = 32 * kOut * kVStride;
   static constexpr int kUnits = DC * kKv8Page / 16;  // 16 bytes each, of a page's K as of its V
 
   int b, h, len, first_page, pages;
@@ -399,9 +400,9 @@ __device__ __forceinline__ void stage16(_Float16 *to, v4u w) {
 
 // One phase after another: every wave does scores, softmax and values of a page, and its
 // part of the next page's codes, between two barriers.
-template <int DP, int WAVES>
+template <int DP, int DC, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, DP > 128 ? 1 : 2) void kv8_tile_kernel(Kv8Attn a, Kv8Parts parts) {
-  using Tile = Kv8Tile<DP, DP>;
+  using Tile = Kv8Tile<DP, DC>;
   constexpr int kThreads = 64 * WAVES, kUnits = Tile::kUnits;
   constexpr int kLoads = (2 * kUnits + kThreads - 1) / kThreads;  // K's units, then V's
   static_assert(kUnits % 64 == 0, "whole waves");
@@ -540,10 +541,10 @@ __global__ __launch_bounds__(512, 2) void kv8_pair_kernel(Kv8Attn a, Kv8Parts pa
 
 }  // namespace detail
 
-template <int DP, int WAVES>
+template <int DP, int DC = DP, int WAVES = 4>
 static hipError_t tile_launch(const Kv8Attn &a, Kv8Parts p, hipStream_t st) {
   p.slots = (int)kv8_tile_slots((int64_t)a.T * (a.Hq / a.Hkv), a.B, 32 * WAVES);
-  detail::kv8_tile_kernel<DP, WAVES><<<(unsigned)p.slots * p.parts * a.Hkv, 64 * WAVES, 0, st>>>(a, p);
+  detail::kv8_tile_kernel<DP, DC, WAVES><<<(unsigned)p.slots * p.parts * a.Hkv, 64 * WAVES, 0, st>>>(a, p);
   return hipGetLastError();
 }
 template <int DP, int DC = DP>
@@ -554,12 +555,17 @@ static hipError_t pair_launch(const Kv8Attn &a, Kv8Parts p, hipStream_t st) {
 }
 
 hipError_t launch_kv8_tiles(const Kv8Attn &a, int rows, const Kv8Parts &p, hipStream_t st) {
-  switch (kv8_width(a.D)) {
-    case 64: return tile_launch<64, 4>(a, p, st);
-    case 96: return tile_launch<96, 4>(a, p, st);
-    case 128: return rows == 256 ? pair_launch<128>(a, p, st) : tile_launch<128, 4>(a, p, st);
-    case 192: return a.D <= 160 ? pair_launch<192, 160>(a, p, st) : pair_launch<192>(a, p, st);
-    default: return tile_launch<256, 4>(a, p, st);
+  // The widths that a head's 16 channels make, but for the narrowest and the widest.
+  switch ((a.D + 15) / 16) {
+    case 5: return tile_launch<96, 80>(a, p, st);
+    case 6: return tile_launch<96>(a, p, st);
+    case 7: return rows == 256 ? pair_launch<128, 112>(a, p, st) : tile_launch<128, 112>(a, p, st);
+    case 8: return rows == 256 ? pair_launch<128>(a, p, st) : tile_launch<128>(a, p, st);
+    case 9: return pair_launch<192, 144>(a, p, st);
+    case 10: return pair_launch<192, 160>(a, p, st);
+    case 11: return pair_launch<192, 176>(a, p, st);
+    case 12: return pair_launch<192>(a, p, st);
+    default: return a.D <= 64 ? tile_launch<64>(a, p, st) : tile_launch<256>(a, p, st);
   }
 }
 

@@ -314,6 +314,13 @@ def test_prompts(Hq, H, D, lengths, counts, causal, window):
     check_attend(*batch(D + Hq, Hq, H, D, lengths, counts, pad=4), causal=causal, window=window)
 
 
+@pytest.mark.parametrize("D", range(16, 257, 16))
+def test_every_width(D):
+    """A prompt, a piece over many pages (shared) and single tokens of every width."""
+    check_attend(*batch(D, 3, 1, D, [150, 1700], [150, 90], pad=1))
+    check_attend(*batch(D + 1, 2, 2, D, [150, 1300], [1, 1], pad=1))
+
+
 @pytest.mark.parametrize("Hq,H,D,lengths,counts", [
     (4, 1, 128, [64 * 70 + 5, 300], [40, 300]),       # more pages than a wave's lanes
     (2, 2, 64, [64 * 140, 64 * 3], [130, 7]), (1, 1, 96, [5000], [33]),

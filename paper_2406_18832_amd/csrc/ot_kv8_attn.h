@@ -177,11 +177,12 @@ hipError_t launch_kv8_decode(const Kv8Attn &a, const Kv8Split &s, hipStream_t st
 hipError_t launch_kv8_combine(const Kv8Attn &a, const Kv8Split &s, hipStream_t st);
 
 // A launch of tiles in which one's pages are shared between up to `parts` workgroups,
-// `least` pages and more to each; `groups` of them run at a time.  slots: tiles of one
-// key head at most; rows: all query rows, T Hq; for each of them how many
-// parts it has, and part by part m, L and O [Dp].
+// `least` pages and more to each; `groups` of them run at a time, each key head has
+// `slots`.  rows: all query rows, T Hq; for each of them how many parts it has, and part
+// by part m, L and O [Dp].
 struct Kv8Parts {
   int parts, least, groups, slots;
+  int whole;  // pages up to which a tile is not split
   int64_t rows;
   int *counts;  // nullptr: one part
   float *m, *l, *o;

@@ -9,12 +9,22 @@ namespace {
 // Up to so many query rows to a key head and sequence the kernel for few rows runs.
 constexpr int64_t kFewRows = 32;
 // Pages to an item, at least, and pages of a sequence up to which it is not split: a
-// second launch takes as long as a workgroup's waves take for so many.
+// second launch takes as long as a workgroup's waves take for so many (of tiles that leave
+// less than half of the device idle: a few per cent, which pays from kManyPages on; 1941
+// tokens of 24 heads over 9000-48000 keys, 364 tiles for 512 workgroups, 485 us against
+// 1058).  More tiles than the device takes at a time are not split (8192 tokens of 12 heads
+// of 64 channels, 768 tiles: 161 us against 200).
 constexpr int kLeastPages = 4, kWholePages = 16, kManyPages = 128;
-// Parts of a tile's pages, at most; of four passes of tiles and more none is split.
+// Parts of a tile's pages, at most.
 constexpr int64_t kMostParts = 64;
 
 bool few_rows(int64_t G, int64_t max_q) { return max_q * G <= kFewRows; }
+
+// Pages that `tokens` of a sequence one after another see, at most.
+int64_t most_pages(const Kv8Attn &a, int64_t tokens) {
+  const int64_t all = a.cache.max_pages;
+  return a.window > 0 ? kv8_min(all, (a.window + tokens) / kKv8Page + 2) : all;
+}
 
 // How a call of few rows is split, and the bytes that takes (0: not at all).
 size_t plan_split(int64_t B, int64_t Hq, int64_t Hkv, int64_t D, int64_t max_q, Kv8Split &s) {
@@ -55,11 +65,12 @@ size_t plan_tiles(int64_t T, int64_t B, int64_t Hq, int64_t Hkv, int64_t D, int 
   p.parts = 1;
   p.least = 4;
   p.rows = T * Hq;
-  const int64_t groups = (T * G / rows + (B + 1) / 2) * Hkv;  // half a tile of each sequence is empty
+  const int64_t tiles = (T * G / rows + (B + 1) / 2) * Hkv;  // half a tile of each sequence is empty
   p.groups = (int)(rows == 128 && dp <= 128 ? 2 * cus : cus);
-  const int64_t parts = kv8_min(4 * p.groups / groups, kMostParts);
-  if (parts <= 1) return 0;
+  if (tiles > p.groups) return 0;
+  const int64_t parts = kv8_min(4 * p.groups / tiles, kMostParts);
   p.parts = (int)parts;
+  p.whole = 2 * tiles <= p.groups ? kWholePages : kManyPages;
   const int64_t all = p.rows + (p.rows & 1);
   return sizeof(float) * (size_t)(2 * all + 2 * parts * all + parts * p.rows * dp);
 }
@@ -89,12 +100,7 @@ hipError_t launch_attn_kv8(const Kv8Attn &a, void *workspace, hipStream_t st) {
     Kv8Parts p;
     int rows;
     const size_t bytes = plan_tiles(a.T, a.B, a.Hq, a.Hkv, a.D, rows, p);
-    // A tile's pages, at most.  Tiles that fill half of the card are only split where one
-    // of them can have very many: the launch that joins the parts costs a few per cent.
-    int64_t most = a.cache.max_pages;
-    if (a.window > 0) most = kv8_min(most, (a.window + rows) / kKv8Page + 2);
-    const bool few = p.rows / rows * 2 <= p.groups;
-    if (workspace == nullptr || bytes == 0 || most <= (few ? kWholePages : kManyPages)) {
+    if (workspace == nullptr || bytes == 0 || most_pages(a, rows) <= p.whole) {
       p.parts = 1;
       return launch_kv8_tiles(a, rows, p, st);
     }
@@ -108,7 +114,7 @@ hipError_t launch_attn_kv8(const Kv8Attn &a, void *workspace, hipStream_t st) {
   }
   Kv8Split s;
   const size_t bytes = plan_split(a.B, a.Hq, a.Hkv, a.D, a.max_q, s);
-  if (workspace == nullptr || bytes == 0 || a.cache.max_pages <= kWholePages) {
+  if (workspace == nullptr || bytes == 0 || most_pages(a, a.max_q) <= kWholePages) {
     s.wanted = 0;
     s.items = a.B;
     return launch_kv8_decode(a, s, st);

@@ -27,105 +27,128 @@
 namespace ot {
 namespace detail {
 
-// All tiles' pages, of one key head: those of a sequence taken to lie evenly between its
-// first tile's and its last one's.
+// A sequence's tiles, and the pages of its first and its last one.
+struct Kv8Tiles {
+  Kv8Rows rows;
+  int kv_len, tiles, first, last;
+};
 template <int kRows>
-__device__ __forceinline__ float kv8_tile_pages(const Kv8Attn &a, int lane) {
-  const int G = a.Hq / a.Hkv;
-  float sum = 0.f;
-  for (int b = lane; b < a.B; b += 64) {
-    const Kv8Rows rows = kv8_rows(a.cu[b], a.cu[b + 1], a.T);
-    if (rows.n == 0) continue;
-    const int64_t len = kv8_len(a.kv_len[b], a.cache.max_pages), q = (kRows + G - 1) / G;
-    const Kv8Span first = kv8_span(len, rows.n, 0, kv8_min(q, rows.n), a.causal, a.window);
-    const Kv8Span last = kv8_span(len, rows.n, kv8_max(rows.n - q, 0), kv8_min(q, rows.n), a.causal, a.window);
-    const float tiles = (float)(((int64_t)rows.n * G + kRows - 1) / kRows);
-    sum += tiles * 0.5f * (float)(first.p1 - first.p0 + last.p1 - last.p0);
-  }
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) sum += __shfl_xor(sum, off);
-  return sum;
+__device__ __forceinline__ Kv8Tiles kv8_tiles(const Kv8Attn &a, int b) {
+  Kv8Tiles s{{0, 0}, 0, 0, 0, 0};
+  if (b >= a.B) return s;
+  s.rows = kv8_rows(a.cu[b], a.cu[b + 1], a.T);
+  s.kv_len = a.kv_len[b];
+  const int G = a.Hq / a.Hkv, n = s.rows.n;
+  s.tiles = (int)(((int64_t)n * G + kRows - 1) / kRows);
+  const int64_t len = kv8_len(s.kv_len, a.cache.max_pages), q = kv8_min((kRows + G - 1) / G, n);
+  const Kv8Span first = kv8_span(len, n, 0, q, a.causal, a.window);
+  const Kv8Span last = kv8_span(len, n, n - q, q, a.causal, a.window);
+  s.first = first.p1 - first.p0;
+  s.last = last.p1 - last.p0;
+  return s;
 }
 
 // Which tile a key head's i-th workgroup takes, and which part of its pages.
-//
-// A few sequences' tiles come in the order of their pages, the most first (under a causal
-// mask a tile's pages go with its number, and its sequence's earlier tokens count as tiles
-// in front of it), so that the last ones to run are short: with S(x) the number of tiles
-// with x and more tiles before them, the s-th tile is among those with the largest x that
-// S(x) > s has.  Tiles that can have more pages than `run` come with all their parts.
-// Otherwise, and of more than a wave's lanes of sequences, workgroups come part by part:
-// most of the later parts are none, and hold no CU there that something waits for.
 struct Kv8Slot {
   int b;  // sequence, or -1
   int64_t tile;
-  int part, parts;  // of at most so many, all of which are launched
-  Kv8Rows rows;     // the sequence's, and its keys
+  int part, parts, most;  // of at most so many with so many pages each
+  Kv8Rows rows;           // the sequence's, and its keys
   int kv_len;
 };
+
+// With tiles' pages shared between workgroups: all of a sequence's tiles come in as many
+// parts as its last one needs.  A part has a quarter over a workgroup's even share of all
+// pages (those of a sequence's tiles taken to lie evenly between the first one's and the
+// last one's), or more where the launch has too few workgroups for that.
 template <int kRows>
-__device__ __forceinline__ Kv8Slot kv8_slot(const Kv8Attn &a, const Kv8Parts &p, int run, int i, int lane) {
+__device__ __forceinline__ Kv8Slot kv8_part(const Kv8Attn &a, const Kv8Parts &p, int i, int lane) {
+  const Kv8Tiles front = kv8_tiles<kRows>(a, lane);
+  const auto seq = [&](int b0) { return b0 == 0 ? front : kv8_tiles<kRows>(a, b0 + lane); };
+  float pages = 0.f;
+  for (int b0 = 0; b0 < a.B; b0 += 64) {
+    const Kv8Tiles s = seq(b0);
+    pages += 0.5f * (float)s.tiles * (float)(s.first + s.last);
+  }
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) pages += __shfl_xor(pages, off);
+  int most = max(p.least, (int)fminf(1.25f * pages * (float)a.Hkv / (float)p.groups, 1e9f) + 1);
+  const auto parts = [&](const Kv8Tiles &s) { return max(min((s.last + most - 1) / most, p.parts), 1); };
+  for (;; most += most / 4 + 1) {
+    int all = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 64) {
+      const Kv8Tiles s = seq(b0);
+      all += s.tiles * parts(s);
+    }
+    if (__builtin_amdgcn_readlane(wave_upto(all), 63) <= p.slots || most > a.cache.max_pages) break;
+  }
+  int before = 0;
+  for (int b0 = 0; b0 < a.B; b0 += 64) {
+    const Kv8Tiles s = seq(b0);
+    const int own = s.tiles * parts(s), upto = wave_upto(own);
+    const uint64_t past = __ballot(before + upto > i);
+    if (past != 0) {
+      const int at = __builtin_ctzll(past), count = __builtin_amdgcn_readlane(parts(s), at);
+      const int j = i - before - __builtin_amdgcn_readlane(upto - own, at);
+      return {b0 + at, __builtin_amdgcn_readlane(s.tiles, at) - 1 - j / count, j % count, count, most,
+              {__builtin_amdgcn_readlane(s.rows.row0, at), __builtin_amdgcn_readlane(s.rows.n, at)},
+              __builtin_amdgcn_readlane(s.kv_len, at)};
+    }
+    before += __builtin_amdgcn_readlane(upto, 63);
+  }
+  return {-1, 0, 0, 0, 0, {0, 0}, 0};
+}
+
+// A workgroup to a tile.  A few sequences' tiles come in the order of their pages, the
+// most first (under a causal mask a tile's pages go with its number, and its sequence's
+// earlier tokens count as tiles in front of it), so that the last ones to run are short:
+// with S(x) the number of tiles with x and more tiles before them, the i-th tile is among
+// those with the largest x that S(x) > i has.
+template <int kRows>
+__device__ __forceinline__ Kv8Slot kv8_slot(const Kv8Attn &a, int i, int lane) {
+  constexpr int kAll = 1 << 30;
   const int G = a.Hq / a.Hkv;
-  const Kv8Slot none{-1, 0, 0, 0, {0, 0}, 0};
+  const Kv8Slot none{-1, 0, 0, 0, 0, {0, 0}, 0};
   if (a.B > 64) {
-    const int64_t slot = i % p.slots;
-    const int b = kv8_find(a.B, lane, slot,
+    const int b = kv8_find(a.B, lane, i,
                            [&](int x) { return kv8_tile_slot((int64_t)a.cu[x] * G, x, kRows); });
     if (b < 0) return none;
     const Kv8Rows rows = kv8_rows(a.cu[b], a.cu[b + 1], a.T);
     const int64_t tiles = ((int64_t)rows.n * G + kRows - 1) / kRows;
-    const int64_t tile = tiles - 1 - (slot - kv8_tile_slot((int64_t)a.cu[b] * G, b, kRows));
+    const int64_t tile = tiles - 1 - (i - kv8_tile_slot((int64_t)a.cu[b] * G, b, kRows));
     if (tile < 0 || tile >= tiles) return none;
-    return {b, tile, i / p.slots, p.parts, rows, a.kv_len[b]};
+    return {b, tile, 0, 1, kAll, rows, a.kv_len[b]};
   }
-  const bool rising = a.causal && a.window == 0;
   int tiles = 0, before = 0, kv_len = 0;
   Kv8Rows rows{0, 0};
   if (lane < a.B) {
     rows = kv8_rows(a.cu[lane], a.cu[lane + 1], a.T);
     kv_len = a.kv_len[lane];
     tiles = (int)(((int64_t)rows.n * G + kRows - 1) / kRows);
-    if (rising)
+    if (a.causal && a.window == 0)
       before = (int)kv8_min(kv8_max(kv8_len(kv_len, a.cache.max_pages) - rows.n, 0) * G / kRows, 1 << 24);
   }
   const auto more = [&](int x) {
     return __builtin_amdgcn_readlane(wave_upto(max(min(tiles + before - x, tiles), 0)), 63);
   };
-  const int all = more(0);
-  int slot = i, part = 0, parts = p.parts;
-  if (p.parts > 1) {
-    // a tile with x before it ends before x + 2 tiles' queries and one more
-    const int whole = (int)kv8_min((int64_t)run * kKv8Page * G / kRows, 1 << 24);
-    const int split = rising ? more(max(whole - 1 - (G + kRows - 1) / kRows, 0)) : 0;
-    if (i < split * p.parts) {
-      slot = i / p.parts;
-      part = i % p.parts;
-    } else if (rising) {
-      slot = i - split * (p.parts - 1);
-      parts = 1;
-    } else if (all > 0) {
-      slot = i % all;
-      part = i / all;
-    }
-  }
-  if (slot >= all || part >= p.parts) return none;
+  if (i >= more(0)) return none;
   int x = 0, past = tiles + before;
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1) past = max(past, __shfl_xor(past, off));
   past = __builtin_amdgcn_readfirstlane(past);
   while (past - x > 1) {
     const int half = x + (past - x) / 2;
-    if (more(half) > slot)
+    if (more(half) > i)
       x = half;
     else
       past = half;
   }
-  const int rank = slot - more(x + 1);
+  const int rank = i - more(x + 1);
   const bool has = x >= before && x < before + tiles;
   const uint64_t like = __ballot(has);
   const bool mine = has && __popcll(like & ((uint64_t(1) << lane) - 1)) == rank;
   const int b = __builtin_ctzll(__ballot(mine));
-  return {b, x - __builtin_amdgcn_readlane(before, b), part, parts,
+  return {b, x - __builtin_amdgcn_readlane(before, b), 0, 1, kAll,
           {__builtin_amdgcn_readlane(rows.row0, b), __builtin_amdgcn_readlane(rows.n, b)},
           __builtin_amdgcn_readlane(kv_len, b)};
 }
@@ -161,12 +184,7 @@ struct Kv8Tile {
     const int col = lane & 31, half = lane >> 5;
     const int G = a.Hq / a.Hkv;
     h = head_k;
-    // the longest part: a quarter over a workgroup's share of all pages
-    int most = 1 << 30;
-    if (p.parts > 1)
-      most = max(p.least, (int)fminf(1.25f * kv8_tile_pages<kRows>(a, lane) * (float)a.Hkv / (float)p.groups,
-                                     1e9f) + 1);
-    const Kv8Slot at = kv8_slot<kRows>(a, p, most, i, lane);
+    const Kv8Slot at = p.parts > 1 ? kv8_part<kRows>(a, p, i, lane) : kv8_slot<kRows>(a, i, lane);
     b = at.b;
     if (b < 0) return false;
     const int64_t tile = at.tile;
@@ -177,9 +195,9 @@ struct Kv8Tile {
     const int all = rows.n * G, row0 = (int)tile * kRows + 32 * wave;
     const int q0 = (int)tile * kRows / G, q1 = min((int)(tile + 1) * kRows - 1, all - 1) / G;
     const Kv8Span span = kv8_span(len, rows.n, q0, q1 - q0 + 1, a.causal, a.window);
-    // even runs of pages, none longer than that where p.parts are enough
+    // even runs of pages
     const int count = span.p1 - span.p0;
-    const int some_parts = max(min(at.parts, (int)(((int64_t)count + most - 1) / most)), 1);
+    const int some_parts = max(min(at.parts, (int)(((int64_t)count + at.most - 1) / at.most)), 1);
     const int run = (count + some_parts - 1) / some_parts;
     part = at.part;
     parts = run == 0 ? 1 : (count + run - 1) / run;
@@ -541,16 +559,23 @@ __global__ __launch_bounds__(512, 2) void kv8_pair_kernel(Kv8Attn a, Kv8Parts pa
 
 }  // namespace detail
 
+// Workgroups of a key head: with shared tiles twice as many as run at a time (the first
+// tiles' pages may be none, so the last ones' sum may be twice the even one) and one for
+// every tile.
+static int kv8_workgroups(const Kv8Attn &a, const Kv8Parts &p, int rows) {
+  const int tiles = (int)kv8_tile_slots((int64_t)a.T * (a.Hq / a.Hkv), a.B, rows);
+  return p.parts > 1 ? tiles + 2 * p.groups / a.Hkv + 1 : tiles;
+}
 template <int DP, int DC = DP, int WAVES = 4>
 static hipError_t tile_launch(const Kv8Attn &a, Kv8Parts p, hipStream_t st) {
-  p.slots = (int)kv8_tile_slots((int64_t)a.T * (a.Hq / a.Hkv), a.B, 32 * WAVES);
-  detail::kv8_tile_kernel<DP, DC, WAVES><<<(unsigned)p.slots * p.parts * a.Hkv, 64 * WAVES, 0, st>>>(a, p);
+  p.slots = kv8_workgroups(a, p, 32 * WAVES);
+  detail::kv8_tile_kernel<DP, DC, WAVES><<<(unsigned)p.slots * a.Hkv, 64 * WAVES, 0, st>>>(a, p);
   return hipGetLastError();
 }
 template <int DP, int DC = DP>
 static hipError_t pair_launch(const Kv8Attn &a, Kv8Parts p, hipStream_t st) {
-  p.slots = (int)kv8_tile_slots((int64_t)a.T * (a.Hq / a.Hkv), a.B, 256);
-  detail::kv8_pair_kernel<DP, DC><<<(unsigned)p.slots * p.parts * a.Hkv, 512, 0, st>>>(a, p);
+  p.slots = kv8_workgroups(a, p, 256);
+  detail::kv8_pair_kernel<DP, DC><<<(unsigned)p.slots * a.Hkv, 512, 0, st>>>(a, p);
   return hipGetLastError();
 }
 

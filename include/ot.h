@@ -681,7 +681,8 @@ size_t ot_attn_kv8_workspace_size(int64_t T, int64_t B, int64_t Hq, int64_t Hkv,
  * ot_attn_kv8_plan -- which kernel configuration ot_attn_kv8 launches for these sizes
  * on the current device, as ot_qlinear_plan: "none" (T or B == 0), "few <rows> rows"
  * (16 or 32 at a time), with ", <items> items" at most where a sequence's keys are shared
- * between workgroups, or "tiles <rows>", with ", <parts> parts" at most where a tile's are.
+ * between workgroups, or "tiles <rows>" (128 or 256; small windows take 128), with
+ * ", <parts> parts" at most where a tile's are.
  */
 ot_status ot_attn_kv8_plan(int64_t T, int64_t B, int64_t Hq, int64_t Hkv,
                            int64_t D, int64_t max_q, int with_workspace,

@@ -17,6 +17,8 @@ constexpr int64_t kFewRows = 32;
 constexpr int kLeastPages = 4, kWholePages = 16, kManyPages = 128;
 // Parts of a tile's pages, at most.
 constexpr int64_t kMostParts = 64;
+// Windows below this take tiles of 128 rows.
+constexpr int64_t kWideWindow = 1500;
 
 bool few_rows(int64_t G, int64_t max_q) { return max_q * G <= kFewRows; }
 
@@ -56,6 +58,9 @@ size_t plan_split(int64_t B, int64_t Hq, int64_t Hkv, int64_t D, int64_t max_q, 
 // channels the stages of a page leave LDS for one workgroup of either: 12 prompts of 1300
 // tokens of 3 x 5 heads of 144 channels 155 against 240 (150 in products of 160 channels).
 // With 256 they leave registers for one wave to a SIMD, and 128 rows.
+// A small window leaves a tile few pages: 4096 tokens of 40 heads in one of 512 tokens 134 us
+// against 97 (6 pieces of 700-1000 tokens of 8 x 4 heads: 100 against 89; of 1024 tokens 142
+// against 139, of 2048 228 against 240).
 // Bytes of the workspace (0: none).
 size_t plan_tiles(int64_t T, int64_t B, int64_t Hq, int64_t Hkv, int64_t D, int &rows, Kv8Parts &p) {
   const int64_t G = Hq / Hkv, cus = device_cus();
@@ -100,6 +105,7 @@ hipError_t launch_attn_kv8(const Kv8Attn &a, void *workspace, hipStream_t st) {
     Kv8Parts p;
     int rows;
     const size_t bytes = plan_tiles(a.T, a.B, a.Hq, a.Hkv, a.D, rows, p);
+    if (a.window > 0 && a.window < kWideWindow && kv8_width(a.D) == 128) rows = 128;
     if (workspace == nullptr || bytes == 0 || most_pages(a, rows) <= p.whole) {
       p.parts = 1;
       return launch_kv8_tiles(a, rows, p, st);

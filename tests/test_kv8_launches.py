@@ -115,6 +115,15 @@ def test_few_rows_take_one_launch_where_tables_are_short(launch):
     assert [len(g[1]) for g in launch(calls)] == [1, 1, 1, 2]
 
 
+def test_windows_choose_launches(launch):
+    """Windows of few pages: no joining, and tiles of 128 rows."""
+    calls = [("attend", 4, 4, 8, 8, 64, 1, w, 4000, 1) for w in (1, 800, 2000)]
+    assert [len(g[1]) for g in launch(calls)] == [1, 1, 2]
+    calls = [("attend", 8192, 1, 40, 40, 112, 8192, w, 4000, ws) for w in (0, 1500, 1499, 5) for ws in (0, 1)]
+    assert [g[1][0][1][0] for g in launch(calls)] == [512] * 4 + [256] * 4
+    assert all(len(g[1]) == 1 for g in launch(calls))
+
+
 def test_plans_say_how_tiles_are_shared():
     plan, size = ot.ot_attn_kv8_plan, ot.ot_attn_kv8_workspace_size
     assert plan(64, 1, 8, 8, 128, 64, True) == "tiles 128, 64 parts" and size(64, 1, 8, 8, 128, 64) > 0

@@ -29,12 +29,19 @@ namespace ot {
 namespace detail {
 
 constexpr int kDecodeWaves = 4;
+// In how many parts the waves' outputs meet: some 8 tiles of 16 channels and rows at a time.
+constexpr int kv8_meetings(int out, int tiles) {
+  int n = (out * tiles + 7) / 8;
+  while (out % n != 0) --n;
+  return n;
+}
 constexpr int kNonTemporal = 2;  // buffer load hint: codes are read once
 
-template <int DP, int RT>
+// The first DC channels of DP.
+template <int DP, int DC, int RT>
 __global__ __launch_bounds__(64 * kDecodeWaves, kv8_decode_waves(DP, RT)) void kv8_decode_kernel(Kv8Attn a, Kv8Split s) {
-  constexpr int kChunks = DP / 64, kTail = DP % 64 / 32;  // of a key's row
-  constexpr int kSteps = DP / 32, kOut = DP / 16;
+  constexpr int kSteps = (DC + 31) / 32, kOut = DC / 16;
+  constexpr int kChunks = kSteps / 2, kTail = kSteps % 2;  // of a key's row
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int col = lane & 15, g = lane >> 4;
   const int h = blockIdx.y;
@@ -233,7 +240,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, kv8_decode_waves(DP, RT)) void k
 
   // The waves' results meet, some channels at a time; only rows that exist are written.
   constexpr int kRows = 16 * RT;
-  constexpr int kGroups = (kOut * RT + 7) / 8, kPer = kOut / kGroups, kCols = 16 * kPer;
+  constexpr int kGroups = kv8_meetings(kOut, RT), kPer = kOut / kGroups, kCols = 16 * kPer;
   static_assert(kPer * kGroups == kOut, "whole groups");
   __shared__ float meet_m[kDecodeWaves][kRows], meet_l[kDecodeWaves][kRows];
   __shared__ __attribute__((aligned(16))) float meet_o[kDecodeWaves][kRows][kCols];
@@ -447,30 +454,37 @@ __global__ __launch_bounds__(256) void kv8_join_kernel(Kv8Attn a, Kv8Parts p) {
     a.lse[row] = marked < 0 ? kNegInf : (top + log2f(sum)) * kLn2;
 }
 
-template <int DP, int RT>
+template <int DP, int DC, int RT>
 hipError_t decode_launch(const Kv8Attn &a, int64_t max_rows, const Kv8Split &s, hipStream_t st) {
   const dim3 grid((unsigned)s.items, (unsigned)a.Hkv, (unsigned)((max_rows + 16 * RT - 1) / (16 * RT)));
-  kv8_decode_kernel<DP, RT><<<grid, 64 * kDecodeWaves, 0, st>>>(a, s);
+  kv8_decode_kernel<DP, DC, RT><<<grid, 64 * kDecodeWaves, 0, st>>>(a, s);
   return hipGetLastError();
 }
 
-template <int DP>
+template <int DP, int DC = DP>
 hipError_t decode_width(const Kv8Attn &a, int64_t max_rows, const Kv8Split &s, hipStream_t st) {
   if constexpr (kv8_decode_tiles(DP, 32) == 2)
-    if (max_rows > 16) return decode_launch<DP, 2>(a, max_rows, s, st);
-  return decode_launch<DP, 1>(a, max_rows, s, st);
+    if (max_rows > 16) return decode_launch<DP, DC, 2>(a, max_rows, s, st);
+  return decode_launch<DP, DC, 1>(a, max_rows, s, st);
 }
 
 }  // namespace detail
 
 hipError_t launch_kv8_decode(const Kv8Attn &a, const Kv8Split &s, hipStream_t st) {
   const int64_t max_rows = (int64_t)a.max_q * (a.Hq / a.Hkv);
-  switch (kv8_width(a.D)) {
-    case 64: return detail::decode_width<64>(a, max_rows, s, st);
-    case 96: return detail::decode_width<96>(a, max_rows, s, st);
-    case 128: return detail::decode_width<128>(a, max_rows, s, st);
-    case 192: return detail::decode_width<192>(a, max_rows, s, st);
-    default: return detail::decode_width<256>(a, max_rows, s, st);
+  // The widths that a head's 16 channels make, but for the narrowest and the widest.
+  switch ((a.D + 15) / 16) {
+    case 5: return detail::decode_width<96, 80>(a, max_rows, s, st);
+    case 6: return detail::decode_width<96>(a, max_rows, s, st);
+    case 7: return detail::decode_width<128, 112>(a, max_rows, s, st);
+    case 8: return detail::decode_width<128>(a, max_rows, s, st);
+    case 9: return detail::decode_width<192, 144>(a, max_rows, s, st);
+    case 10: return detail::decode_width<192, 160>(a, max_rows, s, st);
+    case 11: return detail::decode_width<192, 176>(a, max_rows, s, st);
+    case 12: return detail::decode_width<192>(a, max_rows, s, st);
+    default:
+      return a.D <= 64 ? detail::decode_width<64>(a, max_rows, s, st)
+                       : detail::decode_width<256>(a, max_rows, s, st);
   }
 }
 

@@ -328,6 +328,8 @@ def test_every_width(D):
     (1, 1, 64, [i % 90 for i in range(75)], [i % 90 for i in range(75)]),  # more sequences
     (2, 1, 64, [5 + i % 9 for i in range(64)], [i % 5 for i in range(64)]),
     (300, 1, 64, [2500, 1900, 700], [3, 4, 1]),       # a tile is part of a token's heads
+    (3, 1, 64, [4] * 40 + [3000] + [5, 0] * 14 + [2900], [3] * 40 + [40] + [2, 0] * 14 + [33]),
+    (2, 1, 80, [40, 1000], [200, 150]),               # rows without a key among shared pages
     (6, 2, 16, [64 * 60 + 1, 64 * 59, 10, 64 * 40], [64 * 30, 33, 10, 200])])
 @pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 700)])
 def test_prompts_long_and_many(Hq, H, D, lengths, counts, causal, window):

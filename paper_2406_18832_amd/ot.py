@@ -1034,11 +1034,14 @@ def ot_attn_kv8(q, cu, kv_len, table, Kc, Vc, Ks, Vs, scale, causal, window, max
                      workspace, stream)
     if rc is not None:
         return _check(rc, "ot_attn_kv8")
+    window, max_q = int(window), int(max_q)
+    if max(abs(window), abs(max_q)) >= 1 << 63:
+        raise ValueError("window and max_q must fit 64 bits")
     T, Hq, D, ldq, pq = _kv8_rows(q, "q")
     pages, Hkv, pKc, pVc, pKs, pVs = _kv8_cache(Kc, Vc, Ks, Vs, D)
     B, most, pcu, plen, ptable = _kv8_batch(cu, kv_len, table, "kv_len")
     rc = lib().ot_attn_kv8(pq, ldq, T, B, Hq, Hkv, D, pcu, plen, ptable, most, pages, pKc, pVc,
-                           pKs, pVs, float(scale), int(bool(causal)), int(window), int(max_q),
+                           pKs, pVs, float(scale), int(bool(causal)), window, max_q,
                            _mx4_dev(Y, torch.float16, "Y", (T, Hq, D)),
                            _mx4_dev(lse, torch.float32, "lse", (T, Hq)),
                            _scratch(workspace,

@@ -139,6 +139,14 @@ def test_binding_refuses_host_tensors():
         ot.ot_attn_kv8(t["q"], t["cu"], t["kv_len"], t["table"], *t["cache"], 0.1, True, 0, 1, t["Y"])
 
 
+def test_binding_refuses_numbers_past_64_bits():
+    t = _tensors()
+    for window, max_q in ((2 ** 64 + 5, 1), (0, 2 ** 64 + 1), (-2 ** 64, 1)):
+        with pytest.raises(ValueError, match="64 bits"):
+            ot.ot_attn_kv8(t["q"], t["cu"], t["kv_len"], t["table"], *t["cache"], 0.1, True, window, max_q,
+                           t["Y"])
+
+
 def test_binding_names_rows_that_are_not_dense():
     t = _tensors()
     for bad in (t["k"][:, :, ::2], t["k"].transpose(1, 2), t["k"][:, ::2]):

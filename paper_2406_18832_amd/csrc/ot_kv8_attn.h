@@ -157,6 +157,9 @@ __device__ __forceinline__ int64_t kv8_partial(int64_t item, int64_t h, int64_t 
 
 }  // namespace detail
 
+// Up to so many query rows to a key head and sequence the kernel for few rows runs.
+constexpr int64_t kFewRows = 32;
+
 // The kernel for few rows: 16-row tiles that a workgroup takes (two, where a wave's
 // registers hold them: 117 sequences of 169-5610 keys of 2 x 24 heads of 144 channels 88 us
 // against 118), and the workgroups that a CU holds.

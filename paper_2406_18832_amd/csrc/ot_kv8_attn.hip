@@ -6,8 +6,6 @@
 namespace ot {
 namespace {
 
-// Up to so many query rows to a key head and sequence the kernel for few rows runs.
-constexpr int64_t kFewRows = 32;
 // Pages to an item, at least, and pages of a sequence up to which it is not split: a
 // second launch takes as long as a workgroup's waves take for so many (of tiles that leave
 // less than half of the device idle: a few per cent, which pays from kManyPages on; 1941

@@ -47,11 +47,19 @@ __global__ __launch_bounds__(64 * kDecodeWaves, kv8_decode_waves(DP, RT)) void k
   const int h = blockIdx.y;
   const int G = a.Hq / a.Hkv;
 
-  const Kv8Item item = kv8_item(a, lane, blockIdx.x, s.wanted, s.least);
+  // Where a workgroup does not take 32 rows, an item's two row tiles are eight workgroups
+  // apart, and read its pages through one L2 (30 sequences of 1000-20000 keys of 2 x 24 heads
+  // of 256 channels 109 us, one after the other 124).
+  int z = 0, number = blockIdx.x;
+  if (kv8_decode_tiles(DP, 32) == 1 && a.max_q * G > 16) {
+    z = blockIdx.x / 8 % 2;
+    number = blockIdx.x / 16 * 8 + blockIdx.x % 8;
+  }
+  const Kv8Item item = kv8_item(a, lane, number, s.wanted, s.least);
   if (item.b < 0) return;
   const Kv8Seq seq = kv8_seq(a, item.b);
-  const int rows = min(seq.rows.n, a.max_q) * G, row_base = blockIdx.z * (16 * RT);
-  if (blockIdx.z == 0 && h == 0 && item.index == 0 && threadIdx.x == 0 && s.wanted != 0)
+  const int rows = min(seq.rows.n, a.max_q) * G, row_base = z * (16 * RT);
+  if (z == 0 && h == 0 && item.index == 0 && threadIdx.x == 0 && s.wanted != 0)
     s.spans[item.b] = make_int2(item.first, item.count);
   if (row_base >= rows) return;
   const int p0 = seq.span.p0 + item.index * item.chunk;
@@ -299,7 +307,7 @@ __global__ __launch_bounds__(64 * kDecodeWaves, kv8_decode_waves(DP, RT)) void k
         if (d == 0 && a.lse != nullptr)
           a.lse[at] = empty ? kNegInf : (top + log2f(sum)) * kLn2;
       } else {
-        const int64_t at = kv8_partial(blockIdx.x, h, full, a.Hkv, s.rows);
+        const int64_t at = kv8_partial(number, h, full, a.Hkv, s.rows);
         if (d == 0) {
           s.m[at] = top;
           s.l[at] = sum;
@@ -456,7 +464,9 @@ __global__ __launch_bounds__(256) void kv8_join_kernel(Kv8Attn a, Kv8Parts p) {
 
 template <int DP, int DC, int RT>
 hipError_t decode_launch(const Kv8Attn &a, int64_t max_rows, const Kv8Split &s, hipStream_t st) {
-  const dim3 grid((unsigned)s.items, (unsigned)a.Hkv, (unsigned)((max_rows + 16 * RT - 1) / (16 * RT)));
+  static_assert(kFewRows <= 32, "two row tiles at most");
+  const bool two = max_rows > 16 * RT;
+  const dim3 grid((unsigned)(two ? (s.items + 7) / 8 * 16 : s.items), (unsigned)a.Hkv);
   kv8_decode_kernel<DP, DC, RT><<<grid, 64 * kDecodeWaves, 0, st>>>(a, s);
   return hipGetLastError();
 }

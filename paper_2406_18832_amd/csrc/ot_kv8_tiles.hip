@@ -491,8 +491,9 @@ __device__ __forceinline__ void meet() {
 // odd i: scores of page j in 2 j and 2 j + 1, values in 2 j + 2 and 2 j + 3.  The first
 // team brings K: page j + 1 in interval 2 j + 1, over page j - 1, last read in 2 j - 1.
 // The second brings V: page j + 1 in interval 2 j + 2, over page j - 1, last read in
-// 2 j + 1.  Each therefore has two stages.  (8192 tokens of 72 heads, one phase after
-// another in 256 rows: 1430 us, and 1235 so; an interval is some 2000 cycles, evenly matched.)
+// 2 j + 1.  Each therefore has two stages.  (On 8192 tokens of 72 heads 256 rows took 1430 us
+// one phase after another where the teams took 1235; an interval is some 2000 cycles, evenly
+// matched.)
 template <int DP, int DC>
 __global__ __launch_bounds__(512, 2) void kv8_pair_kernel(Kv8Attn a, Kv8Parts parts) {
   using Tile = Kv8Tile<DP, DC>;

@@ -45,7 +45,8 @@ OT_HD int64_t kv8_page_slots(int64_t T, int64_t B) { return T / kKv8Page + 2 * B
 
 // The j-th page that tokens [start, start + n) of a sequence touch: the sequence's
 // page number `col` (below 0 for a start below 0) and their places [lo, hi) in it;
-// lo >= hi where there is no such page.
+// lo >= hi where there is no such page (for any j: offsets that fall can find a slot up to
+// 2^25 and more before their sequence's first, whose distance in tokens passes 32 bits).
 struct Kv8Touch {
   int64_t col;
   int lo, hi;
@@ -53,7 +54,7 @@ struct Kv8Touch {
 OT_HD Kv8Touch kv8_touch(int64_t start, int64_t n, int64_t j) {
   const int64_t first = start >= 0 ? start / kKv8Page : -((-start + kKv8Page - 1) / kKv8Page);
   const int64_t col = first + j, at = col * kKv8Page;
-  return {col, (int)(kv8_max(start, at) - at),
+  return {col, (int)kv8_min(kv8_max(start, at) - at, kKv8Page),
           (int)kv8_max(kv8_min(start + n, at + kKv8Page) - at, -1)};
 }
 

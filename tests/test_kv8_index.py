@@ -157,3 +157,41 @@ def test_spans_hold_every_key_that_a_row_sees_and_no_page_without(lib):
             assert got[0] >= got[1]
         else:
             assert got == want, (length, n, causal, window, i0, count)
+
+
+def _found(lib, cu, slot):
+    """The sequence whose slot this is, as a wave counts them (64 at a time), or -1."""
+    b = -1
+    for b0 in range(0, len(cu) - 1, 64):
+        n = sum(lib.page_slot(L(cu[x]), L(x)) <= slot for x in range(b0, min(b0 + 64, len(cu) - 1)))
+        if n:
+            b = b0 + n - 1
+        if n < 64:
+            break
+    return b
+
+
+def test_offsets_of_any_value_touch_rows_of_the_batch_only(lib):
+    """Offsets that fall, or lie far outside the batch, can give a sequence slots far before
+    its first one: no such slot has a place, and every place has a row of the sequence."""
+    top, T = (1 << 31) - 1, 5
+    r = np.random.default_rng(7)
+    batches = [[-top - 1] * 100 + [top, -top - 1] + [top] * 29, [top] * 70 + [0],
+               [0, top, -5, top, 3, 5], [-top - 1, 5], [7] * 130 + [top]]
+    batches += [[int(x) for x in r.choice([-top - 1, -64, 0, 2, 5, 64, top], 140)] for _ in range(20)]
+    far = 0
+    for cu in batches:
+        for slot in range(lib.page_slots(L(T), L(len(cu) - 1))):
+            b = _found(lib, cu, slot)
+            if b < 0:
+                continue
+            row0, n = rows(lib, cu[b], cu[b + 1], T)
+            j = slot - lib.page_slot(L(cu[b]), L(b))
+            far += j <= -(1 << 25)
+            for start in (-top - 1, -1, 0, 64, 1 << 30, top - 63, top):
+                col, lo, hi = touch(lib, start, n, j)
+                assert 0 <= lo <= 64 and hi <= 64, (b, slot, start)
+                if lo < hi:
+                    assert row0 <= row0 + col * 64 + lo - start, (b, slot, start)
+                    assert row0 + col * 64 + hi - start <= row0 + n, (b, slot, start)
+    assert far > 0

@@ -86,6 +86,12 @@ __device__ __forceinline__ Kv8Seq kv8_seq(const Kv8Attn &a, int b) {
   s.span = kv8_span(s.len, s.rows.n, 0, s.rows.n, a.causal, a.window);
   return s;
 }
+// Whether a row at position pos of len keys sees none, and is 0.  Where the sequence has more
+// keys than its table has pages for (bad), len and with it pos are not its own: its rows are
+// NaN, also those before position 0.
+__device__ __forceinline__ bool kv8_empty(const Kv8Attn &a, int64_t len, int64_t pos, bool bad) {
+  return !bad && (len == 0 || (a.causal && pos < 0));
+}
 // Pages that count in the sharing: at least one, which writes the rows that see no key.
 __device__ __forceinline__ int kv8_shared_pages(const Kv8Seq &s) {
   return s.rows.n == 0 ? 0 : max(s.span.p1 - s.span.p0, 1);

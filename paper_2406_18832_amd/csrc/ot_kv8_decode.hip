@@ -294,7 +294,8 @@ __global__ __launch_bounds__(64 * kDecodeWaves, kv8_decode_waves(DP, RT)) void k
         const int i = full / G, head = h * G + full % G;
         const int64_t pos = seq.len - seq.rows.n + i;
         // a row that sees no key: as its position says, not as its sum does
-        const bool empty = seq.len == 0 || (a.causal && pos < 0);
+        const bool empty = kv8_empty(a, seq.len, pos, seq.bad);
+        if (seq.bad) sum = __builtin_nanf("");
         const int64_t at = (int64_t)(seq.rows.row0 + i) * a.Hq + head;
         const float scale = 1.f / sum;
         if (d < a.D) {
@@ -331,7 +332,8 @@ __global__ __launch_bounds__(256) void kv8_combine_kernel(Kv8Attn a, Kv8Split s)
   if (rows.n == 0) return;
   const int2 span = s.spans[b];
   if (span.y <= 1) return;
-  const int64_t len = kv8_len(a.kv_len[b], a.cache.max_pages);
+  const int64_t whole = a.kv_len[b], len = kv8_len(whole, a.cache.max_pages);
+  const bool bad = whole > len;
   const int mine = min(rows.n, a.max_q) * G, all = a.Hkv * mine;
   const int team = span.y > 2 * kAhead ? 4 : 1, first = team == 4 ? wave : 0;
   for (int base = blockIdx.x * (4 / team); base < all; base += gridDim.x * (4 / team)) {
@@ -398,7 +400,8 @@ __global__ __launch_bounds__(256) void kv8_combine_kernel(Kv8Attn a, Kv8Split s)
       continue;
     }
     const int i = row / G, head = h * G + row % G;
-    const bool empty = len == 0 || (a.causal && len - rows.n + i < 0);
+    const bool empty = kv8_empty(a, len, len - rows.n + i, bad);
+    if (bad) sum = __builtin_nanf("");
     const int64_t at = (int64_t)(rows.row0 + i) * a.Hq + head;
     const float scale = 1.f / sum;
 #pragma unroll

@@ -220,7 +220,7 @@ struct Kv8Tile {
       q[st] = __builtin_bit_cast(v8h, w);
     }
     const int pos = len - rows.n + qi;
-    empty = len == 0 || (a.causal && pos < 0);
+    empty = kv8_empty(a, len, pos, bad);
     key_hi = a.causal ? pos : len - 1;
     key_lo = a.window > 0 ? (int)kv8_max(pos - a.window + 1, 0) : 0;
     const int w0 = min(row0, all - 1) / G, w1 = min(row0 + 31, all - 1) / G;
@@ -366,6 +366,7 @@ struct Kv8Tile {
 
   __device__ __forceinline__ void finish(const Kv8Attn &a, const Kv8Parts &p, int half) {
     l += __shfl_xor(l, 32);
+    if (bad) l = __builtin_nanf("");  // also where the row sees none of the table's places
     if (!in) return;
     if (p.counts != nullptr && part == 0 && half == 0) p.counts[out] = empty ? -parts : parts;
     if (parts > 1) {

@@ -432,3 +432,28 @@ def test_strided_queries_and_repeats():
         for _ in range(3):
             b = ot.attn_kv8(q.contiguous(), *args, max_q=max(counts), want_lse=True)
             assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+@pytest.mark.parametrize("n,cols,max_q", [(100, 1, 100), (200, 2, 200), (1300, 18, 1300), (100, 1, 3),
+                                          (1300, 18, 2)])
+@pytest.mark.parametrize("causal,window", [(True, 0), (True, 50), (False, 0)])
+def test_rows_of_a_length_past_the_table_are_nan(n, cols, max_q, causal, window):
+    """More rows than the table has places: also those that stand before the first key of
+    the places that there are.  The next sequence is whole."""
+    r = np.random.default_rng(n + max_q)
+    cache, table = K.filled(r, [64 * cols, 40], 2, 80, slack=0)
+    assert table.shape[1] == cols
+    counts = [n, min(20, max_q)]
+    cu = K.rows_of(counts)
+    q = r.normal(size=(cu[-1], 4, 80)).astype(np.float16)
+    for length in (n, n + 500):
+        lens = np.array([length, 40])
+        want, wlse, tol, ltol = O.attend(cache, q, cu, lens, table, 0.1, causal, window)
+        for split in (False, True):
+            plan = ot.ot_attn_kv8_plan(len(q), 2, 4, 2, 80, max_q, split)
+            case(f"length past the table n={n} length={length} causal={causal} window={window} plan={plan}")
+            Y, lse = run_attend(cache, q, cu, lens, table, 0.1, causal, window, max_q, split)
+            rows = min(n, max_q)
+            assert np.isnan(Y[:rows]).all() and np.isnan(lse[:rows]).all()
+            assert (np.abs(Y[n:].astype(np.float64) - want[n:]) <= tol[n:]).all()
+            assert (np.abs(lse[n:] - wlse[n:]) <= ltol[n:]).all()

@@ -642,11 +642,13 @@ ot_status ot_kv8_read(const uint8_t *Kc, const uint8_t *Vc, const float *Ks,
  *                           window > 0 (causal calls) only j > p - window
  *   Y   = sum_j e^x_j V_j / sum_j e^x_j,    lse = log sum_j e^x_j
  * A row without a key gets Y = 0 and lse = -inf.  Products are exact, sums and the
- * softmax's statistics in fp32; its weights are rounded to fp16 for the second product,
- * whose sum is in fp32, and Y once at the end.  Keys behind the mask are never seen,
- * also where they are NaN.  A NaN that a row sees, among keys or values, makes its Y and
- * its lse NaN; a page that the pool does not have counts as NaN, and a kv_len past the
- * table makes all of its sequence's rows NaN.
+ * softmax's statistics in fp32; its weights, times their page's value scale (of a page
+ * of zeros: 2^-31), are rounded to fp16 for the second product, by 2^-11 of themselves or
+ * 2^-33 of the row's largest, whichever is more; its sum is in fp32, Y rounded once at the
+ * end.  Keys behind the mask are never seen, also where they are NaN.  A NaN that a row
+ * sees, among keys or values, makes its Y and its lse NaN; a page that the pool does not
+ * have counts as NaN, and a kv_len past the table makes all of its sequence's rows NaN,
+ * whatever they see of it.
  *   q      [T x Hq x D] fp16, rows ldq elements apart (>= Hq D, a multiple of 8).
  *   Hq     1 .. 16384, a multiple of Hkv.
  *   scale  finite (scores past fp32's range are unspecified).   window  >= 0; 0: all

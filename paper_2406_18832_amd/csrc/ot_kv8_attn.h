@@ -9,10 +9,13 @@
 // The weights 2^(x_j + l_j - m) are an operand of the matrix cores in fp16 (half a
 // step is 2^-11 of a weight).  m is set kSet binades under the largest exponent and stays
 // until a weight would pass 2^kMost: O and L are scaled anew a few times in a row's life,
-// and fp16's normal numbers reach 2^-22 of the largest, what is lost below is at most
-// 2^-33 of it for a key.  L sums the fp32 weights.  (Tiles, whose time goes by vector
-// instructions, look for the largest exponent only where the sum of a lane's weights of a
-// page, none of which is larger than it, passes kMostSum or a row has no m yet.)
+// and fp16's normal numbers reach 2^-22 of the largest weight.  Below them a weight is off
+// by at most 2^-33 of the largest; with a code of up to 127 that is 2^-26 of a step of the
+// page with the largest, whose own values are only known to half a step.  (But for a page
+// of zeros, whose values are exact: there l_j is the least that a scale has.)  L sums the
+// fp32 weights.  (Tiles, whose time goes by vector instructions, look for the largest
+// exponent only where the sum of a lane's weights of a page, none of which is larger than
+// it, passes kMostSum or a row has no m yet.)
 //
 // Which weight belongs to which token.  S^T = K Q^T has tokens as the MFMA's rows
 // and queries as its columns, and leaves a lane with weights of one query alone,
@@ -32,11 +35,13 @@ constexpr float kNegInf = -__builtin_inff();
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// A value scale's exponent and what undoes it: a page of zeros (scale 0) counts as
-// scale 1.  A NaN goes by the exponent alone, which reaches the rows that see the page
+// A value scale's exponent and what undoes it: a page of zeros (scale 0) counts as scale
+// 2^-31, below which no page's is (fp16's least number over 127).  With scale 1 a zero page
+// with a key 14 binades ahead of the others', whose values are of 1e-3 and their scales of
+// 2^-17, would take the others' weights out of fp16's normal numbers.  A NaN goes by the exponent alone, which reaches the rows that see the page
 // and no others.
 __device__ __forceinline__ void value_scale(float s, float &lg, float &inv) {
-  const float v = s == 0.f ? 1.f : s;
+  const float v = s == 0.f ? 0x1p-31f : s;
   lg = __builtin_amdgcn_logf(v);  // log2
   inv = v == v ? 1.f / v : 1.f;
 }

@@ -457,3 +457,32 @@ def test_rows_of_a_length_past_the_table_are_nan(n, cols, max_q, causal, window)
             assert np.isnan(Y[:rows]).all() and np.isnan(lse[:rows]).all()
             assert (np.abs(Y[n:].astype(np.float64) - want[n:]) <= tol[n:]).all()
             assert (np.abs(lse[n:] - wlse[n:]) <= ltol[n:]).all()
+
+
+@pytest.mark.parametrize("size", [2.0 ** -10, 2.0 ** -3, 1.0])
+@pytest.mark.parametrize("zero", [0, 20])
+@pytest.mark.parametrize("G,rows", [(32, 1), (1, 64), (2, 40)])
+def test_a_page_of_zero_values_costs_the_others_no_digits(G, rows, zero, size):
+    """A key whose score leads the others' by 0 to 30 binades, on a page whose values are all
+    0: it adds nothing to Y, and what the others add keeps its digits.  Scores and values
+    are such that Y stays among fp16's normal numbers, or near them.
+
+    The oracle's tolerance takes a weight to be off by 2^-11 of itself.  Weights below fp16's
+    normal numbers are off by 2^-25 where the largest is 2^8 or more, which is 2^-33 of the
+    largest p s (s: a page's value scale) times a code: less than N 127 2^-33 max(p s) in Y,
+    and with the zero page's s the least of all, max(p s) is one of the other pages' unless
+    it is smaller still.  For N = 2048 keys with values of 64 s and more that is below
+    2^-31 of Y's sum: within the tolerance's N 2^-23."""
+    r = np.random.default_rng(17)
+    D, N = 64, 2048
+    table, pages = K.tables(r, [N], slack=20)
+    cache = O.empty_cache(pages, 1, D, 0x5A, np.nan)
+    k = np.zeros((N, 1, D), np.float16)
+    k[64 * zero + 11, 0, 0] = 1.0
+    v = (r.uniform(0.5, 1.0, (N, 1, D)) * size).astype(np.float16)
+    v[64 * zero:64 * zero + 64] = 0
+    O.append(cache, k, v, np.array([0, N]), [N], table)
+    assert cache["Vs"][table[0, zero], 0] == 0
+    q = np.zeros((rows, G, D), np.float16)
+    q[:, :, 0] = (np.linspace(0, 30, rows * G) * np.log(2)).reshape(rows, G)
+    check_attend(cache, q, np.array([0, rows]), np.array([N]), table, scale=1.0)

@@ -486,3 +486,60 @@ def test_a_page_of_zero_values_costs_the_others_no_digits(G, rows, zero, size):
     q = np.zeros((rows, G, D), np.float16)
     q[:, :, 0] = (np.linspace(0, 30, rows * G) * np.log(2)).reshape(rows, G)
     check_attend(cache, q, np.array([0, rows]), np.array([N]), table, scale=1.0)
+
+
+def attend_on_device(cache, q, cu, kv_len, table, scale, causal, window):
+    """O.attend's results and tolerances in float64 on the GPU, for rows that all see a key
+    and caches without NaN: for more scores than the host takes in a test."""
+    T, Hq, D = q.shape
+    G = Hq // cache["Ks"].shape[1]
+    Y, tol = (torch.full((T, Hq, D), float("nan"), dtype=torch.float64, device="cuda") for _ in range(2))
+    lse, ltol = (torch.full((T, Hq), float("nan"), dtype=torch.float64, device="cuda") for _ in range(2))
+    step = 2.0 ** -23
+    for b, n in enumerate(np.diff(cu)):
+        r0, N = int(cu[b]), int(kv_len[b])
+        keys, values = (torch.from_numpy(x).cuda() for x in O.keys_values(cache, table, b, N, D))
+        see = torch.from_numpy(O.visible(n, N, causal, window)).cuda()
+        for g in range(Hq):
+            k, v, qq = keys[g // G], values[g // G], f16(q[r0:r0 + n, g]).double()
+            x = (scale * (qq @ k.t().contiguous())).masked_fill(~see, float("-inf"))
+            size = (abs(scale) * (qq.abs() @ k.abs().t().contiguous())).masked_fill(~see, 0.0)
+            p, ls = x.softmax(1), x.logsumexp(1)
+            y = p @ v
+            dx = ((D + 4) * size.amax(1) + 8 * x.amax(1).abs() + 8 * 64) * step
+            w = 2 * dx + 2.0 ** -11 + 2.0 ** -21 + N * step
+            Y[r0:r0 + n, g] = y
+            tol[r0:r0 + n, g] = (w[:, None] * (p @ v.abs()) + dx[:, None] * y.abs()
+                                 + y.abs() * 2.0 ** -11 + 2.0 ** -24)
+            lse[r0:r0 + n, g] = ls
+            ltol[r0:r0 + n, g] = dx + (N + 8 + 8 * ls.abs()) * step
+    return [t.cpu().numpy() for t in (Y, lse, tol, ltol)]
+
+
+@pytest.mark.parametrize("D,tile", [(64, 128), (112, 256), (128, 256), (160, 256)])
+@pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 8300)])
+def test_many_tiles_share_their_pages(D, tile, causal, window):
+    """Tiles for most of the device, with tables long enough that they are split all the
+    same, as the plan says; of two sequences, of which one has fewer pages."""
+    r = np.random.default_rng(D)
+    H, G, lens, counts, pad = 4, 4, [9000, 5000], [2500, 740], 10
+    table, pages = K.tables(r, lens, slack=9)
+    assert table.shape[1] > 128
+    cache = O.empty_cache(pages, H, D)
+    for n in ("Kc", "Vc"):
+        cache[n][:] = r.integers(1, 256, cache[n].shape)
+    for n in ("Ks", "Vs"):
+        cache[n][:] = r.uniform(0.001, 0.02, cache[n].shape)
+    cu, T = K.rows_of(counts), sum(counts) + pad
+    q = r.normal(size=(T, H * G, D)).astype(np.float16)
+    scale, max_q = D ** -0.5, max(counts)
+    plan = ot.ot_attn_kv8_plan(T, 2, H * G, H, D, max_q, True)
+    assert plan.startswith(f"tiles {tile}, ") and plan.endswith(" parts")
+    want, wlse, tol, ltol = attend_on_device(cache, q, cu, lens, table, scale, causal, window)
+    n = cu[-1]
+    for split in (False, True):
+        case(f"shared tiles D={D} causal={causal} window={window} split={split} plan={plan}")
+        Y, lse = run_attend(cache, q, cu, lens, table, scale, causal, window, max_q, split)
+        assert (np.abs(Y[:n].astype(np.float64) - want[:n]) <= tol[:n]).all()
+        assert (np.abs(lse[:n] - wlse[:n]) <= ltol[:n]).all()
+        assert (Y[n:] == 7.0).all() and (lse[n:] == 7.0).all()

@@ -11,7 +11,11 @@ namespace {
 // less than half of the device idle: a few per cent, which pays from kManyPages on; 1941
 // tokens of 24 heads over 9000-48000 keys, 364 tiles for 512 workgroups, 485 us against
 // 1058).  More tiles than the device takes at a time are not split (8192 tokens of 12 heads
-// of 64 channels, 768 tiles: 161 us against 200).
+// of 64 channels, 768 tiles: 161 us against 200).  Both
+// rules go by the number of tiles, not by how much longer than an even share the longest is,
+// which costs a causal prompt of about as many tiles as run at a time: 4096 tokens of 8 heads
+// of 256 channels, 256 tiles of 1 to 64 pages on 256 CUs, take 186 us, as long as without a
+// mask (190).
 constexpr int kLeastPages = 4, kWholePages = 16, kManyPages = 128;
 // Parts of a tile's pages, at most.
 constexpr int64_t kMostParts = 64;

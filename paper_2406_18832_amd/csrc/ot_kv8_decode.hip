@@ -485,7 +485,9 @@ hipError_t decode_width(const Kv8Attn &a, int64_t max_rows, const Kv8Split &s, h
 
 hipError_t launch_kv8_decode(const Kv8Attn &a, const Kv8Split &s, hipStream_t st) {
   const int64_t max_rows = (int64_t)a.max_q * (a.Hq / a.Hkv);
-  // The widths that a head's 16 channels make, but for the narrowest and the widest.
+  // The widths that a head's 16 channels make, but for the narrowest and the widest, whose
+  // time is a whole page's: 16 sequences of 8000 keys of 8 heads 89 us with 208 as with 256
+  // channels, 32 of 16 heads 95 with 16 as with 64.
   switch ((a.D + 15) / 16) {
     case 5: return detail::decode_width<96, 80>(a, max_rows, s, st);
     case 6: return detail::decode_width<96>(a, max_rows, s, st);

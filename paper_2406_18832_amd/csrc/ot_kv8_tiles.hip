@@ -5,8 +5,8 @@
 // instructions, of which five or six find a place beside each product.
 //
 // MI355X, of 1276 TFLOP/s that a large fp16 library product reaches: an 8192-token prompt
-// of 72 heads 1165-1190 us (1050 TFLOP/s of what the mask leaves); 4096-8192 tokens of 32
-// heads without a mask 1130 TFLOP/s at 128 channels, 1190 at 192, 920 at 96, 770 at 64
+// of 72 heads 1165-1270 us (1060-975 TFLOP/s of what the mask leaves; cards differ by their
+// clocks under load); 4096-8192 tokens of 32 heads without a mask 1130 TFLOP/s at 128 channels, 1190 at 192, 920 at 96, 770 at 64
 // (fewer products to a score) and 770 at 256 (registers for one wave to a SIMD).
 //
 // A workgroup takes a tile of query rows (tokens times the query heads of one key head)
@@ -582,7 +582,9 @@ static hipError_t pair_launch(const Kv8Attn &a, Kv8Parts p, hipStream_t st) {
 }
 
 hipError_t launch_kv8_tiles(const Kv8Attn &a, int rows, const Kv8Parts &p, hipStream_t st) {
-  // The widths that a head's 16 channels make, but for the narrowest and the widest.
+  // The widths that a head's 16 channels make, but for the narrowest and the widest: 4 x
+  // 2048 tokens take the same 238 us with 16 heads of 208 as of 256 channels, and with 32
+  // heads of 16, 32, 48 and 64 channels 95, 98, 101 and 102, mostly for the softmax.
   switch ((a.D + 15) / 16) {
     case 5: return tile_launch<96, 80>(a, p, st);
     case 6: return tile_launch<96>(a, p, st);

@@ -1082,7 +1082,9 @@ def attn_kv8_workspace_for(T: int, B: int, Hq: int, Hkv: int, D: int, max_q: int
 def attn_kv8(q, cu, kv_len, table, cache, scale=None, causal=True, window=0, max_q=None,
              want_lse=False, workspace=True):
     """Allocating wrapper of ot_attn_kv8.  scale: D ** -0.5 unless given; max_q: the
-    batch's rows unless given (1 for decode: the kernel for few rows is faster);
+    batch's rows unless given, as the lengths are on the device (give 1 for decode: more
+    than 32 rows to a key head go through tiles of 128 rows, 158 us against 110 for the
+    next tokens of 63 sequences of 1000 keys of 40 heads);
     workspace: True allocates one, None or False use none."""
     T, Hq, D = q.shape
     max_q = max(T, 1) if max_q is None else max_q

@@ -53,6 +53,14 @@ __device__ __forceinline__ v2h pack_half(float a, float b) {
   return v2h{(_Float16)a, (_Float16)b};  // each to nearest even
 }
 
+// A row's reference where `most` is the largest exponent of some keys and m the reference
+// so far: most - kSet where that is larger, or most itself where fp32's numbers are so far
+// apart (from exponents of 2^24 on) that the difference would pass kMost.
+__device__ __forceinline__ float raise_ref(float m, float most) {
+  const float now = fmaxf(m, most - kSet);
+  return most - now > kMost ? most : now;
+}
+
 // The maximum over the lanes of one query: xor 16 and xor 32, or xor 32 alone.  A swap
 // of a register's rows with those of its copy leaves each lane the other's value.
 __device__ __forceinline__ float max_xor16(float v) {

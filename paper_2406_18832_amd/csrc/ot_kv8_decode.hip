@@ -201,8 +201,8 @@ __global__ __launch_bounds__(64 * kDecodeWaves, kv8_decode_waves(DP, RT)) void k
 #pragma unroll
           for (int i = 0; i < 4; ++i) most = fmaxf(most, x[r][t][i]);
         most = max_xor32(max_xor16(most));
-        if (__any(most > m[r] + kMost)) {
-          const float now = most > m[r] + kMost ? most - kSet : m[r];
+        if (__any(most - m[r] > kMost)) {
+          const float now = most - m[r] > kMost ? raise_ref(m[r], most) : m[r];
           const float keep = m[r] == now ? 1.f : exp2_fast(m[r] - now);
           m[r] = now;
           l[r] *= keep;

@@ -543,3 +543,54 @@ def test_many_tiles_share_their_pages(D, tile, causal, window):
         assert (np.abs(Y[:n].astype(np.float64) - want[:n]) <= tol[:n]).all()
         assert (np.abs(lse[:n] - wlse[:n]) <= ltol[:n]).all()
         assert (Y[n:] == 7.0).all() and (lse[n:] == 7.0).all()
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("G,rows", [(8, 4), (2, 40), (12, 300)])
+def test_scores_up_to_the_largest(G, rows, D, sign):
+    """Scores of 2^18 to 2^100, whose neighbours in fp32 are up to 2^77 apart.  Where one key
+    leads by half of its score, its value is the result and its score lse; where all keys
+    have one score, the result is a mean of values.
+
+    Tolerances: a score is D + 8 products, sums and roundings of 2^-23, dx in all; Y is
+    rounded to fp16 and so are the weights (half a step each, 2^-11), N keys are summed in
+    fp32.  Of equal scores a weight is off by e^(2 dx), which for the larger ones says no
+    more than that Y lies between the values."""
+    r = np.random.default_rng(D + G)
+    N, top = 64 * 20 + 37, 64 * 9 + 5
+    table, pages = K.tables(r, [N], slack=20)
+    cu = np.array([0, rows])
+    v = K.heads_of(r, N, 1, D)
+    q = np.zeros((rows, G, D), np.float16)
+    q[:] = 1.0 + r.integers(0, 1024, (rows, G, 1)) / 1024
+    for equal in (False, True):
+        k = np.full((N, 1, D), 32.0 if equal or sign < 0 else 16.0, np.float16)
+        if not equal:
+            k[top] = 16.0 if sign < 0 else 32.0
+        cache = O.append(O.empty_cache(pages, 1, D, 0x5A, np.nan), k, v, np.array([0, N]), [N], table)
+        kk, vv = (x[0] for x in O.keys_values(cache, table, 0, N, D))
+        low, high, size = vv.min(0), vv.max(0), np.abs(vv).mean(0)
+        for lg in [*range(18, 33), 40, 100]:
+            scale = sign * 2.0 ** lg / (32 * D)
+            x = scale * (q[:, :, :1].astype(np.float64) * D) * kk[None, None, :, 0]
+            lead = x.max(2)
+            dx = (D + 8) * np.abs(lead) * 2.0 ** -23
+            step = 2.0 ** -11 + N * 2.0 ** -23
+            if equal:
+                wy, wl = vv.mean(0), lead + np.log(N)
+                tol = (np.expm1(np.minimum(2 * dx, 50))[:, :, None] + step) * size
+            else:
+                wy, wl = vv[top], lead
+                tol = step * np.abs(wy)
+            tol = tol + np.abs(wy) * 2.0 ** -11 + 2.0 ** -24
+            ltol = 3 * dx + (N + 8 * np.abs(wl)) * 2.0 ** -23
+            for split in (False, True):
+                case(f"large scores 2^{lg} sign={sign} equal={equal} D={D} G={G} rows={rows} split={split}")
+                Y, lse = run_attend(cache, q, cu, [N], table, scale, False, 0, rows, split)
+                assert np.isfinite(Y).all() and np.isfinite(lse).all(), (lg, equal, split)
+                Y = Y.astype(np.float64)
+                edge = (np.abs(vv).max(0) * 2 * step) + 2.0 ** -24
+                assert (Y >= low - edge).all() and (Y <= high + edge).all(), (lg, equal, split)
+                assert (np.abs(Y - wy) <= tol).all(), (lg, equal, split)
+                assert (np.abs(lse - wl) <= ltol).all(), (lg, equal, split)

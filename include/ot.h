@@ -651,8 +651,9 @@ ot_status ot_kv8_read(const uint8_t *Kc, const uint8_t *Vc, const float *Ks,
  * whatever they see of it.
  *   q      [T x Hq x D] fp16, rows ldq elements apart (>= Hq D, a multiple of 8).
  *   Hq     1 .. 16384, a multiple of Hkv.
- *   scale  finite (scores past fp32's range are unspecified).   window  >= 0; 0: all
- *          keys (OT_EINVAL for others, and for a window without causal).
+ *   scale  finite (scores past fp32's range are unspecified, and those of a page whose
+ *          scale times log2(e) scale is).   window  >= 0; 0: all keys (OT_EINVAL for
+ *          others, and for a window without causal).
  *   max_q  1 .. T: no sequence has more rows than this (1 for decode).  Up to 32 rows to
  *          a key head (max_q Hq / Hkv) a kernel for few rows runs, which reads the cache
  *          at memory speed; rows of a sequence past max_q may be left as they were.  A

@@ -594,3 +594,34 @@ def test_scores_up_to_the_largest(G, rows, D, sign):
                 assert (Y >= low - edge).all() and (Y <= high + edge).all(), (lg, equal, split)
                 assert (np.abs(Y - wy) <= tol).all(), (lg, equal, split)
                 assert (np.abs(lse - wl) <= ltol).all(), (lg, equal, split)
+
+
+@pytest.mark.parametrize("counts", [[1, 1], [70, 40]])
+def test_queries_and_weights_below_fp16s_normal_numbers(counts):
+    """Queries of 2^-24 to 2^-15, as exact as others; and weights of 2^-15 to 2^-23 beside a
+    leading key whose codes are 0 on a page that has others: each is off by 2^-25 at most,
+    which is 2^-33 of the leading p s, s its page's value scale."""
+    cache, q, cu, lens, table = batch(31, 4, 2, 64, [1500, 90], counts)
+    q[:] = np.clip(np.rint(q.astype(np.float64) * 128), -511, 511) * 2.0 ** -24
+    check_attend(cache, q, cu, lens, table, scale=2.0 ** 14)
+    D, N = 64, 1500
+    r = np.random.default_rng(32)
+    for lead in (12, 14, 17, 20):
+        table, pages = K.tables(r, [N], slack=20)
+        cache = O.empty_cache(pages, 1, D, 0x5A, np.nan)
+        k, v = np.zeros((N, 1, D), np.float16), r.uniform(0.5, 1.0, (N, 1, D)).astype(np.float16)
+        k[700, 0, 0] = 1.0
+        v[640:704] = 1.0
+        v[641, 0, 1] = 2.0 ** 11  # the page's scale: 2^11 / 127, next to which 1 has the code 0
+        O.append(cache, k, v, np.array([0, N]), [N], table)
+        assert (cache["Vc"][table[0, 10], 0, :D, 60] == 128).all()
+        q = np.zeros((counts[0], 2, D), np.float16)
+        q[:, :, 0] = lead * np.log(2)
+        cu = np.array([0, counts[0]])
+        want, wlse, tol, ltol = O.attend(cache, q, cu, [N], table, 1.0)
+        p = 2.0 ** lead / (2.0 ** lead + N)
+        tol = tol + N * 127 * 2.0 ** -33 * p * cache["Vs"][table[0, 10], 0]
+        for split in (False, True):
+            case(f"weights below the normal numbers lead={lead} rows={counts[0]} split={split}")
+            Y, lse = run_attend(cache, q, cu, [N], table, 1.0, True, 0, counts[0], split)
+            assert (np.abs(Y - want) <= tol).all() and (np.abs(lse - wlse) <= ltol).all()
